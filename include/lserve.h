@@ -13,6 +13,8 @@
  * caller-supplied block mask (Sec. 3.1, Sec. 3.4), lserve_sparse_prefill_paged: chunked prefill whose keys
  * and values all come from the paged cache (Sec. 2.1), and lserve_sparse_prefill_chunk: chunked prefill over
  * the history in the cache with the chunk's own K / V alongside, before their write-back (Sec. 3.2).
+ * In front of them: lserve_extend_tables (page table, positions and slots of new tokens), lserve_rotary (rotary
+ * positions), and for drafted tokens lserve_tree_masks (who descends from whom) and lserve_sparse_decode_tree (their attention).
  *
  * Conventions common to every call
  *   - "device" pointers are HIP device memory owned by the caller; "host" pointers are ordinary
@@ -419,6 +421,91 @@ int lserve_sparse_decode_noalloc(const lserve_attn_desc *desc, const lserve_page
                                  const int32_t *sel_pages, const int32_t *sel_count,
                                  const int32_t *sel_seq_len, int32_t sel_stride, void *out, float *lse_out,
                                  void *stream);
+
+/*
+ * New tokens of a batch: takes pages off a free list and writes what the calls on those tokens need, on the device, so that a
+ * serving loop need not wait for lengths on the host (Sec. 2.1 "Paged Attention"; Sec. 3.2 for the ring).  Sequence b has
+ * S_b = kv->seq_lens[b] tokens and gets n_b = new_lens[b] more (negative numbers count as 0 here).  The entries
+ * ceil(S_b / N_P) <= p < ceil((S_b + n_b) / N_P) of its row of the page table, as far as the row goes, are written with pages
+ * free_pages[0], free_pages[1], ... in the order of sequences and then of entries; other entries are left alone.
+ *
+ *   kv             page_table (written), seq_lens, batch, max_pages_per_seq; ring_table for ring_slots; pools and stats are not used
+ *   free_pages     device [num_free] (4-byte alignment will do: the rest of a longer list); pages past num_free are not there:
+ *                  their table entries become -1
+ *   total_new      host: new tokens of the batch or more (the call works on this many; with fewer the rest is left undone)
+ *   cu_new         device [batch + 1] out: running sum of n_b, as lserve_append_kv takes it (with start_pos = kv->seq_lens)
+ *   new_seq_lens   device [batch] out: S_b + n_b; not kv->seq_lens itself
+ *   pages_taken    device [1] out: pages the batch needs; more than num_free: the list was too short, and -1 is what
+ *                  table entries and slots without a page hold: not to be handed to the other calls
+ *   positions      device [total_new] out or NULL: position of every new token in its sequence
+ *   slots          device [total_new] out or NULL: page * N_P + position % N_P; -1 without a page
+ *   ring_slots     device [total_new] out or NULL: the same in the streaming heads' ring (ring_table), -1 for tokens whose page is
+ *                  neither a sink page nor a local one at length S_b + n_b
+ * Entries of the last three from cu_new[batch] on become -1.  No workspace.
+ */
+int lserve_extend_tables(const lserve_attn_desc *desc, const lserve_paged_kv *kv, const int32_t *new_lens,
+                         const int32_t *free_pages, int32_t num_free, int32_t total_new, int32_t *cu_new,
+                         int32_t *new_seq_lens, int32_t *pages_taken, int32_t *positions, int64_t *slots,
+                         int64_t *ring_slots, void *stream);
+
+/*
+ * Rotary positions (the turn applied to queries and keys before attention; keys are cached turned).  The first R = rotary_dim
+ * channels of every head are R / 2 pairs (x_a, x_b): channels i and i + R / 2, or 2 i and 2 i + 1 (interleaved).  For a token at position t
+ *   x_a' = scale (x_a cos(t f_i) - x_b sin(t f_i)),  x_b' = scale (x_b cos(t f_i) + x_a sin(t f_i)),
+ * the angle taken in 64 bits, the rest in fp32, rounded once.  Channels from R on are copied.
+ */
+typedef struct lserve_rotary_desc {
+    int32_t rotary_dim;     /* R: even, 2 .. D */
+    int32_t interleaved;    /* 0: pairs (i, i + R / 2); 1: pairs (2 i, 2 i + 1) */
+    const double *inv_freq; /* device [R / 2]: f_i, radians per position (lserve_rotary_frequencies) */
+    float scale;            /* factor on what turns, > 0; 0 means 1 */
+} lserve_rotary_desc;
+
+/*
+ *   q            device, row t at q + t * q_stride elements, H heads of D; k likewise with Hkv heads; one of the two may be NULL
+ *   q_stride     elements between the rows of two tokens: a multiple of 8, at least H * D (k_stride: Hkv * D); rows cut
+ *                out of those of a fused projection are fine
+ *   positions    device [total]; a token with a negative position is left out: its rows are not written
+ *   q_out, k_out device [total][H][D], [total][Hkv][D]; may be q / k themselves where these are dense, and must
+ *                not overlap them otherwise
+ * desc: num_q_heads, num_kv_heads, head_dim and dtype.  No workspace.
+ */
+int lserve_rotary(const lserve_attn_desc *desc, const lserve_rotary_desc *rotary, const void *q, const void *k,
+                  const int32_t *positions, int32_t total, int64_t q_stride, int64_t k_stride, void *q_out, void *k_out,
+                  void *stream);
+
+#define LSERVE_ROTARY_NONE 0       /* f_i = base^(-2 i / R) */
+#define LSERVE_ROTARY_LINEAR 1     /* f_i / factor: positions drawn together */
+#define LSERVE_ROTARY_WAVELENGTH 2 /* f_i / factor for pairs that turn at most `low` times over original_positions, f_i from `high` times on,
+                                      mixed linearly in the number of turns between */
+#define LSERVE_ROTARY_RAMP 3       /* likewise, but mixed linearly in i, from floor(i(high)) to ceil(i(low)) with i(n) the index of the pair that
+                                      turns n times; scale = 0.1 ln(factor) + 1 (the "YaRN" interpolation, arXiv 2309.00071) */
+typedef struct lserve_rotary_scaling {
+    int32_t kind; /* LSERVE_ROTARY_* */
+    int32_t rotary_dim;
+    double base;               /* > 1 */
+    double factor;             /* >= 1 (ignored for NONE) */
+    double original_positions; /* > 0, WAVELENGTH and RAMP */
+    double low, high;          /* 0 < low < high, WAVELENGTH and RAMP */
+} lserve_rotary_scaling;
+
+/* Host only: the R / 2 frequencies (HOST, out) and the factor on the result (HOST, out) of a scaling. */
+int lserve_rotary_frequencies(const lserve_rotary_scaling *scaling, double *inv_freq, float *scale);
+
+/*
+ * Ancestors of drafted tokens.  Sequence b has n_b = cu_new[b+1] - cu_new[b] of them, and parents[cu_new[b] + j] is the index (inside the
+ * sequence) of the one that token j follows, or -1 where it follows the last token of the history; parents come before
+ * their children (an entry that is not in [0, j) counts as -1).
+ *   seq_lens         device [batch]: S_b, tokens of history
+ *   max_new_per_seq  host bound of n_b, 1 .. 1024 (tokens past it are left alone)
+ *   mask_words       64-bit words of a row of tree_mask, max_new_per_seq / 64 rounded up or more
+ *   tree_mask        device [total_new][mask_words] out: bit i % 64 of word i / 64 of row cu_new[b] + j is set iff i is j or an
+ *                    ancestor of j
+ *   positions        device [total_new] out: S_b plus the number of ancestors of j
+ * Rows from cu_new[batch] on are left alone.  No workspace.
+ */
+int lserve_tree_masks(const int32_t *parents, const int32_t *cu_new, const int32_t *seq_lens, int32_t batch, int32_t total_new,
+                      int32_t max_new_per_seq, int32_t mask_words, uint64_t *tree_mask, int32_t *positions, void *stream);
 
 /*
  * Measurement aid, not part of the attention path (Sec. 3.6 defines what the decode call reads): issues the reads

@@ -23,7 +23,9 @@ from .binding import (  # noqa: F401
     lserve_sparse_prefill_paged,
     lserve_sparse_prefill_chunk,
     lserve_build_page_stats,
+    RotaryDesc,
     lserve_chunk_scratch_bytes,
+    lserve_extend_tables,
     lserve_init,
     lserve_last_hip_error,
     lserve_probe_decode_read,
@@ -31,10 +33,13 @@ from .binding import (  # noqa: F401
     lserve_probe_prefill_longest_first,
     lserve_probe_prefill_plan,
     lserve_probe_prefill_shape,
+    lserve_rotary,
+    lserve_rotary_frequencies,
     lserve_select_pages,
     lserve_sparse_decode,
     lserve_sparse_decode_noalloc,
     lserve_sparse_prefill,
     lserve_strerror,
+    lserve_tree_masks,
     lserve_workspace_bytes,
 )

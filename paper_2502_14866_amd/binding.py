@@ -45,6 +45,11 @@ EXPORTED_SYMBOLS = (
     "lserve_probe_prefill_plan",
     "lserve_probe_prefill_longest_first",
     "lserve_probe_mask_walk",
+    "lserve_extend_tables",
+    "lserve_rotary",
+    "lserve_rotary_frequencies",
+    "RotaryDesc",
+    "lserve_tree_masks",
 )
 
 
@@ -81,6 +86,15 @@ class _CBlockMask(ctypes.Structure):
         ("cols", ctypes.c_void_p),
         ("num_masks", ctypes.c_int32), ("rows_per_mask", ctypes.c_int32), ("nnz", ctypes.c_int32),
     ]
+
+
+class _CRotaryDesc(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("inv_freq", ctypes.c_void_p), ("scale", ctypes.c_float)]
+
+
+class _CRotaryScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_positions", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double)]
 
 
 def library_path() -> str:
@@ -138,6 +152,15 @@ def load_library():
         lib.lserve_probe_prefill_longest_first.restype = ctypes.c_int
         lib.lserve_probe_mask_walk.argtypes = [dp, i32, i32, i32, i32, i32, i32, ctypes.POINTER(i32)]
         lib.lserve_probe_mask_walk.restype = ctypes.c_int
+        lib.lserve_extend_tables.argtypes = [dp, kp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+        lib.lserve_extend_tables.restype = ctypes.c_int
+        i64 = ctypes.c_int64
+        lib.lserve_rotary.argtypes = [dp, ctypes.POINTER(_CRotaryDesc), vp, vp, vp, i32, i64, i64, vp, vp, vp]
+        lib.lserve_rotary.restype = ctypes.c_int
+        lib.lserve_rotary_frequencies.argtypes = [ctypes.POINTER(_CRotaryScaling), vp, vp]
+        lib.lserve_rotary_frequencies.restype = ctypes.c_int
+        lib.lserve_tree_masks.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
+        lib.lserve_tree_masks.restype = ctypes.c_int
         lib.lserve_init.argtypes = []
         lib.lserve_init.restype = ctypes.c_int
         for name in ("lserve_build_page_stats", "lserve_select_pages", "lserve_sparse_prefill",
@@ -503,3 +526,124 @@ def lserve_probe_mask_walk(desc: AttnDesc, batch: int, total_tokens: int, max_se
     _check(load_library().lserve_probe_mask_walk(desc.c(), batch, total_tokens, max_seqlen, num_masks, rows_per_mask, nnz,
                                                  ctypes.byref(walk)), "lserve_probe_mask_walk")
     return walk.value
+
+
+def _checked(where: str, *args) -> None:
+    """(tensor or None, type or types, least number of elements) each: what the library cannot see from an address."""
+    device = None
+    for t, kinds, least in args:
+        if t is None:
+            continue
+        if t.dtype not in (kinds if isinstance(kinds, tuple) else (kinds,)):
+            raise ValueError(f"{where}: a tensor of {t.dtype} where {kinds} is taken")
+        if t.numel() < least:
+            raise ValueError(f"{where}: a tensor of {t.numel()} elements where {least} are read or written")
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError(f"{where}: tensors on {device} and {t.device}")
+    if device is not None and device.type == "cuda" and device.index != torch.cuda.current_device():
+        raise ValueError(f"{where}: tensors on {device} while device {torch.cuda.current_device()} is current")
+
+
+def lserve_extend_tables(desc: AttnDesc, kv: PagedKV, new_lens: torch.Tensor, free_pages: Optional[torch.Tensor], cu_new: torch.Tensor,
+                         new_seq_lens: torch.Tensor, pages_taken: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                         slots: Optional[torch.Tensor] = None, ring_slots: Optional[torch.Tensor] = None, stream=None,
+                         total_new: Optional[int] = None) -> None:
+    """total_new: new tokens of the batch or more, the length of positions, slots and ring_slots (and taken from the first of
+    them that is given)."""
+    if total_new is None:
+        given = positions if positions is not None else slots if slots is not None else ring_slots
+        if given is None:
+            raise ValueError("lserve_extend_tables: total_new, where no positions or slots are asked for")
+        total_new = given.numel()
+    batch, i32, i64 = kv.page_table.shape[0], torch.int32, torch.int64
+    _checked("lserve_extend_tables", (kv.page_table, i32, 0), (kv.seq_lens, i32, batch), (kv.ring_table, i32, 0), (new_lens, i32, batch),
+             (free_pages, i32, 0), (cu_new, i32, batch + 1), (new_seq_lens, i32, batch), (pages_taken, i32, 1),
+             (positions, i32, total_new), (slots, i64, total_new), (ring_slots, i64, total_new))
+    if ring_slots is not None and kv.ring_table is not None:
+        ring = -(-desc.sink_tokens // desc.page_size) - (-desc.local_tokens // desc.page_size)
+        if kv.ring_table.numel() < batch * ring:
+            raise ValueError(f"lserve_extend_tables: a ring table of {kv.ring_table.numel()} entries for {batch} sequences of {ring}")
+    _check(load_library().lserve_extend_tables(
+        desc.c(), kv.c(), _ptr(new_lens), _ptr(free_pages), 0 if free_pages is None else free_pages.numel(), total_new, _ptr(cu_new),
+        _ptr(new_seq_lens), _ptr(pages_taken), _ptr(positions), _ptr(slots), _ptr(ring_slots), _stream(stream)), "lserve_extend_tables")
+
+
+_SCALINGS = ("none", "linear", "wavelength", "ramp")
+
+
+def lserve_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                              original_positions: float = 8192.0, low: float = 1.0, high: float = 4.0) -> tuple:
+    """(rotary_dim / 2 frequencies, radians per position, float64 on the host; factor on what turns)."""
+    if scaling not in _SCALINGS:
+        raise ValueError(f"scaling is one of {_SCALINGS}")
+    out = torch.empty((max(1, rotary_dim // 2),), dtype=torch.float64)
+    loud = ctypes.c_float()
+    c = _CRotaryScaling(_SCALINGS.index(scaling), rotary_dim, base, factor, original_positions, low, high)
+    _check(load_library().lserve_rotary_frequencies(ctypes.byref(c), out.data_ptr(), ctypes.addressof(loud)), "lserve_rotary_frequencies")
+    return out, loud.value
+
+
+@dataclass
+class RotaryDesc:
+    """Mirror of lserve_rotary_desc: how the heads of a layer turn.  The frequencies are those of lserve_rotary_frequencies, or the
+    caller's own (inv_freq: float64 [rotary_dim / 2], radians per position), kept on `device` (the current GPU)."""
+    rotary_dim: int = 128
+    interleaved: bool = False
+    base: float = 10000.0
+    scaling: str = "none"
+    factor: float = 1.0
+    original_positions: float = 8192.0
+    low: float = 1.0
+    high: float = 4.0
+    scale: float = 0.0  # 0: what the scaling gives
+    inv_freq: Optional[torch.Tensor] = None
+    device: Optional[object] = None
+
+    def __post_init__(self):
+        if self.inv_freq is None:
+            self.inv_freq, loud = lserve_rotary_frequencies(self.rotary_dim, self.base, self.scaling, self.factor,
+                                                            self.original_positions, self.low, self.high)
+            self.scale = self.scale or loud
+        if self.inv_freq.dtype != torch.float64 or self.inv_freq.numel() < self.rotary_dim // 2:
+            raise ValueError("RotaryDesc: inv_freq holds rotary_dim / 2 numbers of 64 bits")
+        where = self.device if self.device is not None else ("cuda" if torch.cuda.is_available() else "cpu")
+        self.inv_freq = self.inv_freq.to(where).contiguous()
+        self._c = _CRotaryDesc(self.rotary_dim, int(self.interleaved), self.inv_freq.data_ptr(), float(self.scale))
+
+    def c(self):
+        return ctypes.byref(self._c)
+
+
+def _rows(t: Optional[torch.Tensor], heads: int, dim: int, what: str) -> tuple:
+    """(address, elements between two rows) of [total][heads][dim] whose rows may lie apart."""
+    if t is None:
+        return None, 0
+    if t.dim() != 3 or t.shape[1:] != (heads, dim) or t.stride(2) != 1 or t.stride(1) != dim:
+        raise ValueError(f"lserve_rotary: {what} is [total][{heads}][{dim}], heads next to each other")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+def lserve_rotary(desc: AttnDesc, rotary: RotaryDesc, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor,
+                  q_out: Optional[torch.Tensor], k_out: Optional[torch.Tensor], stream=None) -> None:
+    """q and k may be cut out of the rows of a fused projection (any distance between rows that is a multiple of eight elements)."""
+    total = positions.numel()
+    dim, hq, hkv = desc.head_dim, desc.num_q_heads, desc.num_kv_heads
+    q_at, q_stride = _rows(q, hq, dim, "q")
+    k_at, k_stride = _rows(k, hkv, dim, "k")
+    _checked("lserve_rotary", (positions, torch.int32, 1), (rotary.inv_freq, torch.float64, rotary.rotary_dim // 2),
+             (q, desc.dtype, total * hq * dim), (q_out, desc.dtype, total * hq * dim),
+             (k, desc.dtype, total * hkv * dim), (k_out, desc.dtype, total * hkv * dim))
+    _check(load_library().lserve_rotary(desc.c(), rotary.c(), q_at, k_at, _ptr(positions), total, q_stride, k_stride, _ptr(q_out),
+                                        _ptr(k_out), _stream(stream)), "lserve_rotary")
+
+
+def lserve_tree_masks(parents: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor, max_new_per_seq: int,
+                      tree_mask: torch.Tensor, positions: torch.Tensor, stream=None) -> None:
+    """tree_mask: int64 [total_new][words], 64 drafted tokens to a word."""
+    total, batch, words = parents.numel(), cu_new.numel() - 1, tree_mask.shape[-1]
+    _checked("lserve_tree_masks", (parents, torch.int32, 1), (cu_new, torch.int32, 2), (seq_lens, torch.int32, batch),
+             (tree_mask, torch.int64, total * words), (positions, torch.int32, total))
+    _check(load_library().lserve_tree_masks(_ptr(parents), _ptr(cu_new), _ptr(seq_lens), batch, total, max_new_per_seq, words,
+                                            _ptr(tree_mask), _ptr(positions), _stream(stream)), "lserve_tree_masks")

@@ -14,7 +14,8 @@ LIB_PATH = os.path.join(HERE, "liblserve.so")
 # the binding's native marshalling (host code only), under a name that other versions of Python do not take for theirs
 CALLS_PATH = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 
-SOURCES = ["lserve_api.hip", "page_stats.hip", "select_pages.hip", "sparse_decode.hip", "sparse_prefill.hip"]
+SOURCES = ["lserve_api.hip", "page_stats.hip", "select_pages.hip", "sparse_decode.hip", "sparse_prefill.hip", "batch_tables.hip",
+           "rotary.hip"]
 
 # Packed fp32 VALU forms are switched off for the device pass; the host pass does not know the
 # feature and says so, which is harmless.

@@ -87,4 +87,31 @@ hipError_t launch_sparse_prefill(int dtype, const LayerParams& lp, const void* q
                                  const int* cu_seqlens, int batch, int total_tokens, int max_seqlen, void* out,
                                  float* lse_out, void* workspace, const PrefillMaskArgs* mask, hipStream_t stream);
 
+// New tokens of a batch (lserve_extend_tables); positions, slots and ring_slots may be null.
+struct ExtendArgs {
+    int* page_table;
+    const int *seq_lens, *new_lens, *free_pages, *ring_table;
+    int *cu_new, *new_seq_lens, *pages_taken, *positions;
+    long long *slots, *ring_slots;
+    int batch, max_pages, num_free, total, page_log2, sink_pages, local_pages;
+};
+constexpr int kMaxTreeNodes = 1024;  // drafted tokens of a sequence
+hipError_t preload_table_kernels();
+hipError_t launch_extend_tables(const ExtendArgs& args, hipStream_t stream);
+hipError_t launch_tree_masks(const int* parents, const int* cu_new, const int* seq_lens, int batch, int total_new, int max_new, int mask_words,
+                             unsigned long long* tree_mask, int* positions, hipStream_t stream);
+
+// Rotary positions (lserve_rotary); q or k may be null, strides in elements.
+struct RotaryArgs {
+    const void *q, *k;
+    void *q_out, *k_out;
+    const int* positions;
+    const double* inv_freq;
+    long long q_stride, k_stride;
+    int heads_q, heads_k, total, rotary_dim, interleaved;
+    float scale;
+};
+hipError_t preload_rotary_kernels();
+hipError_t launch_rotary(int dtype, const RotaryArgs& args, hipStream_t stream);
+
 }  // namespace lserve

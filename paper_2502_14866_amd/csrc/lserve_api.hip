@@ -456,6 +456,121 @@ int lserve_sparse_decode_noalloc(const lserve_attn_desc* desc, const lserve_page
     return e == hipSuccess ? LSERVE_OK : fail_hip(e);
 }
 
+int lserve_extend_tables(const lserve_attn_desc* desc, const lserve_paged_kv* kv, const int32_t* new_lens, const int32_t* free_pages,
+                         int32_t num_free, int32_t total_new, int32_t* cu_new, int32_t* new_seq_lens, int32_t* pages_taken,
+                         int32_t* positions, int64_t* slots, int64_t* ring_slots, void* stream) {
+    LayerParams lp;
+    const int rc = make_layer(desc, &lp);
+    if (rc) return rc;
+    if (!kv || !kv->page_table || !kv->seq_lens || kv->batch <= 0 || kv->max_pages_per_seq <= 0) return LSERVE_ERR_INVALID_ARG;
+    if (kv->batch > 65535) return LSERVE_ERR_UNSUPPORTED;
+    if (!new_lens || num_free < 0 || (num_free > 0 && !free_pages) || total_new < 0 || !cu_new || !new_seq_lens || !pages_taken)
+        return LSERVE_ERR_INVALID_ARG;
+    if (new_seq_lens == kv->seq_lens || (ring_slots && !kv->ring_table)) return LSERVE_ERR_INVALID_ARG;
+    if (!aligned16(kv->page_table) || !aligned16(kv->seq_lens) || !aligned16(kv->ring_table) || !aligned16(new_lens) ||
+        (reinterpret_cast<uintptr_t>(free_pages) & 3u) != 0 || !aligned16(cu_new) || !aligned16(new_seq_lens) || !aligned16(pages_taken) || !aligned16(positions) ||
+        !aligned16(slots) || !aligned16(ring_slots))
+        return LSERVE_ERR_INVALID_ARG;
+    ExtendArgs a = {};
+    a.page_table = const_cast<int*>(kv->page_table);  // device memory of the caller's, which only this call writes
+    a.seq_lens = kv->seq_lens;
+    a.new_lens = new_lens;
+    a.free_pages = free_pages;
+    a.ring_table = kv->ring_table;
+    a.cu_new = cu_new;
+    a.new_seq_lens = new_seq_lens;
+    a.pages_taken = pages_taken;
+    a.positions = positions;
+    a.slots = (long long*)slots;
+    a.ring_slots = (long long*)ring_slots;
+    a.batch = kv->batch;
+    a.max_pages = kv->max_pages_per_seq;
+    a.num_free = num_free;
+    a.total = total_new;
+    a.page_log2 = __builtin_ctz((unsigned)lp.NP);
+    a.sink_pages = lp.sink_pages;
+    a.local_pages = lp.local_pages;
+    const hipError_t e = launch_extend_tables(a, (hipStream_t)stream);
+    return e == hipSuccess ? LSERVE_OK : fail_hip(e);
+}
+
+int lserve_rotary(const lserve_attn_desc* desc, const lserve_rotary_desc* rotary, const void* q, const void* k, const int32_t* positions,
+                  int32_t total, int64_t q_stride, int64_t k_stride, void* q_out, void* k_out, void* stream) {
+    LayerParams lp;
+    const int rc = make_layer(desc, &lp);
+    if (rc) return rc;
+    if (!rotary || !rotary->inv_freq || !positions || total <= 0 || (!q && !k) || !q != !q_out || !k != !k_out) return LSERVE_ERR_INVALID_ARG;
+    if (rotary->rotary_dim < 2 || rotary->rotary_dim % 2 != 0) return LSERVE_ERR_INVALID_ARG;
+    if (!(rotary->scale >= 0.f) || std::isinf(rotary->scale) || (rotary->interleaved != 0 && rotary->interleaved != 1))
+        return LSERVE_ERR_INVALID_ARG;
+    if (rotary->rotary_dim > kHeadDim) return LSERVE_ERR_UNSUPPORTED;
+    const int64_t q_row = (int64_t)lp.H * kHeadDim, k_row = (int64_t)lp.Hkv * kHeadDim;
+    if (q && (q_stride < q_row || q_stride % 8 != 0 || (q_out == q && q_stride != q_row))) return LSERVE_ERR_INVALID_ARG;
+    if (k && (k_stride < k_row || k_stride % 8 != 0 || (k_out == k && k_stride != k_row))) return LSERVE_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(positions) || !aligned16(rotary->inv_freq))
+        return LSERVE_ERR_INVALID_ARG;
+    RotaryArgs a = {};
+    a.q = q;
+    a.k = k;
+    a.q_out = q_out;
+    a.k_out = k_out;
+    a.positions = positions;
+    a.inv_freq = rotary->inv_freq;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.heads_q = q ? lp.H : 0;
+    a.heads_k = k ? lp.Hkv : 0;
+    a.total = total;
+    a.rotary_dim = rotary->rotary_dim;
+    a.interleaved = rotary->interleaved;
+    a.scale = rotary->scale == 0.f ? 1.f : rotary->scale;
+    const hipError_t e = launch_rotary(desc->dtype, a, (hipStream_t)stream);
+    return e == hipSuccess ? LSERVE_OK : fail_hip(e);
+}
+
+int lserve_rotary_frequencies(const lserve_rotary_scaling* s, double* inv_freq, float* scale) {
+    if (!s || !inv_freq || !scale || s->rotary_dim < 2 || s->rotary_dim % 2 != 0) return LSERVE_ERR_INVALID_ARG;
+    if (s->rotary_dim > kHeadDim || s->kind < LSERVE_ROTARY_NONE || s->kind > LSERVE_ROTARY_RAMP) return LSERVE_ERR_UNSUPPORTED;
+    const bool stretched = s->kind != LSERVE_ROTARY_NONE, by_turns = s->kind == LSERVE_ROTARY_WAVELENGTH || s->kind == LSERVE_ROTARY_RAMP;
+    if (!(s->base > 1.0) || std::isinf(s->base)) return LSERVE_ERR_INVALID_ARG;
+    if (stretched && (!(s->factor >= 1.0) || std::isinf(s->factor))) return LSERVE_ERR_INVALID_ARG;
+    if (by_turns && (!(s->original_positions > 0.0) || std::isinf(s->original_positions) || !(s->low > 0.0) || !(s->high > s->low) ||
+                     std::isinf(s->high)))
+        return LSERVE_ERR_INVALID_ARG;
+    const double kTurn = 6.283185307179586476925, R = s->rotary_dim;
+    // index (not a whole number) of the pair that turns n times over the original positions
+    auto index_of = [&](double n) { return R * std::log(s->original_positions / (n * kTurn)) / (2.0 * std::log(s->base)); };
+    double first = 0.0, last = 0.0;
+    if (s->kind == LSERVE_ROTARY_RAMP) {
+        first = std::fmax(std::floor(index_of(s->high)), 0.0);
+        last = std::fmin(std::ceil(index_of(s->low)), R - 1.0);
+    }
+    for (int i = 0; i < s->rotary_dim / 2; ++i) {
+        const double f = std::pow(s->base, -2.0 * i / R);
+        double kept = 1.0;  // share of the frequency as it is; the rest is f / factor
+        if (s->kind == LSERVE_ROTARY_LINEAR) kept = 0.0;
+        if (s->kind == LSERVE_ROTARY_WAVELENGTH) kept = (s->original_positions * f / kTurn - s->low) / (s->high - s->low);
+        if (s->kind == LSERVE_ROTARY_RAMP) kept = 1.0 - (i - first) / std::fmax(last - first, 0.001);
+        kept = std::fmin(std::fmax(kept, 0.0), 1.0);
+        inv_freq[i] = kept == 1.0 ? f : f * kept + f / s->factor * (1.0 - kept);
+    }
+    *scale = s->kind == LSERVE_ROTARY_RAMP ? (float)(0.1 * std::log(s->factor) + 1.0) : 1.f;
+    return LSERVE_OK;
+}
+
+int lserve_tree_masks(const int32_t* parents, const int32_t* cu_new, const int32_t* seq_lens, int32_t batch, int32_t total_new,
+                      int32_t max_new_per_seq, int32_t mask_words, uint64_t* tree_mask, int32_t* positions, void* stream) {
+    if (!parents || !cu_new || !seq_lens || !tree_mask || !positions) return LSERVE_ERR_INVALID_ARG;
+    if (batch <= 0 || total_new <= 0 || max_new_per_seq <= 0 || max_new_per_seq > total_new || mask_words < (max_new_per_seq + 63) / 64)
+        return LSERVE_ERR_INVALID_ARG;
+    if (batch > 65535 || max_new_per_seq > kMaxTreeNodes) return LSERVE_ERR_UNSUPPORTED;
+    if (!aligned16(parents) || !aligned16(cu_new) || !aligned16(seq_lens) || !aligned16(tree_mask) || !aligned16(positions))
+        return LSERVE_ERR_INVALID_ARG;
+    const hipError_t e = launch_tree_masks(parents, cu_new, seq_lens, batch, total_new, max_new_per_seq, mask_words,
+                                           (unsigned long long*)tree_mask, positions, (hipStream_t)stream);
+    return e == hipSuccess ? LSERVE_OK : fail_hip(e);
+}
+
 int lserve_probe_decode_read(const lserve_attn_desc* desc, const lserve_paged_kv* kv, const int32_t* sel_pages,
                              const int32_t* sel_count, const int32_t* sel_seq_len, int32_t sel_stride, void* stream) {
     LayerParams lp;
@@ -498,6 +613,8 @@ int lserve_init(void) {
     if (e == hipSuccess) e = preload_select_kernels();
     if (e == hipSuccess) e = preload_prefill_kernels();
     if (e == hipSuccess) e = preload_decode_kernels();
+    if (e == hipSuccess) e = preload_table_kernels();
+    if (e == hipSuccess) e = preload_rotary_kernels();
     return e == hipSuccess ? LSERVE_OK : fail_hip(e);
 }
 
