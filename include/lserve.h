@@ -508,6 +508,41 @@ int lserve_tree_masks(const int32_t *parents, const int32_t *cu_new, const int32
                       int32_t max_new_per_seq, int32_t mask_words, uint64_t *tree_mask, int32_t *positions, void *stream);
 
 /*
+ * Attention of drafted tokens (speculative decoding): a decode step (lserve_sparse_decode) of n_b = cu_new[b+1] - cu_new[b] tokens per
+ * sequence at once, which form a tree.  Sequence b has S_b = kv->seq_lens[b] tokens of history in the cache (S_b >= 0 here), and
+ * Q, K and V of its drafted tokens arrive alongside; nothing is written to the cache: call lserve_append_kv with the tokens that were
+ * accepted afterwards.  Drafted token j, at position t_j = positions[cu_new[b] + j] >= S_b, attends
+ *   history:        the pages that a decode step at position t_j attends: of a streaming head the tiles p < s and
+ *                   p > tile(t_j) - w; of a selecting head sel_pages[b][hk][0 .. sel_count) and every page from ceil(sel_seq_len[b] / N_P)
+ *                   on, or all pages where sel_pages is NULL; tokens u < S_b of them;
+ *   drafted tokens: those whose bit in row j of tree_mask is set (lserve_tree_masks sets its own and its ancestors'); of a
+ *                   streaming head only those with tile(t_i) < s or tile(t_i) > tile(t_j) - w.
+ * tree_mask = positions = NULL: a chain, token j at position S_b + j after token j - 1.  A token that attends nothing gets out = 0 and
+ * lse = -inf.  What a token does not attend, be it not a number, leaves no trace in its result.
+ *
+ *   kv              N_P = 64; one pool or the two-way cache, pages of 16-bit rows or quantised (kv_bits 8 or 4: keys enter as code *
+ *                   scale + zero in fp32, values rounded to the layer's type).  stats are not used
+ *   q               device [total_new][H][D]; k_new, v_new device [total_new][Hkv][D]
+ *   cu_new          device [batch + 1] (batch = kv->batch), cu_new[0] = 0, n_b >= 0; rows from cu_new[batch] on are left alone
+ *   max_new_per_seq host bound of n_b, 1 .. 1024
+ *   tree_mask       device [total_new][mask_words] (64 tokens to a word, max_new_per_seq / 64 rounded up words or more); positions device
+ *                   [total_new]; both or neither
+ *   sel_pages, sel_count, sel_seq_len, sel_stride: as in lserve_sparse_decode, or all three NULL (sel_stride is then 0)
+ *   out             device [total_new][H][D]; lse_out device [total_new][H] fp32 or NULL
+ *   workspace       device, lserve_tree_workspace_bytes(...) for these sizes or more, any contents; calls that may run at the same time
+ *                   need one each
+ */
+int lserve_sparse_decode_tree(const lserve_attn_desc *desc, const lserve_paged_kv *kv, const void *q, const void *k_new,
+                              const void *v_new, const int32_t *cu_new, const uint64_t *tree_mask, int32_t mask_words,
+                              const int32_t *positions, const int32_t *sel_pages, const int32_t *sel_count,
+                              const int32_t *sel_seq_len, int32_t sel_stride, int32_t total_new, int32_t max_new_per_seq, void *out,
+                              float *lse_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace of lserve_sparse_decode_tree (0 on invalid arguments, or where none is needed). */
+size_t lserve_tree_workspace_bytes(const lserve_attn_desc *desc, int32_t batch, int32_t total_new, int32_t max_new_per_seq,
+                                   int32_t max_pages_per_seq, int32_t sel_stride);
+
+/*
  * Measurement aid, not part of the attention path (Sec. 3.6 defines what the decode call reads): issues the reads
  * of lserve_sparse_decode for the same arguments (the K and V slabs of every page the index tables of the batch
  * list, through the same page tables) from one short workgroup per table entry, and discards the data.  Nothing

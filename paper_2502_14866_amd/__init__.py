@@ -38,8 +38,10 @@ from .binding import (  # noqa: F401
     lserve_select_pages,
     lserve_sparse_decode,
     lserve_sparse_decode_noalloc,
+    lserve_sparse_decode_tree,
     lserve_sparse_prefill,
     lserve_strerror,
     lserve_tree_masks,
+    lserve_tree_workspace_bytes,
     lserve_workspace_bytes,
 )

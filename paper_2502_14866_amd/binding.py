@@ -50,6 +50,8 @@ EXPORTED_SYMBOLS = (
     "lserve_rotary_frequencies",
     "RotaryDesc",
     "lserve_tree_masks",
+    "lserve_sparse_decode_tree",
+    "lserve_tree_workspace_bytes",
 )
 
 
@@ -161,6 +163,10 @@ def load_library():
         lib.lserve_rotary_frequencies.restype = ctypes.c_int
         lib.lserve_tree_masks.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
         lib.lserve_tree_masks.restype = ctypes.c_int
+        lib.lserve_sparse_decode_tree.argtypes = [dp, kp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
+        lib.lserve_sparse_decode_tree.restype = ctypes.c_int
+        lib.lserve_tree_workspace_bytes.argtypes = [dp, i32, i32, i32, i32, i32]
+        lib.lserve_tree_workspace_bytes.restype = sz
         lib.lserve_init.argtypes = []
         lib.lserve_init.restype = ctypes.c_int
         for name in ("lserve_build_page_stats", "lserve_select_pages", "lserve_sparse_prefill",
@@ -647,3 +653,29 @@ def lserve_tree_masks(parents: torch.Tensor, cu_new: torch.Tensor, seq_lens: tor
              (tree_mask, torch.int64, total * words), (positions, torch.int32, total))
     _check(load_library().lserve_tree_masks(_ptr(parents), _ptr(cu_new), _ptr(seq_lens), batch, total, max_new_per_seq, words,
                                             _ptr(tree_mask), _ptr(positions), _stream(stream)), "lserve_tree_masks")
+
+
+def lserve_tree_workspace_bytes(desc: AttnDesc, batch: int, total_new: int, max_new_per_seq: int, max_pages_per_seq: int,
+                                sel_stride: int = 0) -> int:
+    return int(load_library().lserve_tree_workspace_bytes(desc.c(), batch, total_new, max_new_per_seq, max_pages_per_seq, sel_stride))
+
+
+def lserve_sparse_decode_tree(desc: AttnDesc, kv: PagedKV, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                              cu_new: torch.Tensor, max_new_per_seq: int, out: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
+                              tree_mask: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                              sel_pages: Optional[torch.Tensor] = None, sel_count: Optional[torch.Tensor] = None,
+                              sel_seq_len: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """tree_mask: int64 [total_new][words], 64 drafted tokens to a word; without it and positions the drafted tokens are a chain.
+    Without sel_pages, sel_count and sel_seq_len selecting heads attend the whole history."""
+    total, batch, i32 = q.shape[0], kv.page_table.shape[0], torch.int32
+    dim, hq, hkv, dt = desc.head_dim, desc.num_q_heads, desc.num_kv_heads, desc.dtype
+    words = 0 if tree_mask is None else tree_mask.shape[-1]
+    stride = 0 if sel_pages is None else sel_pages.shape[-1]
+    _checked("lserve_sparse_decode_tree", (q, dt, total * hq * dim), (k_new, dt, total * hkv * dim), (v_new, dt, total * hkv * dim),
+             (out, dt, total * hq * dim), (lse_out, torch.float32, total * hq), (cu_new, i32, batch + 1), (kv.seq_lens, i32, batch),
+             (kv.page_table, i32, 0), (kv.k_pool, (dt, torch.uint8), 0), (tree_mask, torch.int64, total * words), (positions, i32, total),
+             (sel_pages, i32, batch * hkv * stride), (sel_count, i32, batch * hkv), (sel_seq_len, i32, batch))
+    _check(load_library().lserve_sparse_decode_tree(
+        desc.c(), kv.c(), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(cu_new), _ptr(tree_mask), words, _ptr(positions), _ptr(sel_pages),
+        _ptr(sel_count), _ptr(sel_seq_len), stride, total, max_new_per_seq, _ptr(out), _ptr(lse_out), _ptr(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "lserve_sparse_decode_tree")

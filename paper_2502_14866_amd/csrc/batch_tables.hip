@@ -12,26 +12,6 @@ namespace {
 constexpr int kTableThreads = 256, kTableWaves = kTableThreads / kWave;
 constexpr int kTokensPerThread = 4, kTableTokens = kTableThreads * kTokensPerThread;  // tokens of a workgroup
 
-constexpr int kDppRowShr1 = 0x111, kDppRowShr2 = 0x112, kDppRowShr4 = 0x114, kDppRowShr8 = 0x118;
-constexpr int kDppRowBcast15 = 0x142, kDppRowBcast31 = 0x143;
-
-// x of a lane to the left, or `none` where there is no such lane (or the step does not reach this row of lanes).
-template <int Ctrl, int Rows> __device__ __forceinline__ int from_left(int none, int x) {
-    return __builtin_amdgcn_update_dpp(none, x, Ctrl, Rows, 0xf, false);
-}
-// Inclusive scan over the wavefront: inside the rows of sixteen lanes, then the rows' last lanes into the rows behind them.
-template <class Op> __device__ __forceinline__ int wave_scan(int x, int none, Op op) {
-    x = op(x, from_left<kDppRowShr1, 0xf>(none, x));
-    x = op(x, from_left<kDppRowShr2, 0xf>(none, x));
-    x = op(x, from_left<kDppRowShr4, 0xf>(none, x));
-    x = op(x, from_left<kDppRowShr8, 0xf>(none, x));
-    x = op(x, from_left<kDppRowBcast15, 0xa>(none, x));
-    x = op(x, from_left<kDppRowBcast31, 0xc>(none, x));
-    return x;
-}
-__device__ __forceinline__ int add(int a, int b) { return a + b; }
-__device__ __forceinline__ int larger(int a, int b) { return max(a, b); }
-
 }  // namespace
 
 // A workgroup owns kTableTokens consecutive new tokens of the batch.  It runs over the sequences, a thread to each, with a running

@@ -114,4 +114,20 @@ struct RotaryArgs {
 hipError_t preload_rotary_kernels();
 hipError_t launch_rotary(int dtype, const RotaryArgs& args, hipStream_t stream);
 
+// Attention of drafted tokens (lserve_sparse_decode_tree).
+struct TreeArgs {
+    LayerParams lp;
+    PagedParams kv;
+    const uint16_t *q, *k_new, *v_new;   // [total_new][H or Hkv][D]
+    const int *cu_new, *positions;       // positions and tree_mask may both be null: a chain
+    const unsigned long long* tree_mask; // [total_new][mask_words]
+    const int *sel_pages, *sel_count, *sel_seq_len;  // all null: every page
+    int mask_words, sel_stride, total_new, max_new;
+    uint16_t* out;
+    float* lse_out;
+};
+size_t tree_workspace_bytes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride);
+hipError_t preload_tree_kernels();
+hipError_t launch_sparse_decode_tree(int dtype, const TreeArgs& args, void* workspace, hipStream_t stream);
+
 }  // namespace lserve

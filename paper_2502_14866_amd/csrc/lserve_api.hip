@@ -571,6 +571,57 @@ int lserve_tree_masks(const int32_t* parents, const int32_t* cu_new, const int32
     return e == hipSuccess ? LSERVE_OK : fail_hip(e);
 }
 
+int lserve_sparse_decode_tree(const lserve_attn_desc* desc, const lserve_paged_kv* kv, const void* q, const void* k_new, const void* v_new,
+                              const int32_t* cu_new, const uint64_t* tree_mask, int32_t mask_words, const int32_t* positions,
+                              const int32_t* sel_pages, const int32_t* sel_count, const int32_t* sel_seq_len, int32_t sel_stride,
+                              int32_t total_new, int32_t max_new_per_seq, void* out, float* lse_out, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+    TreeArgs a = {};
+    int rc = make_layer(desc, &a.lp);
+    if (rc) return rc;
+    rc = make_paged(kv, a.lp, true, true, false, true, &a.kv);
+    if (rc) return rc;
+    if (a.lp.NP != 64) return LSERVE_ERR_UNSUPPORTED;
+    if (!q || !k_new || !v_new || !cu_new || !out) return LSERVE_ERR_INVALID_ARG;
+    if (total_new <= 0 || max_new_per_seq <= 0 || max_new_per_seq > total_new || !tree_mask != !positions) return LSERVE_ERR_INVALID_ARG;
+    if (tree_mask && mask_words < (max_new_per_seq + 63) / 64) return LSERVE_ERR_INVALID_ARG;
+    if (!sel_pages != !sel_count || !sel_pages != !sel_seq_len || (sel_pages ? sel_stride <= 0 : sel_stride != 0)) return LSERVE_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(cu_new) || !aligned16(tree_mask) || !aligned16(positions) ||
+        !aligned16(sel_pages) || !aligned16(sel_count) || !aligned16(sel_seq_len) || !aligned16(out) || !aligned16(lse_out) ||
+        !aligned16(workspace))
+        return LSERVE_ERR_INVALID_ARG;
+    if (max_new_per_seq > kMaxTreeNodes) return LSERVE_ERR_UNSUPPORTED;
+    const size_t need = tree_workspace_bytes(a.lp, a.kv.batch, total_new, max_new_per_seq, a.kv.max_pages, sel_stride);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return LSERVE_ERR_WORKSPACE;
+    a.q = (const uint16_t*)q;
+    a.k_new = (const uint16_t*)k_new;
+    a.v_new = (const uint16_t*)v_new;
+    a.cu_new = cu_new;
+    a.positions = positions;
+    a.tree_mask = (const unsigned long long*)tree_mask;
+    a.sel_pages = sel_pages;
+    a.sel_count = sel_count;
+    a.sel_seq_len = sel_seq_len;
+    a.mask_words = mask_words;
+    a.sel_stride = sel_stride;
+    a.total_new = total_new;
+    a.max_new = max_new_per_seq;
+    a.out = (uint16_t*)out;
+    a.lse_out = lse_out;
+    const hipError_t e = launch_sparse_decode_tree(desc->dtype, a, workspace, (hipStream_t)stream);
+    return e == hipSuccess ? LSERVE_OK : fail_hip(e);
+}
+
+size_t lserve_tree_workspace_bytes(const lserve_attn_desc* desc, int32_t batch, int32_t total_new, int32_t max_new_per_seq,
+                                   int32_t max_pages_per_seq, int32_t sel_stride) {
+    LayerParams lp;
+    if (make_layer(desc, &lp) != LSERVE_OK || lp.NP != 64) return 0;
+    if (batch <= 0 || batch > 65535 || total_new <= 0 || max_new_per_seq <= 0 || max_new_per_seq > total_new ||
+        max_new_per_seq > kMaxTreeNodes || max_pages_per_seq <= 0 || sel_stride < 0)
+        return 0;
+    return tree_workspace_bytes(lp, batch, total_new, max_new_per_seq, max_pages_per_seq, sel_stride);
+}
+
 int lserve_probe_decode_read(const lserve_attn_desc* desc, const lserve_paged_kv* kv, const int32_t* sel_pages,
                              const int32_t* sel_count, const int32_t* sel_seq_len, int32_t sel_stride, void* stream) {
     LayerParams lp;
@@ -615,6 +666,7 @@ int lserve_init(void) {
     if (e == hipSuccess) e = preload_decode_kernels();
     if (e == hipSuccess) e = preload_table_kernels();
     if (e == hipSuccess) e = preload_rotary_kernels();
+    if (e == hipSuccess) e = preload_tree_kernels();
     return e == hipSuccess ? LSERVE_OK : fail_hip(e);
 }
 

@@ -1,0 +1,793 @@
+// Attention of drafted tokens (Sec. 3.6's page lists under a tree of queries) on the gfx950 matrix cores.
+//
+// The drafted tokens of a sequence all read the same pages of history, so the rows that meet a KV head's keys are (drafted token, query
+// head of the group): n G of them.  Two products of 4 n G D operations per key against the 512 bytes of its K and V row make n G operations
+// per byte, and HBM is the bound up to some two hundred rows.  A list of keys is the head's pages of history followed by tiles of 64 drafted
+// tokens, whose K and V come straight from the call's tensors; who sees whom there is one bit per (row, key).
+//
+// A workgroup owns 32 RG rows of one (sequence, KV head) and a stretch of its list, 64 keys a step, K and V brought into LDS by direct
+// loads (quantised ones through registers), two stages.  Wavefront (rg, kg) works on row block rg and, of the step's keys, on half kg (RG = 1, 2) or
+// all (RG = 4).  Scores are computed transposed, S^T = K Q^T, so that a lane owns a row and the softmax stays in the lane and
+// its partner; the weights are then the second operand of O^T += V^T P^T as they are (see sparse_prefill.hip).
+//
+// Lists are cut into pieces of equal length by what the sequences hold when the kernel runs, which the host does not know: every
+// workgroup works out the cut from the lengths of the batch (TreePlan).  Pieces leave (maximum, sum, outputs) in the workspace and
+// fold_trees_kernel puts them together in order.
+#include <algorithm>
+
+#include "kernels.h"
+#include "matrix.h"
+
+namespace lserve {
+
+namespace {
+
+constexpr int kTile = 64;                        // keys of a step: a page, or drafted tokens
+constexpr int kRowBytes = kHeadDim * 2;          // of a 16-bit row
+constexpr int kTileBytes = kTile * kRowBytes;
+constexpr int kTableEntries = 256;               // list entries looked up at a time
+constexpr int kBlockFloat4 = 16 * kWave;         // outputs of a block of 32 rows, as the lanes hold them
+constexpr int kLeastPiece = 2;                   // list entries
+constexpr int kWorkgroupsPerUnit = 2;            // resident: 64 KiB of LDS each
+
+// How a launch is laid out (host).
+struct TreeLaunch {
+    int target;     // pieces to cut the lists into, about; 0: lists stay whole
+    int exact;      // no more than that
+    int row_tiles;  // of 32 RG rows, of the longest sequence
+    int streams;    // streaming heads
+    int slots;      // of pieces in the workspace
+    float4* partials;
+    float2* partial_ml;
+    int2* pieces;   // [batch][Hkv][row_tiles]: (first slot, pieces)
+};
+
+// What sequence b asks for.  Everything is brought inside the arrays, whatever the lengths say.
+struct SeqShape {
+    int start, n, len, pages;  // first drafted token, how many, tokens and pages of history
+    int dense, stream;         // list entries of a head that attends a selection (or everything), of a streaming head
+    int row_tiles;
+};
+
+__device__ __forceinline__ int first_local_page(const LayerParams& lp, int len) {
+    // of the first drafted token, whose own tile is that of position `len`
+    return max(lp.sink_pages, len / kTile - lp.local_pages + 1);
+}
+
+__device__ __forceinline__ int pages_of(int tokens) { return (int)(((unsigned)max(tokens, 0) + kTile - 1) / kTile); }
+
+template <int R> __device__ __forceinline__ SeqShape seq_shape(const TreeArgs& a, int b) {
+    SeqShape s;
+    s.start = max(a.cu_new[b], 0);
+    s.n = min(min(a.cu_new[b + 1] - s.start, a.max_new), a.total_new - s.start);
+    s.len = (int)min((long long)max(a.kv.seq_lens[b], 0), min((long long)a.kv.max_pages * kTile, 0x7fffffc0LL));
+    s.pages = ceil_div(s.len, kTile);
+    const int drafts = ceil_div(max(s.n, 0), kTile);
+    int dense = s.pages;
+    if (a.sel_pages) {
+        const int then = min(pages_of(a.sel_seq_len[b]), s.pages);
+        dense = min(then, a.sel_stride) + s.pages - then;
+    }
+    s.dense = dense + drafts;
+    s.stream = min(a.lp.sink_pages, s.pages) + max(0, s.pages - first_local_page(a.lp, s.len)) + drafts;
+    s.row_tiles = s.n > 0 ? ceil_div(s.n * a.lp.group, R) : 0;
+    return s;
+}
+
+// Pieces of `span` list entries.
+struct TreePlan {
+    int span;
+    __device__ __forceinline__ int pieces(int entries) const { return span == 0 ? 1 : ceil_div(entries, span); }
+    __device__ __forceinline__ int units(const TreeArgs& a, const TreeLaunch& t, const SeqShape& s) const {
+        return s.row_tiles * (t.streams * pieces(s.stream) + (a.lp.Hkv - t.streams) * pieces(s.dense));
+    }
+};
+
+__device__ __forceinline__ float wave_sum(float x) { return rows4_sum(row16_sum(x)); }
+
+template <int R> __device__ __forceinline__ TreePlan make_plan(const TreeArgs& a, const TreeLaunch& t) {
+    if (t.target == 0) return {0};
+    const int lane = threadIdx.x % kWave, batch = a.kv.batch, denses = a.lp.Hkv - t.streams;
+    float work = 0.f;
+    for (int base = 0; base < batch; base += kWave) {
+        if (base + lane >= batch) continue;
+        const SeqShape s = seq_shape<R>(a, base + lane);
+        work += (float)s.row_tiles * ((float)t.streams * s.stream + (float)denses * s.dense);
+    }
+    work = wave_sum(work);
+    const int whole = __builtin_amdgcn_readfirstlane((int)min(work / t.target, 1e9f));
+    TreePlan plan = {max(kLeastPiece, (float)whole * t.target < work ? whole + 1 : whole)};
+    if (!t.exact) return plan;
+    // as long as it takes to have no more pieces than workgroups that run at once (they are at most twice as many to begin with)
+    for (int i = 0; i < 24; ++i) {
+        float count = 0.f;
+        for (int base = 0; base < batch; base += kWave) {
+            if (base + lane >= batch) continue;
+            count += (float)plan.units(a, t, seq_shape<R>(a, base + lane));
+        }
+        count = wave_sum(count);
+        if (__builtin_amdgcn_readfirstlane(count <= (float)t.target)) break;
+        plan.span += max(1, plan.span / 16);
+    }
+    return plan;
+}
+
+// The unit-th piece of the launch.
+struct TreeUnit {
+    int b, hk, row_tile, piece, pieces;
+};
+template <int R>
+__device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t, const TreePlan& plan, int unit, TreeUnit& u, SeqShape& shape) {
+    const int lane = threadIdx.x % kWave, batch = a.kv.batch;
+    if (t.target == 0) {  // plenty of lists, all whole: by arithmetic, and not all of these row tiles exist
+        u.row_tile = unit % t.row_tiles;
+        unit /= t.row_tiles;
+        u.hk = unit % a.lp.Hkv;
+        u.b = unit / a.lp.Hkv;
+        u.piece = 0;
+        u.pieces = 1;
+        if (u.b >= batch) return false;
+        shape = seq_shape<R>(a, u.b);
+        return u.row_tile < shape.row_tiles;
+    }
+    for (int base = 0;; base += kWave) {
+        if (base >= batch) return false;
+        SeqShape s = {};
+        int units = 0;
+        if (base + lane < batch) {
+            s = seq_shape<R>(a, base + lane);
+            units = plan.units(a, t, s);
+        }
+        const int upto = wave_scan(units, 0, add);
+        const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
+        if (unit >= all) {
+            unit -= all;
+            continue;
+        }
+        const int at = __builtin_ctzll(__ballot(upto > unit));
+        u.b = base + at;
+        shape.start = __builtin_amdgcn_readlane(s.start, at);
+        shape.n = __builtin_amdgcn_readlane(s.n, at);
+        shape.len = __builtin_amdgcn_readlane(s.len, at);
+        shape.pages = __builtin_amdgcn_readlane(s.pages, at);
+        shape.dense = __builtin_amdgcn_readlane(s.dense, at);
+        shape.stream = __builtin_amdgcn_readlane(s.stream, at);
+        shape.row_tiles = __builtin_amdgcn_readlane(s.row_tiles, at);
+        unit -= __builtin_amdgcn_readlane(upto - units, at);
+        break;
+    }
+    // of a sequence: heads that select (the longer lists) first, then pieces, then row tiles, which read the same keys
+    const int denses = a.lp.Hkv - t.streams, of_dense = denses * plan.pieces(shape.dense) * shape.row_tiles;
+    const bool streaming = unit >= of_dense;
+    if (streaming) unit -= of_dense;
+    u.pieces = plan.pieces(streaming ? shape.stream : shape.dense);
+    u.row_tile = unit % shape.row_tiles;
+    unit /= shape.row_tiles;
+    u.piece = unit % u.pieces;
+    int rank = unit / u.pieces;
+    unsigned long long heads = streaming ? a.lp.streaming_mask : ~a.lp.streaming_mask;
+    for (; rank > 0; --rank) heads &= heads - 1;
+    u.hk = __builtin_ctzll(heads);
+    return true;
+}
+
+template <class T> struct BitsOf;
+template <> struct BitsOf<F16> { static constexpr uint32_t exponent = 0x7c00u; };
+template <> struct BitsOf<BF16> { static constexpr uint32_t exponent = 0x7f80u; };
+
+// Eight codes of a quantised row as numbers of the layer's type (exact: 8 bits fit the mantissas of both).
+template <class T, int BITS> __device__ __forceinline__ uint4 codes8(uint2 codes) {
+    return dequantise8<T, BITS>(codes, 0x00003c00u);  // scale 1, zero 0
+}
+
+// A block of 32 output rows, O^T in the lanes ((n, half) holds channels 32 db + 8 (i / 4) + 4 half + i % 4 of row n), out through 8 KiB of LDS so
+// that sixteen lanes store a row.
+template <class T>
+__device__ __forceinline__ void store_rows(const TreeArgs& a, const float16_t (&acc)[4], float inv, unsigned char* room, const SeqShape& s, int hk, int row0) {
+    const int lane = threadIdx.x % kWave, n = lane % 32, half = lane / 32, G = a.lp.group;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+            uint2 w;
+            w.x = Elem<T>::pack(acc[db][4 * g4] * inv, acc[db][4 * g4 + 1] * inv);
+            w.y = Elem<T>::pack(acc[db][4 * g4 + 2] * inv, acc[db][4 * g4 + 3] * inv);
+            *reinterpret_cast<uint2*>(room + n * kRowBytes + k_chunk_pos(n, db * 4 + g4) * 16 + 8 * half) = w;
+        }
+    asm volatile("" ::: "memory");  // LDS serves a wave in order, if the compiler asks in order
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + lane / 16, row = row0 + r;
+        const uint4 w = *reinterpret_cast<const uint4*>(room + r * kRowBytes + k_chunk_pos(r, lane % 16) * 16);
+        if (row < s.n * G)
+            *reinterpret_cast<uint4*>(a.out + ((size_t)(s.start + row / G) * a.lp.H + hk * G + row % G) * kHeadDim + lane % 16 * 8) = w;
+    }
+}
+__device__ __forceinline__ void store_lse(const TreeArgs& a, float m, float l, const SeqShape& s, int hk, int row0) {
+    const int lane = threadIdx.x % kWave, row = row0 + lane % 32, G = a.lp.group;
+    if (a.lse_out && lane < 32 && row < s.n * G)
+        a.lse_out[(size_t)(s.start + row / G) * a.lp.H + hk * G + row % G] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+}  // namespace
+
+template <class T, int BITS, int RG>
+__global__ __launch_bounds__(RG == 1 ? 128 : 256, 2) void draft_tree_kernel(TreeArgs a, TreeLaunch t) {
+    constexpr bool QUANT = BITS != 16;
+    constexpr int KG = RG == 4 ? 1 : 2, kWaves = RG * KG, NB = 2 / KG, R = 32 * RG;
+    constexpr int kLoads = 16 / kWaves;  // 1 KiB loads per wave, operand and step
+    __shared__ __attribute__((aligned(1024))) unsigned char k_lds[2][kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_lds[2][kTileBytes];
+    __shared__ int2 table[kTableEntries];                          // (position of the page or drafted tile, physical page or -1)
+    __shared__ __attribute__((aligned(16))) uint32_t k_scale[QUANT ? 2 : 1][QUANT ? kTile : 1];  // (scale, zero) of the keys of a stage
+    __shared__ float2 fold_ml[RG][32];
+
+    const int tid = threadIdx.x, lane = tid % kWave, n = lane % 32, half = lane / 32;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), rg = wave / KG, kg = wave % KG;
+    const TreePlan plan = make_plan<R>(a, t);
+    // Workgroup ids go round-robin over the XCDs: an XCD takes neighbouring pieces, whose row tiles share keys in its L2.
+    constexpr int kXcds = 8;
+    const int unit = (blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds;  // gridDim.x is a multiple of kXcds
+    TreeUnit u;
+    SeqShape s;
+    if (!find_unit<R>(a, t, plan, unit, u, s)) return;
+    const int b = u.b, hk = u.hk, G = a.lp.group, rows = s.n * G;
+    const bool streaming = (a.lp.streaming_mask >> hk) & 1ull;
+    if (u.piece == 0 && tid == 0 && t.target) t.pieces[(b * a.lp.Hkv + hk) * t.row_tiles + u.row_tile] = make_int2(unit, u.pieces);
+
+    // ---- the list: entries of history, then tiles of drafted tokens
+    const int drafts = ceil_div(s.n, kTile);
+    const bool ring = in_stream_pool(a.lp, a.kv, hk);
+    int listed = s.pages, first_new = 0;  // entries that a list or a formula names; pages from first_new on follow
+    if (streaming) {
+        listed = min(a.lp.sink_pages, s.pages);
+        first_new = first_local_page(a.lp, s.len);
+    } else if (a.sel_pages) {
+        listed = min(max(a.sel_count[(size_t)b * a.lp.Hkv + hk], 0), a.sel_stride);
+        first_new = pages_of(a.sel_seq_len[b]);
+    } else {
+        first_new = s.pages;
+    }
+    const int history = listed + max(0, s.pages - first_new), entries = history + drafts;
+    const int e0 = (int)((long long)entries * u.piece / u.pieces), e1 = (int)((long long)entries * (u.piece + 1) / u.pieces);
+    const int* sel = a.sel_pages ? a.sel_pages + ((size_t)b * a.lp.Hkv + hk) * a.sel_stride : nullptr;
+    // looks up entries from..from + 255 of the list
+    auto look_up = [&](int from) {
+        for (int i = tid; i < kTableEntries; i += kWaves * kWave) {
+            const int e = from + i;
+            if (e >= e1) break;
+            int2 w = make_int2(e - history, -1);
+            if (e < history) {
+                int p = e < listed ? (streaming || !sel ? e : sel[e]) : first_new + (e - listed);
+                if (p < 0 || p >= s.pages) {
+                    w = make_int2(s.pages, 0);  // no such page: nothing of it is read
+                } else {
+                    const int phys = ring ? a.kv.ring_table[(size_t)b * a.kv.ring + ring_slot(a.lp, p)] : a.kv.page_table[(size_t)b * a.kv.max_pages + p];
+                    w = make_int2(p, ring ? max(phys, 0) : min(max(phys, 0), a.kv.num_pages - 1));
+                }
+            }
+            table[i] = w;
+        }
+    };
+
+    // ---- the wave's rows: row r is query head r % G of the group, drafted token r / G; rows past the end repeat the last
+    const int row0 = u.row_tile * R + rg * 32, row = min(row0 + n, rows - 1), token = s.start + row / G;
+    const bool wave_has_rows = row0 < rows;
+    const int own = row / G;  // index of the drafted token in its sequence
+    int own_tile = 0;
+    if (streaming) own_tile = max(a.positions ? a.positions[token] : s.len + own, s.len) / kTile;
+    uint4 qreg[8];
+    {
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + ((size_t)token * a.lp.H + hk * G + row % G) * kHeadDim);
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) qreg[kk] = src[kk * 2 + half];
+    }
+    // (pinned once the first keys are on their way: left alone the loads sink into the loop, where they wait for its prefetch)
+    auto pin_queries = [&] {
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qreg[kk].x), "+v"(qreg[kk].y), "+v"(qreg[kk].z), "+v"(qreg[kk].w));
+    };
+    float q_sum = 0.f;  // of the row, for quantised keys: code * scale + zero
+    if constexpr (QUANT) {
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+            const uint32_t w[4] = {qreg[kk].x, qreg[kk].y, qreg[kk].z, qreg[kk].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q_sum += Elem<T>::lo(w[i]) + Elem<T>::hi(w[i]);
+        }
+        q_sum = halves_sum(q_sum);
+    }
+
+    // ---- staging: wave w brings in rows w 64 / kWaves .., four rows to a load, lane l position l % 16 of row l / 16 of them
+    const size_t slab = slab_chunks(kTile, BITS) * 16;
+    const unsigned char* const k_base = reinterpret_cast<const unsigned char*>(ring ? a.kv.k_stream : a.kv.k_pool) + pool_rank(a.lp, a.kv, hk, ring) * slab;
+    const unsigned char* const v_base = reinterpret_cast<const unsigned char*>(ring ? a.kv.v_stream : a.kv.v_pool) + pool_rank(a.lp, a.kv, hk, ring) * slab;
+    const size_t page_bytes = (size_t)(ring ? a.kv.stream_heads : a.kv.pool_heads) * slab;
+    const unsigned new_row_bytes = (unsigned)a.lp.Hkv * kRowBytes;
+    const size_t new_offset = ((size_t)s.start * a.lp.Hkv + hk) * kRowBytes;
+    const int my_row = wave * (kTile / kWaves) + lane / 16;
+    // rows of an entry that exist
+    auto live_rows = [&](int2 w) { return w.y < 0 ? min(s.n - w.x * kTile, kTile) : min(s.len - w.x * kTile, kTile); };
+    auto entry = [&](int e) {  // of the stretch in the table
+        const int2 w = table[(e - e0) % kTableEntries];
+        return make_int2(__builtin_amdgcn_readfirstlane(w.x), __builtin_amdgcn_readfirstlane(w.y));
+    };
+    auto fetch = [&](int2 w, unsigned char* kd, unsigned char* vd) {  // 16-bit rows; those past the last one repeat it
+        const int live = live_rows(w);
+        if (live <= 0) return;
+        const bool drafted = w.y < 0;
+        const unsigned long long offset = drafted ? new_offset + (size_t)w.x * kTile * new_row_bytes : (size_t)w.y * page_bytes;
+        const unsigned long long ks = uniform64((unsigned long long)(drafted ? (const unsigned char*)a.k_new : k_base) + offset);
+        const unsigned long long vs = uniform64((unsigned long long)(drafted ? (const unsigned char*)a.v_new : v_base) + offset);
+        const unsigned stride = drafted ? new_row_bytes : (unsigned)kRowBytes;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = my_row + 4 * i;
+            const unsigned at = (unsigned)min(r, live - 1) * stride;
+            const unsigned to = (wave * kLoads + i) * 1024;
+            dma_load16(ks, at + k_chunk_pos(r, lane % 16) * 16, __builtin_amdgcn_readfirstlane(lds_address(kd) + to));
+            dma_load16(vs, at + v_chunk_pos(r, lane % 16) * 16, __builtin_amdgcn_readfirstlane(lds_address(vd) + to));
+        }
+    };
+    // quantised rows on their way through registers
+    struct Staged {
+        uint2 k[kLoads], v[kLoads];
+        uint32_t kz[kLoads], vz[kLoads];
+        bool on;
+    } staged;
+    staged.on = false;
+    auto fetch_codes = [&](int2 w) {
+        if constexpr (QUANT) {
+            const int live = live_rows(w);
+            staged.on = w.y >= 0 && live > 0;
+            if (!staged.on) return;
+            const unsigned char *kp = k_base + (size_t)w.y * page_bytes, *vp = v_base + (size_t)w.y * page_bytes;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int r = my_row + 4 * i, from = min(r, live - 1);
+                const unsigned char* kr = kp + from * (kHeadDim * BITS / 8) + k_chunk_pos(r, lane % 16) * BITS;
+                const unsigned char* vr = vp + from * (kHeadDim * BITS / 8) + v_chunk_pos(r, lane % 16) * BITS;
+                if constexpr (BITS == 8) {
+                    staged.k[i] = *reinterpret_cast<const uint2*>(kr);
+                    staged.v[i] = *reinterpret_cast<const uint2*>(vr);
+                } else {
+                    staged.k[i] = make_uint2(*reinterpret_cast<const uint32_t*>(kr), 0u);
+                    staged.v[i] = make_uint2(*reinterpret_cast<const uint32_t*>(vr), 0u);
+                }
+                staged.kz[i] = reinterpret_cast<const uint32_t*>(kp + kTile * kHeadDim * BITS / 8)[from];
+                staged.vz[i] = reinterpret_cast<const uint32_t*>(vp + kTile * kHeadDim * BITS / 8)[from];
+            }
+        }
+    };
+    // Keys go into LDS as their codes, exactly, and meet scale and zero as scores in fp32 (rounded keys would cost the log-sum-exp three
+    // digits); values as numbers of the layer's type, rounded once.
+    auto store_staged = [&](int stage) {
+        if constexpr (QUANT) {
+            if (!staged.on) return;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const unsigned to = (wave * kLoads + i) * 1024 + lane * 16;
+                *reinterpret_cast<uint4*>(k_lds[stage] + to) = codes8<T, BITS>(staged.k[i]);
+                *reinterpret_cast<uint4*>(v_lds[stage] + to) = dequantise8<T, BITS>(staged.v[i], staged.vz[i]);
+                if (lane % 16 == 0) k_scale[stage][my_row + 4 * i] = staged.kz[i];
+            }
+        }
+    };
+
+    // ---- softmax state and outputs of the lane's row (its keys: those of its half)
+    float16_t acc[4] = {};
+    float m_run = -INFINITY, l_run = 0.f;
+    int koff[8], voff[4];
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) koff[kk] = n * kRowBytes + k_chunk_pos(n, kk * 2 + half) * 16;
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+        const int s16 = lane % 16, rr = s16 / 4, chunk = 4 * db + 2 * (n / 16) + (s16 % 4) / 2;
+        voff[db] = half * 1024 + rr * kRowBytes + v_chunk_pos(rr, chunk) * 16 + 8 * (s16 % 2);
+    }
+
+    // keys of the entry that the lane's row sees, one bit each
+    auto seen = [&](int2 w, int live) {
+        unsigned long long bits = live >= kTile ? ~0ull : (1ull << live) - 1ull;
+        if (w.y >= 0) {
+            if (streaming && !(w.x < a.lp.sink_pages || w.x > own_tile - a.lp.local_pages)) bits = 0;
+            return bits;
+        }
+        if (a.tree_mask) {
+            bits &= a.tree_mask[(size_t)token * a.mask_words + w.x];
+        } else {
+            const int last = own - w.x * kTile;  // a chain: its own and those before
+            bits &= last < 0 ? 0ull : last >= kTile - 1 ? ~0ull : (2ull << last) - 1ull;
+        }
+        if (streaming) {
+            // a drafted key counts as a token of the tile of its position
+            const int key = w.x * kTile + min(lane, live - 1);
+            const int key_tile = max(a.positions ? a.positions[s.start + key] : s.len + key, s.len) / kTile;
+            unsigned long long off = 0;
+            for (int i = 0; i < live; ++i) {
+                const int kt = __builtin_amdgcn_readlane(key_tile, i);
+                if (kt >= a.lp.sink_pages && kt <= own_tile - a.lp.local_pages) off |= 1ull << i;
+            }
+            bits &= ~off;
+        }
+        return bits;
+    };
+
+    auto work_on = [&](int2 w, int stage) {
+        const int live = live_rows(w);
+        if (live <= 0 || !wave_has_rows) return;
+        const bool codes = QUANT && w.y >= 0;
+        const unsigned long long bits = seen(w, live);
+        if (!__any(bits != 0)) return;
+        const bool mixed = __any(~bits != 0);
+        const unsigned char *ks = k_lds[stage] + kg * NB * 32 * kRowBytes, *vs = v_lds[stage] + kg * NB * 32 * kRowBytes;
+        float16_t sc[NB] = {};
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+                sc[kb] = Mfma<T>::run(*reinterpret_cast<const uint4*>(ks + kb * 32 * kRowBytes + koff[kk]), qreg[kk], sc[kb]);
+        if (codes) {
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int g4 = 0; g4 < 4; ++g4) {
+                    const uint4 z4 = *reinterpret_cast<const uint4*>(&k_scale[QUANT ? stage : 0][QUANT ? (kg * NB + kb) * 32 + 8 * g4 + 4 * half : 0]);
+                    const uint32_t z[4] = {z4.x, z4.y, z4.z, z4.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        sc[kb][4 * g4 + i] = __builtin_fmaf(sc[kb][4 * g4 + i], Elem<F16>::lo(z[i]), Elem<F16>::hi(z[i]) * q_sum);
+                }
+        }
+        if (mixed) {
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) {
+                const unsigned mine = (unsigned)(bits >> (32 * (kg * NB + kb))) >> (4 * half);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!(mine >> (8 * (i / 4) + i % 4) & 1u)) sc[kb][i] = -INFINITY;
+            }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
+        top = halves_max(top) * a.lp.sm_scale_log2;
+        const float m_new = fmaxf(m_run, top);
+        if (__any(m_new > m_run)) {
+            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[db][i] *= alpha;
+            m_run = m_new;
+        }
+        const float off = m_run == -INFINITY ? 0.f : -m_run;
+        uint4 pb[NB][2];
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][i], a.lp.sm_scale_log2, off));
+                l_run += p[i];  // unrounded; the second product takes them in the layer's type, which is what its operands are
+            }
+            pb[kb][0] = pack8<T>(p);
+            pb[kb][1] = pack8<T>(p + 8);
+        }
+        auto values = [&](int step, int db) {  // V^T operand: channel 32 db + n of the lane's eight keys of the step's sixteen
+            const uint2 lo = lds_read_transposed(vs + (4 * step) * 1024 + voff[db]);
+            const uint2 hi = lds_read_transposed(vs + (4 * step + 2) * 1024 + voff[db]);
+            return make_uint4(lo.x, lo.y, hi.x, hi.y);
+        };
+        // A value that is infinite or not a number must not reach the rows that do not see its key, and zero times it would: tiles that are
+        // not seen whole are looked through first (zero times all of them, 0.1 us), and such keys are added row by row.
+        unsigned long long bad = 0;
+        if (mixed) {
+            float16_t none = {};
+#pragma unroll
+            for (int step = 0; step < 2 * NB; ++step)
+#pragma unroll
+                for (int db = 0; db < 4; ++db) none = Mfma<T>::run(values(step, db), make_uint4(0u, 0u, 0u, 0u), none);
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum += none[i];
+            if (__any(sum != 0.f)) {  // (not a number)
+                constexpr uint32_t kExponent = BitsOf<T>::exponent;
+                const int key = lane % (32 * NB);
+                bool spoiled = false;
+                for (int c = 0; c < 16; ++c) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(vs + key * kRowBytes + c * 16);
+                    const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        spoiled = spoiled || (w4[i] & kExponent) == kExponent || (w4[i] >> 16 & kExponent) == kExponent;
+                }
+                bad = __ballot(spoiled);
+                if (NB == 1) bad &= 0xffffffffull;
+            }
+        }
+        if (__builtin_expect(bad == 0, 1)) {
+#pragma unroll
+            for (int step = 0; step < 2 * NB; ++step)
+#pragma unroll
+                for (int db = 0; db < 4; ++db) acc[db] = Mfma<T>::run(values(step, db), pb[step / 2][step % 2], acc[db]);
+            return;
+        }
+#pragma unroll
+        for (int step = 0; step < 2 * NB; ++step) {
+            const unsigned b0 = (unsigned)(bad >> (16 * step + 4 * half)), b1 = b0 >> 8;  // of the lane's keys, four and four
+            auto keep = [](unsigned two) { return ~((two & 1u ? 0xffffu : 0u) | (two & 2u ? 0xffff0000u : 0u)); };
+#pragma unroll
+            for (int db = 0; db < 4; ++db) {
+                uint4 x = values(step, db);
+                x = make_uint4(x.x & keep(b0), x.y & keep(b0 >> 2), x.z & keep(b1), x.w & keep(b1 >> 2));
+                acc[db] = Mfma<T>::run(x, pb[step / 2][step % 2], acc[db]);
+            }
+        }
+        for (; bad; bad &= bad - 1) {
+            const int key = __builtin_ctzll(bad);
+            float score = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) {
+                const uint4 x = *reinterpret_cast<const uint4*>(ks + key * kRowBytes + k_chunk_pos(key, kk * 2 + half) * 16);
+                score = Elem<T>::dot2(x.x, qreg[kk].x, Elem<T>::dot2(x.y, qreg[kk].y, score));
+                score = Elem<T>::dot2(x.z, qreg[kk].z, Elem<T>::dot2(x.w, qreg[kk].w, score));
+            }
+            score = halves_sum(score);
+            if (codes) {
+                const uint32_t z = k_scale[QUANT ? stage : 0][QUANT ? kg * NB * 32 + key : 0];
+                score = __builtin_fmaf(score, Elem<F16>::lo(z), Elem<F16>::hi(z) * q_sum);
+            }
+            if (!(bits >> (kg * NB * 32 + key) & 1ull)) continue;
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(score, a.lp.sm_scale_log2, off));
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int g4 = 0; g4 < 4; ++g4) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(vs + key * kRowBytes + v_chunk_pos(key, 4 * db + g4) * 16 + 8 * half);
+                    acc[db][4 * g4] += p * Elem<T>::lo(x.x);
+                    acc[db][4 * g4 + 1] += p * Elem<T>::hi(x.x);
+                    acc[db][4 * g4 + 2] += p * Elem<T>::lo(x.y);
+                    acc[db][4 * g4 + 3] += p * Elem<T>::hi(x.y);
+                }
+        }
+    };
+
+    // ---- walk: entry e is worked on, e + 1 on its way into LDS, of quantised pages e + 2 on its way into registers
+    look_up(e0);
+    __syncthreads();
+    int2 w0 = e0 < e1 ? entry(e0) : make_int2(s.pages, 0), w1 = e0 + 1 < e1 ? entry(e0 + 1) : make_int2(s.pages, 0);
+    auto fetch_direct = [&](int2 w, int stage) {
+        if (!QUANT || w.y < 0) fetch(w, k_lds[stage], v_lds[stage]);
+    };
+    if (e0 < e1) {
+        fetch_direct(w0, 0);
+        fetch_codes(w0);
+        store_staged(0);
+    }
+    pin_queries();
+    dma_wait();
+    if (e0 + 1 < e1) fetch_codes(w1);
+    __syncthreads();
+    for (int e = e0; e < e1; ++e) {
+        const int stage = (e - e0) & 1;
+        int2 w2 = make_int2(s.pages, 0);
+        if (e + 2 < e1) {
+            if ((e + 2 - e0) % kTableEntries == 0) {
+                look_up(e + 2);  // (every wave has read the stretch before: the barrier at the end of the last step)
+                __syncthreads();
+            }
+            w2 = entry(e + 2);
+        }
+        if (e + 1 < e1) {
+            fetch_direct(w1, stage ^ 1);
+            store_staged(stage ^ 1);
+        }
+        if (e + 2 < e1) fetch_codes(w2);
+        work_on(w0, stage);
+        if (!QUANT || w1.y < 0) dma_wait();
+        w0 = w1;
+        w1 = w2;
+        __syncthreads();
+    }
+
+    // ---- the two halves of the keys meet in LDS (the tiles are done with: the loop ended on a barrier)
+    float l = halves_sum(l_run), m = m_run;
+    if constexpr (KG == 2) {
+        float4* const room = reinterpret_cast<float4*>(k_lds[RG == 1 ? 0 : rg]);
+        if (kg == 1) {
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int g4 = 0; g4 < 4; ++g4)
+                    room[(db * 4 + g4) * kWave + lane] = make_float4(acc[db][4 * g4], acc[db][4 * g4 + 1], acc[db][4 * g4 + 2], acc[db][4 * g4 + 3]);
+            if (half == 0) fold_ml[rg][n] = make_float2(m, l);
+        }
+        __syncthreads();
+        if (kg == 1) return;
+        const float2 other = fold_ml[rg][n];
+        const float m_all = fmaxf(m, other.x);
+        const float f0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_all), f1 = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other.x - m_all);
+        l = l * f0 + other.y * f1;
+        m = m_all;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+                const float4 x = room[(db * 4 + g4) * kWave + lane];
+                acc[db][4 * g4] = acc[db][4 * g4] * f0 + x.x * f1;
+                acc[db][4 * g4 + 1] = acc[db][4 * g4 + 1] * f0 + x.y * f1;
+                acc[db][4 * g4 + 2] = acc[db][4 * g4 + 2] * f0 + x.z * f1;
+                acc[db][4 * g4 + 3] = acc[db][4 * g4 + 3] * f0 + x.w * f1;
+            }
+    }
+    if (!wave_has_rows) return;
+    if (u.pieces > 1) {  // as the lanes hold it
+        const size_t block = (size_t)unit * RG + rg;
+        float4* const dst = t.partials + block * kBlockFloat4;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4)
+                dst[(db * 4 + g4) * kWave + lane] = make_float4(acc[db][4 * g4], acc[db][4 * g4 + 1], acc[db][4 * g4 + 2], acc[db][4 * g4 + 3]);
+        if (half == 0) t.partial_ml[block * 32 + n] = make_float2(m, l);
+        return;
+    }
+    unsigned char* const room = RG == 4 ? (wave < 2 ? k_lds[wave] : v_lds[wave - 2]) : v_lds[RG == 1 ? 0 : rg];
+    store_rows<T>(a, acc, l == 0.f ? 0.f : 1.f / l, room, s, hk, row0);
+    store_lse(a, m, l, s, hk, row0);
+}
+
+// Puts the pieces of 32 rows of a (sequence, KV head) together, in the order of the list: a wavefront to 32 channels.
+template <class T, int RG>
+__global__ __launch_bounds__(256) void fold_trees_kernel(TreeArgs a, TreeLaunch t) {
+    __shared__ __attribute__((aligned(16))) unsigned char rows_lds[4][32 * 64];
+    const int lane = threadIdx.x % kWave, n = lane % 32, half = lane / 32, G = a.lp.group;
+    const int db = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    int at = blockIdx.x;
+    const int rg = at % RG;
+    at /= RG;
+    const int row_tile = at % t.row_tiles, list = at / t.row_tiles, hk = list % a.lp.Hkv, b = list / a.lp.Hkv;
+    const SeqShape s = seq_shape<32 * RG>(a, b);
+    const int row0 = (row_tile * RG + rg) * 32;
+    if (row0 >= s.n * G) return;
+    const int2 pieces = t.pieces[(size_t)list * t.row_tiles + row_tile];
+    // (lengths that contradict each other may ask for more pieces than there is room for, and lead to no address outside it)
+    if (pieces.x < 0 || pieces.y < 2 || pieces.x + (long long)(pieces.y - 1) * s.row_tiles >= t.slots) return;
+    // piece i of a row tile is row_tiles (of this sequence) slots behind piece i - 1
+    const size_t step = (size_t)s.row_tiles * RG, first = (size_t)pieces.x * RG + rg;
+    float m = -INFINITY;
+    for (int i = 0; i < pieces.y; ++i) m = fmaxf(m, t.partial_ml[(first + i * step) * 32 + n].x);
+    float l = 0.f, o[16] = {};
+#pragma unroll 4
+    for (int i = 0; i < pieces.y; ++i) {
+        const float2 ml = t.partial_ml[(first + i * step) * 32 + n];
+        const float4* src = t.partials + (first + i * step) * kBlockFloat4 + db * 4 * kWave + lane;
+        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+        l += ml.y * f;
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+            const float4 x = src[g4 * kWave];
+            o[4 * g4] += x.x * f;
+            o[4 * g4 + 1] += x.y * f;
+            o[4 * g4 + 2] += x.z * f;
+            o[4 * g4 + 3] += x.w * f;
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    unsigned char* const room = rows_lds[db];
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4)
+        *reinterpret_cast<uint2*>(room + n * 64 + (g4 ^ (n / 4 % 4)) * 16 + 8 * half) =
+            make_uint2(Elem<T>::pack(o[4 * g4] * inv, o[4 * g4 + 1] * inv), Elem<T>::pack(o[4 * g4 + 2] * inv, o[4 * g4 + 3] * inv));
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = 16 * i + lane / 4, row = row0 + r;
+        const uint4 w = *reinterpret_cast<const uint4*>(room + r * 64 + (lane % 4 ^ (r / 4 % 4)) * 16);
+        if (row < s.n * G)
+            *reinterpret_cast<uint4*>(a.out + ((size_t)(s.start + row / G) * a.lp.H + hk * G + row % G) * kHeadDim + db * 32 + lane % 4 * 8) = w;
+    }
+    if (db == 0) store_lse(a, m, l, s, hk, row0);
+}
+
+// ---- host side -----------------------------------------------------------------------------------
+
+namespace {
+
+struct TreeSizes {
+    int RG, row_tiles, target, exact, streams;
+    long long grid, folds;  // workgroups of the two kernels
+    size_t pieces_bytes, ml_bytes, partial_bytes;
+};
+
+TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride) {
+    TreeSizes z = {};
+    const long long rows = (long long)max_new * lp.group;
+    z.RG = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    const int R = 32 * z.RG;
+    z.row_tiles = (int)((rows + R - 1) / R);
+    z.streams = __builtin_popcountll(lp.streaming_mask);
+    // row tiles of all sequences: a part of one each, and no more than the tokens there are
+    const long long tiles = std::min((long long)batch * z.row_tiles, (long long)total_new * lp.group / R + batch), lists = tiles * lp.Hkv;
+    const int resident = num_compute_units() * kWorkgroupsPerUnit;
+    // list entries as far as the host knows: pages of the table, or of a selection (and those since, which are few)
+    const int drafts = ceil_div(max_new, kTile), dense = sel_stride > 0 ? std::min(max_pages, sel_stride + 1) : max_pages;
+    const int stream = std::min(max_pages, lp.sink_pages + lp.local_pages);
+    const long long shortest = tiles * ((lp.Hkv - z.streams) * (long long)(dense + drafts) + z.streams * (long long)(stream + drafts)) / kLeastPiece;
+    // Few lists: as many pieces as workgroups run at once.  More: three times as many, so that what is left over at the end is short.
+    // Plenty: whole lists.
+    z.exact = 2 * lists <= resident && 2 * lists <= shortest;
+    z.target = lists >= 8LL * resident || std::max(dense, stream) + drafts <= kLeastPiece
+                   ? 0 : (int)std::min<long long>(shortest, z.exact ? resident : 3 * resident);
+    z.exact = z.exact && z.target > 0;
+    z.grid = z.target == 0 ? (long long)batch * lp.Hkv * z.row_tiles : z.exact ? z.target : z.target + lists;
+    z.grid = (z.grid + 8 + 7) / 8 * 8;
+    z.folds = z.target == 0 ? 0 : (long long)batch * lp.Hkv * z.row_tiles * z.RG;
+    if (z.target) {
+        z.pieces_bytes = ((size_t)batch * lp.Hkv * z.row_tiles * sizeof(int2) + 255) / 256 * 256;
+        z.ml_bytes = (size_t)z.grid * z.RG * 32 * sizeof(float2);
+        z.partial_bytes = (size_t)z.grid * z.RG * kBlockFloat4 * sizeof(float4);
+    }
+    return z;
+}
+
+template <class T, int BITS> hipError_t launch_tree(const TreeArgs& a, void* workspace, hipStream_t stream) {
+    const TreeSizes z = tree_sizes(a.lp, a.kv.batch, a.total_new, a.max_new, a.kv.max_pages, a.sel_stride);
+    if (z.grid > 0x7fffffffLL || z.folds > 0x7fffffffLL) return hipErrorInvalidValue;
+    TreeLaunch t = {};
+    t.target = z.target;
+    t.exact = z.exact;
+    t.row_tiles = z.row_tiles;
+    t.streams = z.streams;
+    t.slots = z.target ? (int)z.grid : 0;
+    if (z.target) {
+        unsigned char* p = static_cast<unsigned char*>(workspace);
+        t.pieces = reinterpret_cast<int2*>(p);
+        t.partial_ml = reinterpret_cast<float2*>(p + z.pieces_bytes);
+        t.partials = reinterpret_cast<float4*>(p + z.pieces_bytes + z.ml_bytes);
+    }
+    const dim3 grid((unsigned)z.grid), folds((unsigned)z.folds);
+#define LSERVE_TREE(RG)                                                                                                  hipLaunchKernelGGL((draft_tree_kernel<T, BITS, RG>), grid, dim3(RG == 1 ? 128 : 256), 0, stream, a, t);              if (z.folds) hipLaunchKernelGGL((fold_trees_kernel<T, RG>), folds, dim3(256), 0, stream, a, t)
+    if (z.RG == 1) {
+        LSERVE_TREE(1);
+    } else if (z.RG == 2) {
+        LSERVE_TREE(2);
+    } else {
+        LSERVE_TREE(4);
+    }
+#undef LSERVE_TREE
+    return hipGetLastError();
+}
+
+template <class T> hipError_t launch_bits(const TreeArgs& a, void* workspace, hipStream_t stream) {
+    switch (a.kv.kv_bits) {
+        case 8:
+            return launch_tree<T, 8>(a, workspace, stream);
+        case 4:
+            return launch_tree<T, 4>(a, workspace, stream);
+        default:
+            return launch_tree<T, 16>(a, workspace, stream);
+    }
+}
+
+}  // namespace
+
+size_t tree_workspace_bytes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride) {
+    const TreeSizes z = tree_sizes(lp, batch, total_new, max_new, max_pages, sel_stride);
+    return z.pieces_bytes + z.ml_bytes + z.partial_bytes;
+}
+
+hipError_t preload_tree_kernels() {
+    hipFuncAttributes attr;
+    return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&draft_tree_kernel<F16, 16, 1>));
+}
+
+hipError_t launch_sparse_decode_tree(int dtype, const TreeArgs& a, void* workspace, hipStream_t stream) {
+    return dtype == 0 ? launch_bits<F16>(a, workspace, stream) : launch_bits<BF16>(a, workspace, stream);
+}
+
+}  // namespace lserve
