@@ -25,10 +25,10 @@ namespace {
 constexpr int kTile = 64;                        // keys of a step: a page, or drafted tokens
 constexpr int kRowBytes = kHeadDim * 2;          // of a 16-bit row
 constexpr int kTileBytes = kTile * kRowBytes;
+constexpr int kAhead = 4;                        // operand reads in flight ahead of the products
 constexpr int kTableEntries = 256;               // list entries looked up at a time
 constexpr int kBlockFloat4 = 16 * kWave;         // outputs of a block of 32 rows, as the lanes hold them
 constexpr int kLeastPiece = 2;                   // list entries
-constexpr int kWorkgroupsPerUnit = 2;            // resident: 64 KiB of LDS each
 
 // How a launch is laid out (host).
 struct TreeLaunch {
@@ -85,27 +85,23 @@ struct TreePlan {
 
 __device__ __forceinline__ float wave_sum(float x) { return rows4_sum(row16_sum(x)); }
 
-template <int R> __device__ __forceinline__ TreePlan make_plan(const TreeArgs& a, const TreeLaunch& t) {
+// (own: the shape of sequence `lane`, which is all there is to load for batches of up to 64)
+template <int R> __device__ __forceinline__ TreePlan make_plan(const TreeArgs& a, const TreeLaunch& t, const SeqShape& own) {
     if (t.target == 0) return {0};
     const int lane = threadIdx.x % kWave, batch = a.kv.batch, denses = a.lp.Hkv - t.streams;
-    float work = 0.f;
-    for (int base = 0; base < batch; base += kWave) {
-        if (base + lane >= batch) continue;
-        const SeqShape s = seq_shape<R>(a, base + lane);
-        work += (float)s.row_tiles * ((float)t.streams * s.stream + (float)denses * s.dense);
-    }
-    work = wave_sum(work);
+    auto total = [&](auto f) {  // of f over the sequences
+        float x = f(own);
+        for (int base = kWave; base < batch; base += kWave)
+            if (base + lane < batch) x += f(seq_shape<R>(a, base + lane));
+        return wave_sum(x);
+    };
+    const float work = total([&](const SeqShape& s) { return (float)s.row_tiles * ((float)t.streams * s.stream + (float)denses * s.dense); });
     const int whole = __builtin_amdgcn_readfirstlane((int)min(work / t.target, 1e9f));
     TreePlan plan = {max(kLeastPiece, (float)whole * t.target < work ? whole + 1 : whole)};
     if (!t.exact) return plan;
     // as long as it takes to have no more pieces than workgroups that run at once (they are at most twice as many to begin with)
     for (int i = 0; i < 24; ++i) {
-        float count = 0.f;
-        for (int base = 0; base < batch; base += kWave) {
-            if (base + lane >= batch) continue;
-            count += (float)plan.units(a, t, seq_shape<R>(a, base + lane));
-        }
-        count = wave_sum(count);
+        const float count = total([&](const SeqShape& s) { return (float)plan.units(a, t, s); });
         if (__builtin_amdgcn_readfirstlane(count <= (float)t.target)) break;
         plan.span += max(1, plan.span / 16);
     }
@@ -117,7 +113,8 @@ struct TreeUnit {
     int b, hk, row_tile, piece, pieces;
 };
 template <int R>
-__device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t, const TreePlan& plan, int unit, TreeUnit& u, SeqShape& shape) {
+__device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t, const TreePlan& plan, const SeqShape& own, int unit, TreeUnit& u,
+                                          SeqShape& shape) {
     const int lane = threadIdx.x % kWave, batch = a.kv.batch;
     if (t.target == 0) {  // plenty of lists, all whole: by arithmetic, and not all of these row tiles exist
         u.row_tile = unit % t.row_tiles;
@@ -132,12 +129,9 @@ __device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t
     }
     for (int base = 0;; base += kWave) {
         if (base >= batch) return false;
-        SeqShape s = {};
-        int units = 0;
-        if (base + lane < batch) {
-            s = seq_shape<R>(a, base + lane);
-            units = plan.units(a, t, s);
-        }
+        SeqShape s = own;
+        if (base > 0) s = base + lane < batch ? seq_shape<R>(a, base + lane) : SeqShape{};
+        const int units = plan.units(a, t, s);
         const int upto = wave_scan(units, 0, add);
         const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
         if (unit >= all) {
@@ -170,6 +164,10 @@ __device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t
     u.hk = __builtin_ctzll(heads);
     return true;
 }
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 template <class T> struct BitsOf;
 template <> struct BitsOf<F16> { static constexpr uint32_t exponent = 0x7c00u; };
@@ -211,26 +209,46 @@ __device__ __forceinline__ void store_lse(const TreeArgs& a, float m, float l, c
 
 }  // namespace
 
+// How a workgroup of RG row blocks is made up.
+template <int BITS, int RG> struct TreeShape {
+    static constexpr bool kQuant = BITS != 16;
+    static constexpr int kKeyHalves = RG <= 2 ? 2 : 1;  // wavefronts that share a step's keys
+    static constexpr int kWaves = RG * kKeyHalves;
+    // 16-bit tiles: three on the way while one is worked on, one workgroup to a compute unit, where rows are few and memory is the bound;
+    // two stages and two workgroups where a step's products take as long as its tiles.
+    static constexpr int kStages = kQuant || RG == 4 ? 2 : 4;
+    static constexpr int kResident = kStages == 2 && RG <= 4 ? 2 : 1;
+    static constexpr int kPerSimd = (kResident * kWaves + 3) / 4;  // wavefronts
+};
+
 template <class T, int BITS, int RG>
-__global__ __launch_bounds__(RG == 1 ? 128 : 256, 2) void draft_tree_kernel(TreeArgs a, TreeLaunch t) {
-    constexpr bool QUANT = BITS != 16;
-    constexpr int KG = RG == 4 ? 1 : 2, kWaves = RG * KG, NB = 2 / KG, R = 32 * RG;
+__global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draft_tree_kernel(TreeArgs a, TreeLaunch t) {
+    using Shape = TreeShape<BITS, RG>;
+    constexpr bool QUANT = Shape::kQuant;
+    constexpr int KG = Shape::kKeyHalves, kWaves = Shape::kWaves, NB = 2 / KG, R = 32 * RG, kStages = Shape::kStages;
     constexpr int kLoads = 16 / kWaves;  // 1 KiB loads per wave, operand and step
-    __shared__ __attribute__((aligned(1024))) unsigned char k_lds[2][kTileBytes];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_lds[2][kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_lds[kStages][kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_lds[kStages][kTileBytes];
     __shared__ int2 table[kTableEntries];                          // (position of the page or drafted tile, physical page or -1)
-    __shared__ __attribute__((aligned(16))) uint32_t k_scale[QUANT ? 2 : 1][QUANT ? kTile : 1];  // (scale, zero) of the keys of a stage
+    __shared__ __attribute__((aligned(16))) uint32_t k_scale[QUANT ? 2 : 1][QUANT ? kTile : 4];  // (scale, zero) of the keys of a stage
     __shared__ float2 fold_ml[RG][32];
+    __shared__ unsigned spoiled_keys[2];
+    __shared__ int deepest[kWaves];  // tile of the wave's rows
 
     const int tid = threadIdx.x, lane = tid % kWave, n = lane % 32, half = lane / 32;
-    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), rg = wave / KG, kg = wave % KG;
-    const TreePlan plan = make_plan<R>(a, t);
+    const int wave = uniform(tid / kWave), rg = wave / KG, kg = wave % KG;
+    SeqShape mine = {};
+    if (t.target && lane < a.kv.batch) mine = seq_shape<R>(a, lane);
+    const TreePlan plan = make_plan<R>(a, t, mine);
     // Workgroup ids go round-robin over the XCDs: an XCD takes neighbouring pieces, whose row tiles share keys in its L2.
     constexpr int kXcds = 8;
     const int unit = (blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds;  // gridDim.x is a multiple of kXcds
     TreeUnit u;
     SeqShape s;
-    if (!find_unit<R>(a, t, plan, unit, u, s)) return;
+    if (!find_unit<R>(a, t, plan, mine, unit, u, s)) return;
+    // (all of it comes out of lane arithmetic, and what stays in vector registers takes the addresses of the walk there with it)
+    u.b = uniform(u.b), u.hk = uniform(u.hk), u.row_tile = uniform(u.row_tile), u.piece = uniform(u.piece), u.pieces = uniform(u.pieces);
+    s.start = uniform(s.start), s.n = uniform(s.n), s.len = uniform(s.len), s.pages = uniform(s.pages);
     const int b = u.b, hk = u.hk, G = a.lp.group, rows = s.n * G;
     const bool streaming = (a.lp.streaming_mask >> hk) & 1ull;
     if (u.piece == 0 && tid == 0 && t.target) t.pieces[(b * a.lp.Hkv + hk) * t.row_tiles + u.row_tile] = make_int2(unit, u.pieces);
@@ -243,13 +261,15 @@ __global__ __launch_bounds__(RG == 1 ? 128 : 256, 2) void draft_tree_kernel(Tree
         listed = min(a.lp.sink_pages, s.pages);
         first_new = first_local_page(a.lp, s.len);
     } else if (a.sel_pages) {
-        listed = min(max(a.sel_count[(size_t)b * a.lp.Hkv + hk], 0), a.sel_stride);
-        first_new = pages_of(a.sel_seq_len[b]);
+        listed = uniform(min(max(a.sel_count[(size_t)b * a.lp.Hkv + hk], 0), a.sel_stride));
+        first_new = uniform(pages_of(a.sel_seq_len[b]));
     } else {
         first_new = s.pages;
     }
     const int history = listed + max(0, s.pages - first_new), entries = history + drafts;
-    const int e0 = (int)((long long)entries * u.piece / u.pieces), e1 = (int)((long long)entries * (u.piece + 1) / u.pieces);
+    // (fewer entries than the plan counted on leave some pieces empty)
+    const int share = entries / u.pieces, rest = entries - share * u.pieces;
+    const int e0 = uniform(u.piece * share + min(u.piece, rest)), e1 = uniform(e0 + share + (u.piece < rest ? 1 : 0));
     const int* sel = a.sel_pages ? a.sel_pages + ((size_t)b * a.lp.Hkv + hk) * a.sel_stride : nullptr;
     // looks up entries from..from + 255 of the list
     auto look_up = [&](int from) {
@@ -271,32 +291,30 @@ __global__ __launch_bounds__(RG == 1 ? 128 : 256, 2) void draft_tree_kernel(Tree
     };
 
     // ---- the wave's rows: row r is query head r % G of the group, drafted token r / G; rows past the end repeat the last
-    const int row0 = u.row_tile * R + rg * 32, row = min(row0 + n, rows - 1), token = s.start + row / G;
+    const int row0 = u.row_tile * R + rg * 32, row = min(row0 + n, rows - 1), own = row / G, token = s.start + own;  // own: index in its sequence
     const bool wave_has_rows = row0 < rows;
-    const int own = row / G;  // index of the drafted token in its sequence
-    int own_tile = 0;
-    if (streaming) own_tile = max(a.positions ? a.positions[token] : s.len + own, s.len) / kTile;
+    // all that depends on the row alone is requested before anything is waited for
     uint4 qreg[8];
     {
         const uint4* src = reinterpret_cast<const uint4*>(a.q + ((size_t)token * a.lp.H + hk * G + row % G) * kHeadDim);
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) qreg[kk] = src[kk * 2 + half];
     }
+    const unsigned long long row_mask = a.tree_mask ? a.tree_mask[(size_t)token * a.mask_words] : 0ull;  // of the first drafted tile
+    int own_tile = 0, key_tile = 0;  // of the row's position; of the position of drafted key `lane`
+    if (streaming) {
+        const int key = min(lane, s.n - 1);
+        own_tile = max(a.positions ? a.positions[token] : s.len + own, s.len);
+        key_tile = max(a.positions ? a.positions[s.start + key] : s.len + key, s.len) / kTile;
+        own_tile /= kTile;
+    }
+    look_up(e0);
     // (pinned once the first keys are on their way: left alone the loads sink into the loop, where they wait for its prefetch)
     auto pin_queries = [&] {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qreg[kk].x), "+v"(qreg[kk].y), "+v"(qreg[kk].z), "+v"(qreg[kk].w));
     };
     float q_sum = 0.f;  // of the row, for quantised keys: code * scale + zero
-    if constexpr (QUANT) {
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-            const uint32_t w[4] = {qreg[kk].x, qreg[kk].y, qreg[kk].z, qreg[kk].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) q_sum += Elem<T>::lo(w[i]) + Elem<T>::hi(w[i]);
-        }
-        q_sum = halves_sum(q_sum);
-    }
 
     // ---- staging: wave w brings in rows w 64 / kWaves .., four rows to a load, lane l position l % 16 of row l / 16 of them
     const size_t slab = slab_chunks(kTile, BITS) * 16;
@@ -313,8 +331,7 @@ __global__ __launch_bounds__(RG == 1 ? 128 : 256, 2) void draft_tree_kernel(Tree
         return make_int2(__builtin_amdgcn_readfirstlane(w.x), __builtin_amdgcn_readfirstlane(w.y));
     };
     auto fetch = [&](int2 w, unsigned char* kd, unsigned char* vd) {  // 16-bit rows; those past the last one repeat it
-        const int live = live_rows(w);
-        if (live <= 0) return;
+        const int live = max(live_rows(w), 1);  // (nothing of an entry without a page is used, but the loads are counted)
         const bool drafted = w.y < 0;
         const unsigned long long offset = drafted ? new_offset + (size_t)w.x * kTile * new_row_bytes : (size_t)w.y * page_bytes;
         const unsigned long long ks = uniform64((unsigned long long)(drafted ? (const unsigned char*)a.k_new : k_base) + offset);
@@ -386,6 +403,7 @@ __global__ __launch_bounds__(RG == 1 ? 128 : 256, 2) void draft_tree_kernel(Tree
         voff[db] = half * 1024 + rr * kRowBytes + v_chunk_pos(rr, chunk) * 16 + 8 * (s16 % 2);
     }
 
+    int deepest_tile = 0;  // of the workgroup's rows
     // keys of the entry that the lane's row sees, one bit each
     auto seen = [&](int2 w, int live) {
         unsigned long long bits = live >= kTile ? ~0ull : (1ull << live) - 1ull;
@@ -394,26 +412,116 @@ __global__ __launch_bounds__(RG == 1 ? 128 : 256, 2) void draft_tree_kernel(Tree
             return bits;
         }
         if (a.tree_mask) {
-            bits &= a.tree_mask[(size_t)token * a.mask_words + w.x];
+            bits &= w.x == 0 ? row_mask : a.tree_mask[(size_t)token * a.mask_words + w.x];
         } else {
             const int last = own - w.x * kTile;  // a chain: its own and those before
             bits &= last < 0 ? 0ull : last >= kTile - 1 ? ~0ull : (2ull << last) - 1ull;
         }
-        if (streaming) {
+        if (streaming && deepest_tile >= a.lp.local_pages) {
             // a drafted key counts as a token of the tile of its position
-            const int key = w.x * kTile + min(lane, live - 1);
-            const int key_tile = max(a.positions ? a.positions[s.start + key] : s.len + key, s.len) / kTile;
-            unsigned long long off = 0;
-            for (int i = 0; i < live; ++i) {
-                const int kt = __builtin_amdgcn_readlane(key_tile, i);
-                if (kt >= a.lp.sink_pages && kt <= own_tile - a.lp.local_pages) off |= 1ull << i;
+            int tile = key_tile;
+            if (w.x > 0) {
+                const int key = w.x * kTile + min(lane, live - 1);
+                tile = max(a.positions ? a.positions[s.start + key] : s.len + key, s.len) / kTile;
             }
-            bits &= ~off;
+            // (off for some row, if at all: the deepest is the first to lose a key)
+            unsigned long long far = __ballot(lane < live && tile >= a.lp.sink_pages && tile <= deepest_tile - a.lp.local_pages);
+            for (; far; far &= far - 1) {
+                const int i = __builtin_ctzll(far);
+                if (__builtin_amdgcn_readlane(tile, i) <= own_tile - a.lp.local_pages) bits &= ~(1ull << i);
+            }
         }
         return bits;
     };
 
-    auto work_on = [&](int2 w, int stage) {
+    // A value that is infinite or not a number must not reach the rows that do not see its key, and zero times it would.  Tiles that some row
+    // does not see whole (drafted tokens, the last page, pages at the far end of a streaming head's window) are looked through
+    // together: such values become zeros, and their keys' bits are returned.  Nearly always there are none.
+    auto clear_spoiled = [&](int2 w, int stage) __attribute__((always_inline)) -> unsigned long long {
+        constexpr uint32_t kLow = BitsOf<T>::exponent, kHigh = kLow << 16;
+        constexpr int kPieces = kTileBytes / 16 / (kWaves * kWave);
+        uint4* const mine = reinterpret_cast<uint4*>(v_lds[stage]) + tid;
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint4 x = mine[i * kWaves * kWave];
+            const uint32_t x4[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) found = found || (x4[c] & kLow) == kLow || (x4[c] & kHigh) == kHigh;
+        }
+        if (!__syncthreads_or(found)) return 0;
+        if (tid < 2) spoiled_keys[tid] = 0;
+        __syncthreads();
+#pragma clang loop unroll(disable)
+        for (int i = 0; i < kPieces; ++i) {
+            const int at = i * kWaves * kWave;
+            const uint4 x = mine[at];
+            uint32_t x4[4] = {x.x, x.y, x.z, x.w};
+            bool here = false;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if ((x4[c] & kLow) == kLow) x4[c] &= 0xffff0000u, here = true;
+                if ((x4[c] & kHigh) == kHigh) x4[c] &= 0x0000ffffu, here = true;
+            }
+            if (here) {
+                const int key = (tid + at) / 16;
+                mine[at] = make_uint4(x4[0], x4[1], x4[2], x4[3]);
+                atomicOr(&spoiled_keys[key / 32], 1u << (key % 32));
+            }
+        }
+        __syncthreads();
+        return (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane(spoiled_keys[1]) << 32 |
+               (unsigned)__builtin_amdgcn_readfirstlane(spoiled_keys[0]);
+    };
+    // Those values, from where they came from, to the rows that do see their keys: weight times value in fp32.
+    auto add_spoiled = [&](int2 w, int stage, unsigned long long bits, float off, unsigned long long keys) __attribute__((always_inline)) {
+        const bool drafted = w.y < 0, codes = QUANT && !drafted;
+        for (keys &= (NB == 2 ? ~0ull : 0xffffffffull << (32 * kg)); keys; keys &= keys - 1) {
+            const int key = __builtin_ctzll(keys), from = min(key, live_rows(w) - 1);
+            float score = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) {
+                const uint4 x = *reinterpret_cast<const uint4*>(k_lds[stage] + key * kRowBytes + k_chunk_pos(key, kk * 2 + half) * 16);
+                score = Elem<T>::dot2(x.x, qreg[kk].x, Elem<T>::dot2(x.y, qreg[kk].y, score));
+                score = Elem<T>::dot2(x.z, qreg[kk].z, Elem<T>::dot2(x.w, qreg[kk].w, score));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            score = halves_sum(score);
+            if (codes) {
+                const uint32_t z = k_scale[QUANT ? stage : 0][QUANT ? key : 0];
+                score = __builtin_fmaf(score, Elem<F16>::lo(z), Elem<F16>::hi(z) * q_sum);
+            }
+            const bool on = bits >> key & 1ull;
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(score, a.lp.sm_scale_log2, off));
+            const unsigned char* const page = v_base + (size_t)w.y * page_bytes;
+            const unsigned char* const src =
+                drafted ? (const unsigned char*)a.v_new + new_offset + ((size_t)w.x * kTile + from) * new_row_bytes
+                        : page + from * (kHeadDim * BITS / 8);
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int g4 = 0; g4 < 4; ++g4) {
+                    const int c = 4 * db + g4;  // eight channels, of which the lane has four
+                    uint2 x;
+                    if (codes) {
+                        uint2 raw = make_uint2(0u, 0u);
+                        if constexpr (BITS == 8) raw = *reinterpret_cast<const uint2*>(src + c * 8);
+                        if constexpr (BITS == 4) raw.x = *reinterpret_cast<const uint32_t*>(src + c * 4);
+                        const uint4 eight = dequantise8<T, QUANT ? BITS : 8>(raw, reinterpret_cast<const uint32_t*>(page + kTile * kHeadDim * BITS / 8)[from]);
+                        x = half ? make_uint2(eight.z, eight.w) : make_uint2(eight.x, eight.y);
+                    } else {
+                        x = *reinterpret_cast<const uint2*>(src + c * 16 + 8 * half);
+                    }
+                    const float v4[4] = {Elem<T>::lo(x.x), Elem<T>::hi(x.x), Elem<T>::lo(x.y), Elem<T>::hi(x.y)};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (on && !(fabsf(v4[i]) < INFINITY)) acc[db][4 * g4 + i] += p * v4[i];
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        }
+    };
+
+    auto work_on = [&](int2 w, int stage, unsigned long long spoiled) __attribute__((always_inline)) {
         const int live = live_rows(w);
         if (live <= 0 || !wave_has_rows) return;
         const bool codes = QUANT && w.y >= 0;
@@ -427,6 +535,14 @@ __global__ __launch_bounds__(RG == 1 ? 128 : 256, 2) void draft_tree_kernel(Tree
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb)
                 sc[kb] = Mfma<T>::run(*reinterpret_cast<const uint4*>(ks + kb * 32 * kRowBytes + koff[kk]), qreg[kk], sc[kb]);
+        // schedule: operand reads run four ahead of the products that consume them, and no further (registers)
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < 8 * NB - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
         if (codes) {
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb)
@@ -482,122 +598,125 @@ __global__ __launch_bounds__(RG == 1 ? 128 : 256, 2) void draft_tree_kernel(Tree
             const uint2 hi = lds_read_transposed(vs + (4 * step + 2) * 1024 + voff[db]);
             return make_uint4(lo.x, lo.y, hi.x, hi.y);
         };
-        // A value that is infinite or not a number must not reach the rows that do not see its key, and zero times it would: tiles that are
-        // not seen whole are looked through first (zero times all of them, 0.1 us), and such keys are added row by row.
-        unsigned long long bad = 0;
-        if (mixed) {
-            float16_t none = {};
 #pragma unroll
-            for (int step = 0; step < 2 * NB; ++step)
+        for (int step = 0; step < 2 * NB; ++step)
 #pragma unroll
-                for (int db = 0; db < 4; ++db) none = Mfma<T>::run(values(step, db), make_uint4(0u, 0u, 0u, 0u), none);
-            float sum = 0.f;
+            for (int db = 0; db < 4; ++db) acc[db] = Mfma<T>::run(values(step, db), pb[step / 2][step % 2], acc[db]);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAhead, 0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum += none[i];
-            if (__any(sum != 0.f)) {  // (not a number)
-                constexpr uint32_t kExponent = BitsOf<T>::exponent;
-                const int key = lane % (32 * NB);
-                bool spoiled = false;
-                for (int c = 0; c < 16; ++c) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(vs + key * kRowBytes + c * 16);
-                    const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        spoiled = spoiled || (w4[i] & kExponent) == kExponent || (w4[i] >> 16 & kExponent) == kExponent;
-                }
-                bad = __ballot(spoiled);
-                if (NB == 1) bad &= 0xffffffffull;
-            }
+        for (int i = 0; i < 8 * NB - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
-        if (__builtin_expect(bad == 0, 1)) {
-#pragma unroll
-            for (int step = 0; step < 2 * NB; ++step)
-#pragma unroll
-                for (int db = 0; db < 4; ++db) acc[db] = Mfma<T>::run(values(step, db), pb[step / 2][step % 2], acc[db]);
-            return;
-        }
-#pragma unroll
-        for (int step = 0; step < 2 * NB; ++step) {
-            const unsigned b0 = (unsigned)(bad >> (16 * step + 4 * half)), b1 = b0 >> 8;  // of the lane's keys, four and four
-            auto keep = [](unsigned two) { return ~((two & 1u ? 0xffffu : 0u) | (two & 2u ? 0xffff0000u : 0u)); };
-#pragma unroll
-            for (int db = 0; db < 4; ++db) {
-                uint4 x = values(step, db);
-                x = make_uint4(x.x & keep(b0), x.y & keep(b0 >> 2), x.z & keep(b1), x.w & keep(b1 >> 2));
-                acc[db] = Mfma<T>::run(x, pb[step / 2][step % 2], acc[db]);
-            }
-        }
-        for (; bad; bad &= bad - 1) {
-            const int key = __builtin_ctzll(bad);
-            float score = 0.f;
-#pragma unroll
-            for (int kk = 0; kk < 8; ++kk) {
-                const uint4 x = *reinterpret_cast<const uint4*>(ks + key * kRowBytes + k_chunk_pos(key, kk * 2 + half) * 16);
-                score = Elem<T>::dot2(x.x, qreg[kk].x, Elem<T>::dot2(x.y, qreg[kk].y, score));
-                score = Elem<T>::dot2(x.z, qreg[kk].z, Elem<T>::dot2(x.w, qreg[kk].w, score));
-            }
-            score = halves_sum(score);
-            if (codes) {
-                const uint32_t z = k_scale[QUANT ? stage : 0][QUANT ? kg * NB * 32 + key : 0];
-                score = __builtin_fmaf(score, Elem<F16>::lo(z), Elem<F16>::hi(z) * q_sum);
-            }
-            if (!(bits >> (kg * NB * 32 + key) & 1ull)) continue;
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(score, a.lp.sm_scale_log2, off));
-#pragma unroll
-            for (int db = 0; db < 4; ++db)
-#pragma unroll
-                for (int g4 = 0; g4 < 4; ++g4) {
-                    const uint2 x = *reinterpret_cast<const uint2*>(vs + key * kRowBytes + v_chunk_pos(key, 4 * db + g4) * 16 + 8 * half);
-                    acc[db][4 * g4] += p * Elem<T>::lo(x.x);
-                    acc[db][4 * g4 + 1] += p * Elem<T>::hi(x.x);
-                    acc[db][4 * g4 + 2] += p * Elem<T>::lo(x.y);
-                    acc[db][4 * g4 + 3] += p * Elem<T>::hi(x.y);
-                }
-        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+        if (__builtin_expect(spoiled != 0, 0)) add_spoiled(w, stage, bits, off, spoiled);
     };
 
-    // ---- walk: entry e is worked on, e + 1 on its way into LDS, of quantised pages e + 2 on its way into registers
-    look_up(e0);
-    __syncthreads();
-    int2 w0 = e0 < e1 ? entry(e0) : make_int2(s.pages, 0), w1 = e0 + 1 < e1 ? entry(e0 + 1) : make_int2(s.pages, 0);
-    auto fetch_direct = [&](int2 w, int stage) {
-        if (!QUANT || w.y < 0) fetch(w, k_lds[stage], v_lds[stage]);
-    };
-    if (e0 < e1) {
-        fetch_direct(w0, 0);
-        fetch_codes(w0);
-        store_staged(0);
+    // ---- walk
+    {
+        const int tile = (int)wave_max((float)own_tile);
+        if (lane == 0) deepest[wave] = tile;
     }
-    pin_queries();
-    dma_wait();
-    if (e0 + 1 < e1) fetch_codes(w1);
-    __syncthreads();
-    for (int e = e0; e < e1; ++e) {
-        const int stage = (e - e0) & 1;
-        int2 w2 = make_int2(s.pages, 0);
-        if (e + 2 < e1) {
-            if ((e + 2 - e0) % kTableEntries == 0) {
-                look_up(e + 2);  // (every wave has read the stretch before: the barrier at the end of the last step)
-                __syncthreads();
-            }
-            w2 = entry(e + 2);
+    if constexpr (QUANT) {
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+            const uint32_t w[4] = {qreg[kk].x, qreg[kk].y, qreg[kk].z, qreg[kk].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q_sum += Elem<T>::lo(w[i]) + Elem<T>::hi(w[i]);
         }
-        if (e + 1 < e1) {
-            fetch_direct(w1, stage ^ 1);
-            store_staged(stage ^ 1);
+        q_sum = halves_sum(q_sum);
+    }
+
+    auto step = [&](int2 w, int stage) __attribute__((always_inline)) {
+        const int live = live_rows(w);
+        const bool ragged = live > 0 && (live < kTile || w.y < 0 || (streaming && w.x >= a.lp.sink_pages && w.x <= deepest_tile - a.lp.local_pages));
+        work_on(w, stage, ragged ? clear_spoiled(w, stage) : 0ull);
+    };
+    auto find_deepest = [&] {  // past a barrier
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) deepest_tile = max(deepest_tile, deepest[i]);
+        deepest_tile = uniform(deepest_tile);
+    };
+    const int2 nothing = make_int2(s.pages, 0);
+    // entry e of the list, whose stretch of the table is looked up when its first one is asked for (in order, by all)
+    auto next_entry = [&](int e) {
+        if (e >= e1) return nothing;
+        if ((e - e0) % kTableEntries == 0 && e > e0) {
+            __syncthreads();
+            look_up(e);
+            __syncthreads();
         }
-        if (e + 2 < e1) fetch_codes(w2);
-        work_on(w0, stage);
-        if (!QUANT || w1.y < 0) dma_wait();
-        w0 = w1;
-        w1 = w2;
+        return entry(e);
+    };
+    if constexpr (!QUANT) {
+        // Tiles of up to kStages - 1 steps are on their way.  Loads arrive in order, kPerStep a step and wave: those of step e are there once no
+        // more than those of the steps behind it are missing.
+        constexpr int kPerStep = 2 * kLoads;
+        int2 w[kStages];
         __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) {
+            w[i] = next_entry(e0 + i);
+            if (e0 + i < e1) fetch(w[i], k_lds[i], v_lds[i]);
+        }
+        find_deepest();
+        pin_queries();
+        for (int e = e0; e < e1; e += kStages) {
+#pragma unroll
+            for (int i = 0; i < kStages; ++i) {
+                const int now = e + i;
+                if (now >= e1) break;
+                if (kStages == 4 && now + 2 < e1)
+                    wait_loads<2 * kPerStep>();
+                else if (kStages == 4 && now + 1 < e1)
+                    wait_loads<kPerStep>();
+                else
+                    wait_loads<0>();
+                __syncthreads();  // the tiles of this step are there, and those of the step before are done with
+                constexpr int kBehind = kStages - 1;
+                w[(i + kBehind) % kStages] = next_entry(now + kBehind);
+                if (now + kBehind < e1) fetch(w[(i + kBehind) % kStages], k_lds[(i + kBehind) % kStages], v_lds[(i + kBehind) % kStages]);
+                step(w[i], i);
+            }
+        }
+        __syncthreads();
+    } else {
+        // entry e is worked on, e + 1 on its way into LDS, e + 2 on its way into registers
+        auto fetch_drafted = [&](int2 w, int stage) {
+            if (w.y < 0) fetch(w, k_lds[stage], v_lds[stage]);
+        };
+        __syncthreads();
+        int2 w0 = next_entry(e0), w1 = next_entry(e0 + 1);
+        if (e0 < e1) {
+            fetch_drafted(w0, 0);
+            fetch_codes(w0);
+            store_staged(0);
+        }
+        find_deepest();
+        pin_queries();
+        wait_loads<0>();
+        if (e0 + 1 < e1) fetch_codes(w1);
+        __syncthreads();
+        for (int e = e0; e < e1; ++e) {
+            const int stage = (e - e0) & 1;
+            const int2 w2 = next_entry(e + 2);
+            if (e + 1 < e1) {
+                fetch_drafted(w1, stage ^ 1);
+                store_staged(stage ^ 1);
+            }
+            if (e + 2 < e1) fetch_codes(w2);
+            step(w0, stage);
+            if (w1.y < 0) wait_loads<0>();
+            w0 = w1;
+            w1 = w2;
+            __syncthreads();
+        }
     }
 
     // ---- the two halves of the keys meet in LDS (the tiles are done with: the loop ended on a barrier)
     float l = halves_sum(l_run), m = m_run;
     if constexpr (KG == 2) {
-        float4* const room = reinterpret_cast<float4*>(k_lds[RG == 1 ? 0 : rg]);
+        float4* const room = reinterpret_cast<float4*>(k_lds[rg]);
         if (kg == 1) {
 #pragma unroll
             for (int db = 0; db < 4; ++db)
@@ -636,62 +755,93 @@ __global__ __launch_bounds__(RG == 1 ? 128 : 256, 2) void draft_tree_kernel(Tree
         if (half == 0) t.partial_ml[block * 32 + n] = make_float2(m, l);
         return;
     }
-    unsigned char* const room = RG == 4 ? (wave < 2 ? k_lds[wave] : v_lds[wave - 2]) : v_lds[RG == 1 ? 0 : rg];
+    // 8 KiB for the wave's rows: two waves to a tile of V, four tiles where there are eight waves
+    unsigned char* const room = (rg < 4 ? v_lds[rg / 2] : k_lds[rg / 2 - 2]) + rg % 2 * (kTileBytes / 2);
     store_rows<T>(a, acc, l == 0.f ? 0.f : 1.f / l, room, s, hk, row0);
     store_lse(a, m, l, s, hk, row0);
 }
 
-// Puts the pieces of 32 rows of a (sequence, KV head) together, in the order of the list: a wavefront to 32 channels.
+// Puts the pieces of 32 rows of a (sequence, KV head) together: a workgroup to 32 channels, its eight wavefronts take pieces in turn, and what they
+// have is added in their order.  Pieces come in at the latency of memory, so that many wavefronts with a few loads each are wanted.
+constexpr int kFoldWaves = 8, kFoldThreads = kFoldWaves * kWave;
 template <class T, int RG>
-__global__ __launch_bounds__(256) void fold_trees_kernel(TreeArgs a, TreeLaunch t) {
-    __shared__ __attribute__((aligned(16))) unsigned char rows_lds[4][32 * 64];
-    const int lane = threadIdx.x % kWave, n = lane % 32, half = lane / 32, G = a.lp.group;
-    const int db = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+__global__ __launch_bounds__(kFoldThreads) void fold_trees_kernel(TreeArgs a, TreeLaunch t) {
+    __shared__ float sums[kFoldWaves][kWave * 17];  // a lane's sixteen, one place apart from the next lane's
+    __shared__ float2 wave_ml[kFoldWaves][32];
+    const int tid = threadIdx.x, lane = tid % kWave, n = lane % 32, G = a.lp.group, wave = uniform(tid / kWave);
     int at = blockIdx.x;
+    const int db = at % 4;
+    at /= 4;
     const int rg = at % RG;
     at /= RG;
     const int row_tile = at % t.row_tiles, list = at / t.row_tiles, hk = list % a.lp.Hkv, b = list / a.lp.Hkv;
+    const int2 pieces = t.pieces[(size_t)list * t.row_tiles + row_tile];
     const SeqShape s = seq_shape<32 * RG>(a, b);
     const int row0 = (row_tile * RG + rg) * 32;
     if (row0 >= s.n * G) return;
-    const int2 pieces = t.pieces[(size_t)list * t.row_tiles + row_tile];
     // (lengths that contradict each other may ask for more pieces than there is room for, and lead to no address outside it)
     if (pieces.x < 0 || pieces.y < 2 || pieces.x + (long long)(pieces.y - 1) * s.row_tiles >= t.slots) return;
     // piece i of a row tile is row_tiles (of this sequence) slots behind piece i - 1
-    const size_t step = (size_t)s.row_tiles * RG, first = (size_t)pieces.x * RG + rg;
-    float m = -INFINITY;
-    for (int i = 0; i < pieces.y; ++i) m = fmaxf(m, t.partial_ml[(first + i * step) * 32 + n].x);
-    float l = 0.f, o[16] = {};
-#pragma unroll 4
-    for (int i = 0; i < pieces.y; ++i) {
-        const float2 ml = t.partial_ml[(first + i * step) * 32 + n];
-        const float4* src = t.partials + (first + i * step) * kBlockFloat4 + db * 4 * kWave + lane;
-        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-        l += ml.y * f;
+    const size_t apart = (size_t)s.row_tiles * RG, first = (size_t)pieces.x * RG + rg;
+    float m = -INFINITY, l = 0.f, o[16] = {};
+    for (int i = wave; i < pieces.y; i += 4 * kFoldWaves) {  // four pieces at a time
+        float2 ml[4];
+        float4 x[4][4];
 #pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4) {
-            const float4 x = src[g4 * kWave];
-            o[4 * g4] += x.x * f;
-            o[4 * g4 + 1] += x.y * f;
-            o[4 * g4 + 2] += x.z * f;
-            o[4 * g4 + 3] += x.w * f;
+        for (int k = 0; k < 4; ++k) {
+            const size_t slot = first + min(i + k * kFoldWaves, pieces.y - 1) * apart;
+            ml[k] = t.partial_ml[slot * 32 + n];
+            const float4* src = t.partials + slot * kBlockFloat4 + db * 4 * kWave + lane;
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) x[k][g4] = src[g4 * kWave];
         }
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    unsigned char* const room = rows_lds[db];
+        float top = m;
 #pragma unroll
-    for (int g4 = 0; g4 < 4; ++g4)
-        *reinterpret_cast<uint2*>(room + n * 64 + (g4 ^ (n / 4 % 4)) * 16 + 8 * half) =
-            make_uint2(Elem<T>::pack(o[4 * g4] * inv, o[4 * g4 + 1] * inv), Elem<T>::pack(o[4 * g4 + 2] * inv, o[4 * g4 + 3] * inv));
-    asm volatile("" ::: "memory");
+        for (int k = 0; k < 4; ++k) {
+            if (i + k * kFoldWaves >= pieces.y) ml[k] = make_float2(-INFINITY, 0.f);
+            top = fmaxf(top, ml[k].x);
+        }
+        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        l *= alpha;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = 16 * i + lane / 4, row = row0 + r;
-        const uint4 w = *reinterpret_cast<const uint4*>(room + r * 64 + (lane % 4 ^ (r / 4 % 4)) * 16);
-        if (row < s.n * G)
-            *reinterpret_cast<uint4*>(a.out + ((size_t)(s.start + row / G) * a.lp.H + hk * G + row % G) * kHeadDim + db * 32 + lane % 4 * 8) = w;
+        for (int c = 0; c < 16; ++c) o[c] *= alpha;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (i + k * kFoldWaves >= pieces.y) break;
+            const float f = ml[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - top);
+            l += ml[k].y * f;
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+                o[4 * g4] += x[k][g4].x * f;
+                o[4 * g4 + 1] += x[k][g4].y * f;
+                o[4 * g4 + 2] += x[k][g4].z * f;
+                o[4 * g4 + 3] += x[k][g4].w * f;
+            }
+        }
+        m = top;
     }
-    if (db == 0) store_lse(a, m, l, s, hk, row0);
+#pragma unroll
+    for (int c = 0; c < 16; ++c) sums[wave][lane * 17 + c] = o[c];
+    if (lane < 32) wave_ml[wave][n] = make_float2(m, l);
+    __syncthreads();
+    // thread: row tid / 16, channels 2 (tid % 16) and the next of the 32; lane (row, half) has channel 8 g4 + 4 half + i in place 4 g4 + i
+    const int r = tid / 16, c = 2 * (tid % 16), from = (r + 32 * (c / 4 % 2)) * 17 + c / 8 * 4 + c % 4, row = row0 + r;
+    float top = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFoldWaves; ++w) top = fmaxf(top, wave_ml[w][r].x);
+#pragma unroll
+    for (int w = 0; w < kFoldWaves; ++w) {
+        const float2 ml = wave_ml[w][r];
+        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+        sum += ml.y * f;
+        o0 += sums[w][from] * f;
+        o1 += sums[w][from + 1] * f;
+    }
+    if (row >= s.n * G) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const size_t head = (size_t)(s.start + row / G) * a.lp.H + hk * G + row % G;
+    *reinterpret_cast<uint32_t*>(a.out + head * kHeadDim + db * 32 + c) = Elem<T>::pack(o0 * inv, o1 * inv);
+    if (a.lse_out && db == 0 && c == 0) a.lse_out[head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // ---- host side -----------------------------------------------------------------------------------
@@ -704,16 +854,21 @@ struct TreeSizes {
     size_t pieces_bytes, ml_bytes, partial_bytes;
 };
 
-TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride) {
+template <int BITS> int resident_workgroups(int RG) {
+    return RG == 1 ? TreeShape<BITS, 1>::kResident : RG == 2 ? TreeShape<BITS, 2>::kResident
+           : RG == 4 ? TreeShape<BITS, 4>::kResident : TreeShape<BITS, 8>::kResident;
+}
+
+TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride, bool quantised) {
     TreeSizes z = {};
     const long long rows = (long long)max_new * lp.group;
-    z.RG = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    z.RG = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
     const int R = 32 * z.RG;
     z.row_tiles = (int)((rows + R - 1) / R);
     z.streams = __builtin_popcountll(lp.streaming_mask);
     // row tiles of all sequences: a part of one each, and no more than the tokens there are
     const long long tiles = std::min((long long)batch * z.row_tiles, (long long)total_new * lp.group / R + batch), lists = tiles * lp.Hkv;
-    const int resident = num_compute_units() * kWorkgroupsPerUnit;
+    const int resident = num_compute_units() * (quantised ? resident_workgroups<8>(z.RG) : resident_workgroups<16>(z.RG));
     // list entries as far as the host knows: pages of the table, or of a selection (and those since, which are few)
     const int drafts = ceil_div(max_new, kTile), dense = sel_stride > 0 ? std::min(max_pages, sel_stride + 1) : max_pages;
     const int stream = std::min(max_pages, lp.sink_pages + lp.local_pages);
@@ -726,7 +881,7 @@ TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_ne
     z.exact = z.exact && z.target > 0;
     z.grid = z.target == 0 ? (long long)batch * lp.Hkv * z.row_tiles : z.exact ? z.target : z.target + lists;
     z.grid = (z.grid + 8 + 7) / 8 * 8;
-    z.folds = z.target == 0 ? 0 : (long long)batch * lp.Hkv * z.row_tiles * z.RG;
+    z.folds = z.target == 0 ? 0 : (long long)batch * lp.Hkv * z.row_tiles * z.RG * 4;
     if (z.target) {
         z.pieces_bytes = ((size_t)batch * lp.Hkv * z.row_tiles * sizeof(int2) + 255) / 256 * 256;
         z.ml_bytes = (size_t)z.grid * z.RG * 32 * sizeof(float2);
@@ -736,7 +891,7 @@ TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_ne
 }
 
 template <class T, int BITS> hipError_t launch_tree(const TreeArgs& a, void* workspace, hipStream_t stream) {
-    const TreeSizes z = tree_sizes(a.lp, a.kv.batch, a.total_new, a.max_new, a.kv.max_pages, a.sel_stride);
+    const TreeSizes z = tree_sizes(a.lp, a.kv.batch, a.total_new, a.max_new, a.kv.max_pages, a.sel_stride, BITS != 16);
     if (z.grid > 0x7fffffffLL || z.folds > 0x7fffffffLL) return hipErrorInvalidValue;
     TreeLaunch t = {};
     t.target = z.target;
@@ -751,13 +906,16 @@ template <class T, int BITS> hipError_t launch_tree(const TreeArgs& a, void* wor
         t.partials = reinterpret_cast<float4*>(p + z.pieces_bytes + z.ml_bytes);
     }
     const dim3 grid((unsigned)z.grid), folds((unsigned)z.folds);
-#define LSERVE_TREE(RG)                                                                                                  hipLaunchKernelGGL((draft_tree_kernel<T, BITS, RG>), grid, dim3(RG == 1 ? 128 : 256), 0, stream, a, t);              if (z.folds) hipLaunchKernelGGL((fold_trees_kernel<T, RG>), folds, dim3(256), 0, stream, a, t)
-    if (z.RG == 1) {
+#define LSERVE_TREE(RG)                                                                                                              \
+    case RG:                                                                                                                         \
+        hipLaunchKernelGGL((draft_tree_kernel<T, BITS, RG>), grid, dim3(TreeShape<BITS, RG>::kWaves * kWave), 0, stream, a, t);     \
+        if (z.folds) hipLaunchKernelGGL((fold_trees_kernel<T, RG>), folds, dim3(kFoldThreads), 0, stream, a, t);                     \
+        break
+    switch (z.RG) {
         LSERVE_TREE(1);
-    } else if (z.RG == 2) {
         LSERVE_TREE(2);
-    } else {
         LSERVE_TREE(4);
+        LSERVE_TREE(8);
     }
 #undef LSERVE_TREE
     return hipGetLastError();
@@ -777,8 +935,12 @@ template <class T> hipError_t launch_bits(const TreeArgs& a, void* workspace, hi
 }  // namespace
 
 size_t tree_workspace_bytes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride) {
-    const TreeSizes z = tree_sizes(lp, batch, total_new, max_new, max_pages, sel_stride);
-    return z.pieces_bytes + z.ml_bytes + z.partial_bytes;
+    size_t most = 0;  // one size for pages of every kind
+    for (const bool quantised : {false, true}) {
+        const TreeSizes z = tree_sizes(lp, batch, total_new, max_new, max_pages, sel_stride, quantised);
+        most = std::max(most, z.pieces_bytes + z.ml_bytes + z.partial_bytes);
+    }
+    return most;
 }
 
 hipError_t preload_tree_kernels() {
