@@ -26,14 +26,17 @@ constexpr int kTile = 64;                        // keys of a step: a page, or d
 constexpr int kRowBytes = kHeadDim * 2;          // of a 16-bit row
 constexpr int kTileBytes = kTile * kRowBytes;
 constexpr int kAhead = 4;                        // operand reads in flight ahead of the products
-constexpr int kTableEntries = 256;               // list entries looked up at a time
+constexpr float kSlack = 6.f;                    // a row's reference moves when a weight would pass 2^kSlack
 constexpr int kBlockFloat4 = 16 * kWave;         // outputs of a block of 32 rows, as the lanes hold them
-constexpr int kLeastPiece = 2;                   // list entries
+constexpr int kLeastPiece = 2, kWholeSpan = 48;  // list entries (see make_plan)
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // How a launch is laid out (host).
 struct TreeLaunch {
     int target;     // pieces to cut the lists into, about; 0: lists stay whole
     int exact;      // no more than that
+    int fine;       // there is room for five times as many, where they come out long
     int row_tiles;  // of 32 RG rows, of the longest sequence
     int streams;    // streaming heads
     int slots;      // of pieces in the workspace
@@ -45,6 +48,7 @@ struct TreeLaunch {
 // What sequence b asks for.  Everything is brought inside the arrays, whatever the lengths say.
 struct SeqShape {
     int start, n, len, pages;  // first drafted token, how many, tokens and pages of history
+    int then;                  // pages at the time of the selection
     int dense, stream;         // list entries of a head that attends a selection (or everything), of a streaming head
     int row_tiles;
 };
@@ -63,21 +67,19 @@ template <int R> __device__ __forceinline__ SeqShape seq_shape(const TreeArgs& a
     s.len = (int)min((long long)max(a.kv.seq_lens[b], 0), min((long long)a.kv.max_pages * kTile, 0x7fffffc0LL));
     s.pages = ceil_div(s.len, kTile);
     const int drafts = ceil_div(max(s.n, 0), kTile);
-    int dense = s.pages;
-    if (a.sel_pages) {
-        const int then = min(pages_of(a.sel_seq_len[b]), s.pages);
-        dense = min(then, a.sel_stride) + s.pages - then;
-    }
-    s.dense = dense + drafts;
+    s.then = a.sel_pages ? min(pages_of(a.sel_seq_len[b]), s.pages) : s.pages;
+    s.dense = (a.sel_pages ? min(s.then, a.sel_stride) : s.then) + s.pages - s.then + drafts;
     s.stream = min(a.lp.sink_pages, s.pages) + max(0, s.pages - first_local_page(a.lp, s.len)) + drafts;
     s.row_tiles = s.n > 0 ? ceil_div(s.n * a.lp.group, R) : 0;
     return s;
 }
 
-// Pieces of `span` list entries.
+// Pieces of `span` list entries, or a few more.
 struct TreePlan {
     int span;
-    __device__ __forceinline__ int pieces(int entries) const { return span == 0 ? 1 : ceil_div(entries, span); }
+    float reciprocal;
+    __device__ __forceinline__ static TreePlan of(int span) { return {span, span ? __builtin_amdgcn_rcpf((float)span) : 0.f}; }
+    __device__ __forceinline__ int pieces(int entries) const { return max(1, (int)ceilf((float)entries * reciprocal - 0.01f)); }
     __device__ __forceinline__ int units(const TreeArgs& a, const TreeLaunch& t, const SeqShape& s) const {
         return s.row_tiles * (t.streams * pieces(s.stream) + (a.lp.Hkv - t.streams) * pieces(s.dense));
     }
@@ -87,7 +89,7 @@ __device__ __forceinline__ float wave_sum(float x) { return rows4_sum(row16_sum(
 
 // (own: the shape of sequence `lane`, which is all there is to load for batches of up to 64)
 template <int R> __device__ __forceinline__ TreePlan make_plan(const TreeArgs& a, const TreeLaunch& t, const SeqShape& own) {
-    if (t.target == 0) return {0};
+    if (t.target == 0) return TreePlan::of(0);
     const int lane = threadIdx.x % kWave, batch = a.kv.batch, denses = a.lp.Hkv - t.streams;
     auto total = [&](auto f) {  // of f over the sequences
         float x = f(own);
@@ -96,14 +98,17 @@ template <int R> __device__ __forceinline__ TreePlan make_plan(const TreeArgs& a
         return wave_sum(x);
     };
     const float work = total([&](const SeqShape& s) { return (float)s.row_tiles * ((float)t.streams * s.stream + (float)denses * s.dense); });
-    const int whole = __builtin_amdgcn_readfirstlane((int)min(work / t.target, 1e9f));
-    TreePlan plan = {max(kLeastPiece, (float)whole * t.target < work ? whole + 1 : whole)};
-    if (!t.exact) return plan;
+    // What a workgroup that is always there has to do.  Up to kWholeSpan entries, nothing longer than that stays in one piece; beyond, a quarter
+    // of it, since workgroups with the same number of pages need not take the same time, and those that are quicker then take more.
+    const int each = max(kLeastPiece, (int)min(work / t.target, 1e9f) + 1);
+    const bool fine = t.fine && each > kWholeSpan;
+    TreePlan plan = TreePlan::of(uniform(fine ? max(kWholeSpan, each / 4) : each));
+    if (fine || !t.exact) return plan;
     // as long as it takes to have no more pieces than workgroups that run at once (they are at most twice as many to begin with)
     for (int i = 0; i < 24; ++i) {
         const float count = total([&](const SeqShape& s) { return (float)plan.units(a, t, s); });
-        if (__builtin_amdgcn_readfirstlane(count <= (float)t.target)) break;
-        plan.span += max(1, plan.span / 16);
+        if (uniform(count <= (float)t.target)) break;
+        plan = TreePlan::of(plan.span + max(1, plan.span / 16));
     }
     return plan;
 }
@@ -144,6 +149,7 @@ __device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t
         shape.n = __builtin_amdgcn_readlane(s.n, at);
         shape.len = __builtin_amdgcn_readlane(s.len, at);
         shape.pages = __builtin_amdgcn_readlane(s.pages, at);
+        shape.then = __builtin_amdgcn_readlane(s.then, at);
         shape.dense = __builtin_amdgcn_readlane(s.dense, at);
         shape.stream = __builtin_amdgcn_readlane(s.stream, at);
         shape.row_tiles = __builtin_amdgcn_readlane(s.row_tiles, at);
@@ -164,8 +170,6 @@ __device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t
     u.hk = __builtin_ctzll(heads);
     return true;
 }
-
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
@@ -216,7 +220,7 @@ template <int BITS, int RG> struct TreeShape {
     static constexpr int kWaves = RG * kKeyHalves;
     // 16-bit tiles: three on the way while one is worked on, one workgroup to a compute unit, where rows are few and memory is the bound;
     // two stages and two workgroups where a step's products take as long as its tiles.
-    static constexpr int kStages = kQuant || RG == 4 ? 2 : 4;
+    static constexpr int kStages = kQuant || RG <= 4 ? 2 : 4;
     static constexpr int kResident = kStages == 2 && RG <= 4 ? 2 : 1;
     static constexpr int kPerSimd = (kResident * kWaves + 3) / 4;  // wavefronts
 };
@@ -229,8 +233,7 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
     constexpr int kLoads = 16 / kWaves;  // 1 KiB loads per wave, operand and step
     __shared__ __attribute__((aligned(1024))) unsigned char k_lds[kStages][kTileBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char v_lds[kStages][kTileBytes];
-    __shared__ int2 table[kTableEntries];                          // (position of the page or drafted tile, physical page or -1)
-    __shared__ __attribute__((aligned(16))) uint32_t k_scale[QUANT ? 2 : 1][QUANT ? kTile : 4];  // (scale, zero) of the keys of a stage
+    __shared__ __attribute__((aligned(16))) float k_scale[QUANT ? 2 : 1][2][QUANT ? kTile : 4];  // of the keys of a stage, times the softmax scale: scale, zero
     __shared__ float2 fold_ml[RG][32];
     __shared__ unsigned spoiled_keys[2];
     __shared__ int deepest[kWaves];  // tile of the wave's rows
@@ -240,15 +243,17 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
     SeqShape mine = {};
     if (t.target && lane < a.kv.batch) mine = seq_shape<R>(a, lane);
     const TreePlan plan = make_plan<R>(a, t, mine);
-    // Workgroup ids go round-robin over the XCDs: an XCD takes neighbouring pieces, whose row tiles share keys in its L2.
+    // Workgroup ids go round-robin over the XCDs: row tiles of a piece, which read the same keys, go to one, and its L2 has them.
     constexpr int kXcds = 8;
-    const int unit = (blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds;  // gridDim.x is a multiple of kXcds
+    const int cycle = kXcds * t.row_tiles, place = blockIdx.x % cycle;
+    const int unit = (int)blockIdx.x - place + place % kXcds * t.row_tiles + place / kXcds;
     TreeUnit u;
-    SeqShape s;
+    SeqShape s = {};
     if (!find_unit<R>(a, t, plan, mine, unit, u, s)) return;
     // (all of it comes out of lane arithmetic, and what stays in vector registers takes the addresses of the walk there with it)
     u.b = uniform(u.b), u.hk = uniform(u.hk), u.row_tile = uniform(u.row_tile), u.piece = uniform(u.piece), u.pieces = uniform(u.pieces);
     s.start = uniform(s.start), s.n = uniform(s.n), s.len = uniform(s.len), s.pages = uniform(s.pages);
+    s.then = uniform(s.then), s.dense = uniform(s.dense), s.stream = uniform(s.stream);
     const int b = u.b, hk = u.hk, G = a.lp.group, rows = s.n * G;
     const bool streaming = (a.lp.streaming_mask >> hk) & 1ull;
     if (u.piece == 0 && tid == 0 && t.target) t.pieces[(b * a.lp.Hkv + hk) * t.row_tiles + u.row_tile] = make_int2(unit, u.pieces);
@@ -256,38 +261,32 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
     // ---- the list: entries of history, then tiles of drafted tokens
     const int drafts = ceil_div(s.n, kTile);
     const bool ring = in_stream_pool(a.lp, a.kv, hk);
-    int listed = s.pages, first_new = 0;  // entries that a list or a formula names; pages from first_new on follow
-    if (streaming) {
-        listed = min(a.lp.sink_pages, s.pages);
-        first_new = first_local_page(a.lp, s.len);
-    } else if (a.sel_pages) {
-        listed = uniform(min(max(a.sel_count[(size_t)b * a.lp.Hkv + hk], 0), a.sel_stride));
-        first_new = uniform(pages_of(a.sel_seq_len[b]));
-    } else {
-        first_new = s.pages;
-    }
-    const int history = listed + max(0, s.pages - first_new), entries = history + drafts;
-    // (fewer entries than the plan counted on leave some pieces empty)
+    const int entries = streaming ? s.stream : s.dense, history = entries - drafts;
+    // (the first `listed` entries are named by a list or a formula, the pages from first_new on follow; a list that holds fewer than it may
+    // ends in entries of nothing, so that its length need not be waited for)
+    const int listed = streaming ? min(a.lp.sink_pages, s.pages) : a.sel_pages ? min(s.then, a.sel_stride) : s.pages;
+    const int first_new = streaming ? first_local_page(a.lp, s.len) : s.then;
     const int share = entries / u.pieces, rest = entries - share * u.pieces;
     const int e0 = uniform(u.piece * share + min(u.piece, rest)), e1 = uniform(e0 + share + (u.piece < rest ? 1 : 0));
-    const int* sel = a.sel_pages ? a.sel_pages + ((size_t)b * a.lp.Hkv + hk) * a.sel_stride : nullptr;
-    // looks up entries from..from + 255 of the list
+    const size_t head = (size_t)b * a.lp.Hkv + hk;
+    // Entry from + lane: (position of the page, physical page) or (drafted tile, -1); a position behind the last page: nothing of it is read.
+    // Lane i of every wave has entry i of a stretch of 64: reading it costs no trip to memory, and no wave waits for another.
     auto look_up = [&](int from) {
-        for (int i = tid; i < kTableEntries; i += kWaves * kWave) {
-            const int e = from + i;
-            if (e >= e1) break;
-            int2 w = make_int2(e - history, -1);
-            if (e < history) {
-                int p = e < listed ? (streaming || !sel ? e : sel[e]) : first_new + (e - listed);
-                if (p < 0 || p >= s.pages) {
-                    w = make_int2(s.pages, 0);  // no such page: nothing of it is read
-                } else {
-                    const int phys = ring ? a.kv.ring_table[(size_t)b * a.kv.ring + ring_slot(a.lp, p)] : a.kv.page_table[(size_t)b * a.kv.max_pages + p];
-                    w = make_int2(p, ring ? max(phys, 0) : min(max(phys, 0), a.kv.num_pages - 1));
-                }
+        const int e = from + lane;
+        int2 w = make_int2(s.pages, 0);
+        if (e < e1 && e >= history) w = make_int2(e - history, -1);
+        if (e < min(e1, history)) {
+            int p = e < listed ? e : first_new + (e - listed);
+            if (a.sel_pages && !streaming && e < listed) {
+                p = a.sel_pages[head * a.sel_stride + e];
+                if (e >= a.sel_count[head]) p = -1;
             }
-            table[i] = w;
+            if (p >= 0 && p < s.pages) {
+                const int phys = ring ? a.kv.ring_table[(size_t)b * a.kv.ring + ring_slot(a.lp, p)] : a.kv.page_table[(size_t)b * a.kv.max_pages + p];
+                w = make_int2(p, ring ? max(phys, 0) : min(max(phys, 0), a.kv.num_pages - 1));
+            }
         }
+        return w;
     };
 
     // ---- the wave's rows: row r is query head r % G of the group, drafted token r / G; rows past the end repeat the last
@@ -308,7 +307,7 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
         key_tile = max(a.positions ? a.positions[s.start + key] : s.len + key, s.len) / kTile;
         own_tile /= kTile;
     }
-    look_up(e0);
+    int2 stretch = look_up(e0);
     // (pinned once the first keys are on their way: left alone the loads sink into the loop, where they wait for its prefetch)
     auto pin_queries = [&] {
 #pragma unroll
@@ -324,26 +323,36 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
     const unsigned new_row_bytes = (unsigned)a.lp.Hkv * kRowBytes;
     const size_t new_offset = ((size_t)s.start * a.lp.Hkv + hk) * kRowBytes;
     const int my_row = wave * (kTile / kWaves) + lane / 16;
+    constexpr int kFroms = kLoads < 4 ? kLoads : 4;
+    unsigned k_from[kFroms];
+#pragma unroll
+    for (int i = 0; i < kFroms; ++i) k_from[i] = (unsigned)(my_row + 4 * i) * kRowBytes + k_chunk_pos(my_row + 4 * i, lane % 16) * 16;
+    const unsigned v_from = (unsigned)my_row * kRowBytes + v_chunk_pos(my_row, lane % 16) * 16;
     // rows of an entry that exist
     auto live_rows = [&](int2 w) { return w.y < 0 ? min(s.n - w.x * kTile, kTile) : min(s.len - w.x * kTile, kTile); };
-    auto entry = [&](int e) {  // of the stretch in the table
-        const int2 w = table[(e - e0) % kTableEntries];
-        return make_int2(__builtin_amdgcn_readfirstlane(w.x), __builtin_amdgcn_readfirstlane(w.y));
-    };
     auto fetch = [&](int2 w, unsigned char* kd, unsigned char* vd) {  // 16-bit rows; those past the last one repeat it
         const int live = max(live_rows(w), 1);  // (nothing of an entry without a page is used, but the loads are counted)
         const bool drafted = w.y < 0;
         const unsigned long long offset = drafted ? new_offset + (size_t)w.x * kTile * new_row_bytes : (size_t)w.y * page_bytes;
         const unsigned long long ks = uniform64((unsigned long long)(drafted ? (const unsigned char*)a.k_new : k_base) + offset);
         const unsigned long long vs = uniform64((unsigned long long)(drafted ? (const unsigned char*)a.v_new : v_base) + offset);
+        const unsigned kd_at = uniform(lds_address(kd) + wave * kLoads * 1024), vd_at = uniform(lds_address(vd) + wave * kLoads * 1024);
+        if (!drafted && live == kTile) {
+            // sixteen rows on the permutation of K repeats itself, four rows on that of V
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                dma_load16(ks + (unsigned)(i / 4) * (16 * kRowBytes), k_from[i % kFroms], kd_at + i * 1024);
+                dma_load16(vs + (unsigned)i * (4 * kRowBytes), v_from, vd_at + i * 1024);
+            }
+            return;
+        }
         const unsigned stride = drafted ? new_row_bytes : (unsigned)kRowBytes;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int r = my_row + 4 * i;
             const unsigned at = (unsigned)min(r, live - 1) * stride;
-            const unsigned to = (wave * kLoads + i) * 1024;
-            dma_load16(ks, at + k_chunk_pos(r, lane % 16) * 16, __builtin_amdgcn_readfirstlane(lds_address(kd) + to));
-            dma_load16(vs, at + v_chunk_pos(r, lane % 16) * 16, __builtin_amdgcn_readfirstlane(lds_address(vd) + to));
+            dma_load16(ks, at + k_chunk_pos(r, lane % 16) * 16, kd_at + i * 1024);
+            dma_load16(vs, at + v_chunk_pos(r, lane % 16) * 16, vd_at + i * 1024);
         }
     };
     // quantised rows on their way through registers
@@ -386,7 +395,10 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
                 const unsigned to = (wave * kLoads + i) * 1024 + lane * 16;
                 *reinterpret_cast<uint4*>(k_lds[stage] + to) = codes8<T, BITS>(staged.k[i]);
                 *reinterpret_cast<uint4*>(v_lds[stage] + to) = dequantise8<T, BITS>(staged.v[i], staged.vz[i]);
-                if (lane % 16 == 0) k_scale[stage][my_row + 4 * i] = staged.kz[i];
+                if (lane % 16 == 0) {
+                    k_scale[stage][0][my_row + 4 * i] = Elem<F16>::lo(staged.kz[i]) * a.lp.sm_scale_log2;
+                    k_scale[stage][1][my_row + 4 * i] = Elem<F16>::hi(staged.kz[i]) * a.lp.sm_scale_log2;
+                }
             }
         }
     };
@@ -487,12 +499,10 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
                 __builtin_amdgcn_sched_barrier(0);
             }
             score = halves_sum(score);
-            if (codes) {
-                const uint32_t z = k_scale[QUANT ? stage : 0][QUANT ? key : 0];
-                score = __builtin_fmaf(score, Elem<F16>::lo(z), Elem<F16>::hi(z) * q_sum);
-            }
             const bool on = bits >> key & 1ull;
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(score, a.lp.sm_scale_log2, off));
+            const float p = __builtin_amdgcn_exp2f(codes ? __builtin_fmaf(score, k_scale[QUANT ? stage : 0][0][QUANT ? key : 0],
+                                                                          __builtin_fmaf(k_scale[QUANT ? stage : 0][1][QUANT ? key : 0], q_sum, off))
+                                                         : __builtin_fmaf(score, a.lp.sm_scale_log2, off));
             const unsigned char* const page = v_base + (size_t)w.y * page_bytes;
             const unsigned char* const src =
                 drafted ? (const unsigned char*)a.v_new + new_offset + ((size_t)w.x * kTile + from) * new_row_bytes
@@ -521,13 +531,15 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
         }
     };
 
-    auto work_on = [&](int2 w, int stage, unsigned long long spoiled) __attribute__((always_inline)) {
+    auto work_on = [&](int2 w, int stage, bool ragged, unsigned long long spoiled) __attribute__((always_inline)) {
         const int live = live_rows(w);
         if (live <= 0 || !wave_has_rows) return;
         const bool codes = QUANT && w.y >= 0;
-        const unsigned long long bits = seen(w, live);
-        if (!__any(bits != 0)) return;
-        const bool mixed = __any(~bits != 0);
+        unsigned long long bits = ~0ull;
+        if (ragged) {
+            bits = seen(w, live);
+            if (!__any(bits != 0)) return;
+        }
         const unsigned char *ks = k_lds[stage] + kg * NB * 32 * kRowBytes, *vs = v_lds[stage] + kg * NB * 32 * kRowBytes;
         float16_t sc[NB] = {};
 #pragma unroll
@@ -543,19 +555,29 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+        // Exponents, relative to the row's reference (0 before it has one).  The reference is not the maximum so far but one that follows it at
+        // a distance of up to kSlack: weights up to 2^kSlack do no harm in any of the types, and outputs are rescaled a few times a list
+        // instead of in most steps.
+        const bool unset = m_run == -INFINITY;
+        float off = unset ? 0.f : -m_run;
         if (codes) {
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
                 for (int g4 = 0; g4 < 4; ++g4) {
-                    const uint4 z4 = *reinterpret_cast<const uint4*>(&k_scale[QUANT ? stage : 0][QUANT ? (kg * NB + kb) * 32 + 8 * g4 + 4 * half : 0]);
-                    const uint32_t z[4] = {z4.x, z4.y, z4.z, z4.w};
+                    const int key = QUANT ? (kg * NB + kb) * 32 + 8 * g4 + 4 * half : 0;
+                    const float4 z = *reinterpret_cast<const float4*>(&k_scale[QUANT ? stage : 0][0][key]), o = *reinterpret_cast<const float4*>(&k_scale[QUANT ? stage : 0][1][key]);
+                    const float z4[4] = {z.x, z.y, z.z, z.w}, o4[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        sc[kb][4 * g4 + i] = __builtin_fmaf(sc[kb][4 * g4 + i], Elem<F16>::lo(z[i]), Elem<F16>::hi(z[i]) * q_sum);
+                    for (int i = 0; i < 4; ++i) sc[kb][4 * g4 + i] = __builtin_fmaf(sc[kb][4 * g4 + i], z4[i], __builtin_fmaf(o4[i], q_sum, off));
                 }
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[kb][i] = __builtin_fmaf(sc[kb][i], a.lp.sm_scale_log2, off);
         }
-        if (mixed) {
+        if (ragged) {
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb) {
                 const unsigned mine = (unsigned)(bits >> (32 * (kg * NB + kb))) >> (4 * half);
@@ -564,35 +586,41 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
                     if (!(mine >> (8 * (i / 4) + i % 4) & 1u)) sc[kb][i] = -INFINITY;
             }
         }
-        float top = -INFINITY;
+        float top = sc[0][0];
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
-        top = halves_max(top) * a.lp.sm_scale_log2;
-        const float m_new = fmaxf(m_run, top);
-        if (__any(m_new > m_run)) {
-            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        top = halves_max(top);
+        const bool moves = unset ? top > -INFINITY : top > kSlack;
+        if (__builtin_expect(__any(moves), 0)) {
+            const float delta = moves ? top : 0.f, alpha = unset ? 0.f : __builtin_amdgcn_exp2f(-delta);
             l_run *= alpha;
 #pragma unroll
             for (int db = 0; db < 4; ++db)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[db][i] *= alpha;
-            m_run = m_new;
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[kb][i] -= delta;
+            if (moves) m_run = unset ? delta : m_run + delta;
+            off = m_run == -INFINITY ? 0.f : -m_run;
         }
-        const float off = m_run == -INFINITY ? 0.f : -m_run;
         uint4 pb[NB][2];
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) {
             float p[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][i], a.lp.sm_scale_log2, off));
-                l_run += p[i];  // unrounded; the second product takes them in the layer's type, which is what its operands are
+                p[i] = __builtin_amdgcn_exp2f(sc[kb][i]);
+                sum[i % 2] += p[i];  // unrounded; the second product takes them in the layer's type, which is what its operands are
             }
             pb[kb][0] = pack8<T>(p);
             pb[kb][1] = pack8<T>(p + 8);
         }
+        l_run += sum[0] + sum[1];
         auto values = [&](int step, int db) {  // V^T operand: channel 32 db + n of the lane's eight keys of the step's sixteen
             const uint2 lo = lds_read_transposed(vs + (4 * step) * 1024 + voff[db]);
             const uint2 hi = lds_read_transposed(vs + (4 * step + 2) * 1024 + voff[db]);
@@ -630,7 +658,7 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
     auto step = [&](int2 w, int stage) __attribute__((always_inline)) {
         const int live = live_rows(w);
         const bool ragged = live > 0 && (live < kTile || w.y < 0 || (streaming && w.x >= a.lp.sink_pages && w.x <= deepest_tile - a.lp.local_pages));
-        work_on(w, stage, ragged ? clear_spoiled(w, stage) : 0ull);
+        work_on(w, stage, ragged, ragged ? clear_spoiled(w, stage) : 0ull);
     };
     auto find_deepest = [&] {  // past a barrier
 #pragma unroll
@@ -638,27 +666,24 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
         deepest_tile = uniform(deepest_tile);
     };
     const int2 nothing = make_int2(s.pages, 0);
-    // entry e of the list, whose stretch of the table is looked up when its first one is asked for (in order, by all)
+    // entry e of the list; asked for in order
     auto next_entry = [&](int e) {
         if (e >= e1) return nothing;
-        if ((e - e0) % kTableEntries == 0 && e > e0) {
-            __syncthreads();
-            look_up(e);
-            __syncthreads();
-        }
-        return entry(e);
+        const int i = (e - e0) % kWave;
+        if (i == 0 && e > e0) stretch = look_up(e);
+        return make_int2(__builtin_amdgcn_readlane(stretch.x, i), __builtin_amdgcn_readlane(stretch.y, i));
     };
     if constexpr (!QUANT) {
         // Tiles of up to kStages - 1 steps are on their way.  Loads arrive in order, kPerStep a step and wave: those of step e are there once no
         // more than those of the steps behind it are missing.
         constexpr int kPerStep = 2 * kLoads;
         int2 w[kStages];
-        __syncthreads();
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) {
             w[i] = next_entry(e0 + i);
             if (e0 + i < e1) fetch(w[i], k_lds[i], v_lds[i]);
         }
+        __syncthreads();
         find_deepest();
         pin_queries();
         for (int e = e0; e < e1; e += kStages) {
@@ -685,18 +710,17 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
         auto fetch_drafted = [&](int2 w, int stage) {
             if (w.y < 0) fetch(w, k_lds[stage], v_lds[stage]);
         };
-        __syncthreads();
         int2 w0 = next_entry(e0), w1 = next_entry(e0 + 1);
         if (e0 < e1) {
             fetch_drafted(w0, 0);
             fetch_codes(w0);
             store_staged(0);
         }
-        find_deepest();
         pin_queries();
         wait_loads<0>();
         if (e0 + 1 < e1) fetch_codes(w1);
         __syncthreads();
+        find_deepest();
         for (int e = e0; e < e1; ++e) {
             const int stage = (e - e0) & 1;
             const int2 w2 = next_entry(e + 2);
@@ -849,7 +873,7 @@ __global__ __launch_bounds__(kFoldThreads) void fold_trees_kernel(TreeArgs a, Tr
 namespace {
 
 struct TreeSizes {
-    int RG, row_tiles, target, exact, streams;
+    int RG, row_tiles, target, exact, fine, streams;
     long long grid, folds;  // workgroups of the two kernels
     size_t pieces_bytes, ml_bytes, partial_bytes;
 };
@@ -873,14 +897,13 @@ TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_ne
     const int drafts = ceil_div(max_new, kTile), dense = sel_stride > 0 ? std::min(max_pages, sel_stride + 1) : max_pages;
     const int stream = std::min(max_pages, lp.sink_pages + lp.local_pages);
     const long long shortest = tiles * ((lp.Hkv - z.streams) * (long long)(dense + drafts) + z.streams * (long long)(stream + drafts)) / kLeastPiece;
-    // Few lists: as many pieces as workgroups run at once.  More: three times as many, so that what is left over at the end is short.
-    // Plenty: whole lists.
-    z.exact = 2 * lists <= resident && 2 * lists <= shortest;
-    z.target = lists >= 8LL * resident || std::max(dense, stream) + drafts <= kLeastPiece
-                   ? 0 : (int)std::min<long long>(shortest, z.exact ? resident : 3 * resident);
-    z.exact = z.exact && z.target > 0;
-    z.grid = z.target == 0 ? (long long)batch * lp.Hkv * z.row_tiles : z.exact ? z.target : z.target + lists;
-    z.grid = (z.grid + 8 + 7) / 8 * 8;
+    z.target = lists >= 8LL * resident || std::max(dense, stream) + drafts <= kLeastPiece ? 0 : (int)std::min<long long>(shortest, resident);
+    z.exact = z.target > 0 && 2 * lists <= z.target;
+    // pieces: one for every list, and of `target` times what make_plan makes of a workgroup's share
+    z.fine = z.target > 0 && shortest * kLeastPiece / z.target >= kWholeSpan;
+    z.grid = z.target == 0 ? (long long)batch * lp.Hkv * z.row_tiles : (z.fine ? 5LL : 1LL) * z.target + lists;
+    const long long cycle = 8LL * z.row_tiles;  // see the kernel
+    z.grid = (z.grid + cycle - 1) / cycle * cycle;
     z.folds = z.target == 0 ? 0 : (long long)batch * lp.Hkv * z.row_tiles * z.RG * 4;
     if (z.target) {
         z.pieces_bytes = ((size_t)batch * lp.Hkv * z.row_tiles * sizeof(int2) + 255) / 256 * 256;
@@ -896,6 +919,7 @@ template <class T, int BITS> hipError_t launch_tree(const TreeArgs& a, void* wor
     TreeLaunch t = {};
     t.target = z.target;
     t.exact = z.exact;
+    t.fine = z.fine;
     t.row_tiles = z.row_tiles;
     t.streams = z.streams;
     t.slots = z.target ? (int)z.grid : 0;
