@@ -28,7 +28,7 @@ constexpr int kTileBytes = kTile * kRowBytes;
 constexpr int kAhead = 4;                        // operand reads in flight ahead of the products
 constexpr float kSlack = 6.f;                    // a row's reference moves when a weight would pass 2^kSlack
 constexpr int kBlockFloat4 = 16 * kWave;         // outputs of a block of 32 rows, as the lanes hold them
-constexpr int kLeastPiece = 2, kWholeSpan = 48;  // list entries (see make_plan)
+constexpr int kLeastPiece = 2;                   // list entries
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -36,7 +36,6 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 struct TreeLaunch {
     int target;     // pieces to cut the lists into, about; 0: lists stay whole
     int exact;      // no more than that
-    int fine;       // there is room for five times as many, where they come out long
     int row_tiles;  // of 32 RG rows, of the longest sequence
     int streams;    // streaming heads
     int slots;      // of pieces in the workspace
@@ -98,12 +97,9 @@ template <int R> __device__ __forceinline__ TreePlan make_plan(const TreeArgs& a
         return wave_sum(x);
     };
     const float work = total([&](const SeqShape& s) { return (float)s.row_tiles * ((float)t.streams * s.stream + (float)denses * s.dense); });
-    // What a workgroup that is always there has to do.  Up to kWholeSpan entries, nothing longer than that stays in one piece; beyond, a quarter
-    // of it, since workgroups with the same number of pages need not take the same time, and those that are quicker then take more.
-    const int each = max(kLeastPiece, (int)min(work / t.target, 1e9f) + 1);
-    const bool fine = t.fine && each > kWholeSpan;
-    TreePlan plan = TreePlan::of(uniform(fine ? max(kWholeSpan, each / 4) : each));
-    if (fine || !t.exact) return plan;
+    // what a workgroup that is always there has to do: nothing longer than that stays in one piece
+    TreePlan plan = TreePlan::of(uniform(max(kLeastPiece, (int)min(work / t.target, 1e9f) + 1)));
+    if (!t.exact) return plan;
     // as long as it takes to have no more pieces than workgroups that run at once (they are at most twice as many to begin with)
     for (int i = 0; i < 24; ++i) {
         const float count = total([&](const SeqShape& s) { return (float)plan.units(a, t, s); });
@@ -171,15 +167,52 @@ __device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t
     return true;
 }
 
-template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 template <class T> struct BitsOf;
 template <> struct BitsOf<F16> { static constexpr uint32_t exponent = 0x7c00u; };
 template <> struct BitsOf<BF16> { static constexpr uint32_t exponent = 0x7f80u; };
 
-// Eight codes of a quantised row as numbers of the layer's type (exact: 8 bits fit the mantissas of both).
+// Keys' codes as operands of the layer's type, exactly, a permutation of bytes to two of them where there is a number whose low bits they can be: the
+// operand is code * unit + offset, and unit and offset go into the scale and zero that its score meets in fp32.
+//   fp16: a code alone is the subnormal code * 2^-24, which the matrix instructions take at its value.
+//   bf16: 0x4300 and four bits are 128 + code.  Eight bits do not fit behind a power of two; they are converted.
+template <class T, int BITS> struct KeyCodes;
+template <int BITS> struct KeyCodes<F16, BITS> {
+    static constexpr float unit = 0x1p-24f, offset = 0.f;
+    static constexpr uint32_t high = 0;
+};
+template <> struct KeyCodes<BF16, 4> {
+    static constexpr float unit = 1.f, offset = 128.f;
+    static constexpr uint32_t high = 0x43434343u;
+};
+template <> struct KeyCodes<BF16, 8> {
+    static constexpr float unit = 1.f, offset = 0.f;
+    static constexpr uint32_t high = 0;
+};
 template <class T, int BITS> __device__ __forceinline__ uint4 codes8(uint2 codes) {
-    return dequantise8<T, BITS>(codes, 0x00003c00u);  // scale 1, zero 0
+    uint32_t lo = codes.x, hi = codes.y;  // channels 0..3 and 4..7, one byte each
+    if constexpr (BITS == 4) {
+        hi = (codes.x >> 4) & 0x0f0f0f0fu;
+        lo = codes.x & 0x0f0f0f0fu;
+    }
+    if constexpr (std::is_same<T, BF16>::value && BITS == 8) {
+        auto pair = [](uint32_t word, int at) {  // whole numbers up to 255 are the upper halves of their fp32 numbers
+            const float a = (float)(word >> (8 * at) & 0xffu), b = (float)(word >> (8 * at + 8) & 0xffu);
+            return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
+        };
+        return make_uint4(pair(lo, 0), pair(lo, 2), pair(hi, 0), pair(hi, 2));
+    } else {
+        constexpr uint32_t high = KeyCodes<T, BITS>::high;
+        return make_uint4(__builtin_amdgcn_perm(high, lo, 0x04010400u), __builtin_amdgcn_perm(high, lo, 0x04030402u),
+                          __builtin_amdgcn_perm(high, hi, 0x04010400u), __builtin_amdgcn_perm(high, hi, 0x04030402u));
+    }
+}
+
+__device__ __forceinline__ uint2 two_words(uint2 x) { return x; }
+__device__ __forceinline__ uint2 two_words(uint32_t x) { return make_uint2(x, 0u); }
+__device__ __forceinline__ uint32_t halved(uint32_t two) {  // of fp16
+    const half2_t h = {(_Float16)0.5f, (_Float16)0.5f};
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, two) * h);
 }
 
 // A block of 32 output rows, O^T in the lanes ((n, half) holds channels 32 db + 8 (i / 4) + 4 half + i % 4 of row n), out through 8 KiB of LDS so
@@ -213,29 +246,20 @@ __device__ __forceinline__ void store_lse(const TreeArgs& a, float m, float l, c
 
 }  // namespace
 
-// How a workgroup of RG row blocks is made up.
-template <int BITS, int RG> struct TreeShape {
-    static constexpr bool kQuant = BITS != 16;
-    static constexpr int kKeyHalves = RG <= 2 ? 2 : 1;  // wavefronts that share a step's keys
-    static constexpr int kWaves = RG * kKeyHalves;
-    // 16-bit tiles: three on the way while one is worked on, one workgroup to a compute unit, where rows are few and memory is the bound;
-    // two stages and two workgroups where a step's products take as long as its tiles.
-    static constexpr int kStages = kQuant || RG <= 4 ? 2 : 4;
-    static constexpr int kResident = kStages == 2 && RG <= 4 ? 2 : 1;
-    static constexpr int kPerSimd = (kResident * kWaves + 3) / 4;  // wavefronts
-};
+// Wavefronts of a workgroup: RG row blocks, and with few of them two that share a step's keys.
+constexpr int tree_waves(int RG) { return RG == 4 ? 4 : 2 * RG; }
 
 template <class T, int BITS, int RG>
-__global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draft_tree_kernel(TreeArgs a, TreeLaunch t) {
-    using Shape = TreeShape<BITS, RG>;
-    constexpr bool QUANT = Shape::kQuant;
-    constexpr int KG = Shape::kKeyHalves, kWaves = Shape::kWaves, NB = 2 / KG, R = 32 * RG, kStages = Shape::kStages;
+__global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void draft_tree_kernel(TreeArgs a, TreeLaunch t) {
+    constexpr bool QUANT = BITS != 16;
+    constexpr int kWaves = tree_waves(RG), KG = kWaves / RG, NB = 2 / KG, R = 32 * RG;
     constexpr int kLoads = 16 / kWaves;  // 1 KiB loads per wave, operand and step
-    __shared__ __attribute__((aligned(1024))) unsigned char k_lds[kStages][kTileBytes];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_lds[kStages][kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_lds[2][kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_lds[2][kTileBytes];
     __shared__ __attribute__((aligned(16))) float k_scale[QUANT ? 2 : 1][2][QUANT ? kTile : 4];  // of the keys of a stage, times the softmax scale: scale, zero
     __shared__ float2 fold_ml[RG][32];
     __shared__ unsigned spoiled_keys[2];
+    __shared__ int spoiled[2];  // does a tile that some row does not see whole hold values that are not numbers?
     __shared__ int deepest[kWaves];  // tile of the wave's rows
 
     const int tid = threadIdx.x, lane = tid % kWave, n = lane % 32, half = lane / 32;
@@ -271,7 +295,7 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
     const size_t head = (size_t)b * a.lp.Hkv + hk;
     // Entry from + lane: (position of the page, physical page) or (drafted tile, -1); a position behind the last page: nothing of it is read.
     // Lane i of every wave has entry i of a stretch of 64: reading it costs no trip to memory, and no wave waits for another.
-    auto look_up = [&](int from) {
+    auto look_up = [&](int from) __attribute__((always_inline)) {
         const int e = from + lane;
         int2 w = make_int2(s.pages, 0);
         if (e < e1 && e >= history) w = make_int2(e - history, -1);
@@ -309,7 +333,7 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
     }
     int2 stretch = look_up(e0);
     // (pinned once the first keys are on their way: left alone the loads sink into the loop, where they wait for its prefetch)
-    auto pin_queries = [&] {
+    auto pin_queries = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qreg[kk].x), "+v"(qreg[kk].y), "+v"(qreg[kk].z), "+v"(qreg[kk].w));
     };
@@ -329,8 +353,8 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
     for (int i = 0; i < kFroms; ++i) k_from[i] = (unsigned)(my_row + 4 * i) * kRowBytes + k_chunk_pos(my_row + 4 * i, lane % 16) * 16;
     const unsigned v_from = (unsigned)my_row * kRowBytes + v_chunk_pos(my_row, lane % 16) * 16;
     // rows of an entry that exist
-    auto live_rows = [&](int2 w) { return w.y < 0 ? min(s.n - w.x * kTile, kTile) : min(s.len - w.x * kTile, kTile); };
-    auto fetch = [&](int2 w, unsigned char* kd, unsigned char* vd) {  // 16-bit rows; those past the last one repeat it
+    auto live_rows = [&](int2 w) __attribute__((always_inline)) { return w.y < 0 ? min(s.n - w.x * kTile, kTile) : min(s.len - w.x * kTile, kTile); };
+    auto fetch = [&](int2 w, unsigned char* kd, unsigned char* vd) __attribute__((always_inline)) {  // 16-bit rows; those past the last one repeat it
         const int live = max(live_rows(w), 1);  // (nothing of an entry without a page is used, but the loads are counted)
         const bool drafted = w.y < 0;
         const unsigned long long offset = drafted ? new_offset + (size_t)w.x * kTile * new_row_bytes : (size_t)w.y * page_bytes;
@@ -355,69 +379,86 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
             dma_load16(vs, at + v_chunk_pos(r, lane % 16) * 16, vd_at + i * 1024);
         }
     };
-    // quantised rows on their way through registers
+    // Quantised rows on their way through registers: per load the codes of this lane's 16-byte place (8 channels) and the (scale, zero) of its
+    // V row; of the K rows one wave has all, a lane each.
+    constexpr int kCodeBytes = kHeadDim * BITS / 8;  // of a row
+    using Codes = typename std::conditional<BITS == 8, uint2, uint32_t>::type;
     struct Staged {
-        uint2 k[kLoads], v[kLoads];
-        uint32_t kz[kLoads], vz[kLoads];
+        Codes k[kLoads], v[kLoads];
+        uint32_t vz[kLoads], kz;
         bool on;
     } staged;
     staged.on = false;
-    auto fetch_codes = [&](int2 w) {
+    unsigned k_code[QUANT ? kFroms : 1], v_code = 0;  // from the page to the places of a full one (see k_from)
+    if constexpr (QUANT) {
+#pragma unroll
+        for (int i = 0; i < kFroms; ++i) k_code[i] = (unsigned)(my_row + 4 * i) * kCodeBytes + k_chunk_pos(my_row + 4 * i, lane % 16) * BITS;
+        v_code = (unsigned)my_row * kCodeBytes + v_chunk_pos(my_row, lane % 16) * BITS;
+    }
+    auto fetch_codes = [&](int2 w) __attribute__((always_inline)) {
         if constexpr (QUANT) {
             const int live = live_rows(w);
             staged.on = w.y >= 0 && live > 0;
             if (!staged.on) return;
-            const unsigned char *kp = k_base + (size_t)w.y * page_bytes, *vp = v_base + (size_t)w.y * page_bytes;
+            const unsigned long long page = (unsigned long long)w.y * page_bytes;
+            const unsigned char* const kp = reinterpret_cast<const unsigned char*>(uniform64((unsigned long long)k_base + page));
+            const unsigned char* const vp = reinterpret_cast<const unsigned char*>(uniform64((unsigned long long)v_base + page));
+            if (live == kTile) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int r = my_row + 4 * i, from = min(r, live - 1);
-                const unsigned char* kr = kp + from * (kHeadDim * BITS / 8) + k_chunk_pos(r, lane % 16) * BITS;
-                const unsigned char* vr = vp + from * (kHeadDim * BITS / 8) + v_chunk_pos(r, lane % 16) * BITS;
-                if constexpr (BITS == 8) {
-                    staged.k[i] = *reinterpret_cast<const uint2*>(kr);
-                    staged.v[i] = *reinterpret_cast<const uint2*>(vr);
-                } else {
-                    staged.k[i] = make_uint2(*reinterpret_cast<const uint32_t*>(kr), 0u);
-                    staged.v[i] = make_uint2(*reinterpret_cast<const uint32_t*>(vr), 0u);
+                for (int i = 0; i < kLoads; ++i) {
+                    staged.k[i] = *reinterpret_cast<const Codes*>(kp + (k_code[i % kFroms] + i / 4 * 16 * kCodeBytes));
+                    staged.v[i] = *reinterpret_cast<const Codes*>(vp + (v_code + i * 4 * kCodeBytes));
+                    staged.vz[i] = *reinterpret_cast<const uint32_t*>(vp + (kTile * kCodeBytes + (unsigned)my_row * 4 + i * 16));
                 }
-                staged.kz[i] = reinterpret_cast<const uint32_t*>(kp + kTile * kHeadDim * BITS / 8)[from];
-                staged.vz[i] = reinterpret_cast<const uint32_t*>(vp + kTile * kHeadDim * BITS / 8)[from];
+            } else {  // rows past the last one repeat it
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int r = my_row + 4 * i;
+                    const unsigned from = (unsigned)min(r, live - 1);
+                    staged.k[i] = *reinterpret_cast<const Codes*>(kp + (from * kCodeBytes + k_chunk_pos(r, lane % 16) * BITS));
+                    staged.v[i] = *reinterpret_cast<const Codes*>(vp + (from * kCodeBytes + v_chunk_pos(r, lane % 16) * BITS));
+                    staged.vz[i] = *reinterpret_cast<const uint32_t*>(vp + (kTile * kCodeBytes + from * 4));
+                }
             }
+            if (wave == 0) staged.kz = *reinterpret_cast<const uint32_t*>(kp + (kTile * kCodeBytes + (unsigned)min(lane, live - 1) * 4));
         }
     };
     // Keys go into LDS as their codes, exactly, and meet scale and zero as scores in fp32 (rounded keys would cost the log-sum-exp three
-    // digits); values as numbers of the layer's type, rounded once.
-    auto store_staged = [&](int stage) {
+    // digits).  Values go there as fp16 numbers, under bf16 layers too: they come from fp16 scales and zeros, and 11 bits at three instructions for
+    // two of them are better than 8 at six.  Half of each, so that none passes 65504; the weights they meet are doubled.
+    auto store_staged = [&](int stage) __attribute__((always_inline)) {
         if constexpr (QUANT) {
             if (!staged.on) return;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const unsigned to = (wave * kLoads + i) * 1024 + lane * 16;
-                *reinterpret_cast<uint4*>(k_lds[stage] + to) = codes8<T, BITS>(staged.k[i]);
-                *reinterpret_cast<uint4*>(v_lds[stage] + to) = dequantise8<T, BITS>(staged.v[i], staged.vz[i]);
-                if (lane % 16 == 0) {
-                    k_scale[stage][0][my_row + 4 * i] = Elem<F16>::lo(staged.kz[i]) * a.lp.sm_scale_log2;
-                    k_scale[stage][1][my_row + 4 * i] = Elem<F16>::hi(staged.kz[i]) * a.lp.sm_scale_log2;
-                }
+                *reinterpret_cast<uint4*>(k_lds[stage] + to) = codes8<T, BITS>(two_words(staged.k[i]));
+                *reinterpret_cast<uint4*>(v_lds[stage] + to) = dequantise8<F16, BITS>(two_words(staged.v[i]), halved(staged.vz[i]));
+            }
+            if (wave == 0) {
+                const float scale = Elem<F16>::lo(staged.kz), zero = Elem<F16>::hi(staged.kz);
+                k_scale[stage][0][lane] = scale / KeyCodes<T, BITS>::unit * a.lp.sm_scale_log2;
+                k_scale[stage][1][lane] = (zero - KeyCodes<T, BITS>::offset * scale) * a.lp.sm_scale_log2;
             }
         }
     };
+
+    int deepest_tile = 0;  // of the workgroup's rows
 
     // ---- softmax state and outputs of the lane's row (its keys: those of its half)
     float16_t acc[4] = {};
     float m_run = -INFINITY, l_run = 0.f;
     int koff[8], voff[4];
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) koff[kk] = n * kRowBytes + k_chunk_pos(n, kk * 2 + half) * 16;
+    for (int kk = 0; kk < 8; ++kk) koff[kk] = (kg * NB * 32 + n) * kRowBytes + k_chunk_pos(n, kk * 2 + half) * 16;
 #pragma unroll
     for (int db = 0; db < 4; ++db) {
         const int s16 = lane % 16, rr = s16 / 4, chunk = 4 * db + 2 * (n / 16) + (s16 % 4) / 2;
-        voff[db] = half * 1024 + rr * kRowBytes + v_chunk_pos(rr, chunk) * 16 + 8 * (s16 % 2);
+        voff[db] = kg * NB * 32 * kRowBytes + half * 1024 + rr * kRowBytes + v_chunk_pos(rr, chunk) * 16 + 8 * (s16 % 2);
     }
 
-    int deepest_tile = 0;  // of the workgroup's rows
     // keys of the entry that the lane's row sees, one bit each
-    auto seen = [&](int2 w, int live) {
+    auto seen = [&](int2 w, int live) __attribute__((always_inline)) {
         unsigned long long bits = live >= kTile ? ~0ull : (1ull << live) - 1ull;
         if (w.y >= 0) {
             if (streaming && !(w.x < a.lp.sink_pages || w.x > own_tile - a.lp.local_pages)) bits = 0;
@@ -447,21 +488,35 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
     };
 
     // A value that is infinite or not a number must not reach the rows that do not see its key, and zero times it would.  Tiles that some row
-    // does not see whole (drafted tokens, the last page, pages at the far end of a streaming head's window) are looked through
-    // together: such values become zeros, and their keys' bits are returned.  Nearly always there are none.
-    auto clear_spoiled = [&](int2 w, int stage) __attribute__((always_inline)) -> unsigned long long {
-        constexpr uint32_t kLow = BitsOf<T>::exponent, kHigh = kLow << 16;
-        constexpr int kPieces = kTileBytes / 16 / (kWaves * kWave);
-        uint4* const mine = reinterpret_cast<uint4*>(v_lds[stage]) + tid;
+    // does not see whole (drafted tokens, the last page, pages at the far end of a streaming head's window) are looked through, by each wave
+    // what it has brought in itself, ahead of the barrier in front of their step.  Nearly always there is nothing; otherwise such values become
+    // zeros, and are added to the rows that do see their keys one by one.
+    auto ragged = [&](int2 w) __attribute__((always_inline)) {
+        const int live = live_rows(w);
+        return live > 0 && (live < kTile || w.y < 0 || (streaming && w.x >= a.lp.sink_pages && w.x <= deepest_tile - a.lp.local_pages));
+    };
+    auto exponent = [&](int2 w) __attribute__((always_inline)) { return QUANT && w.y >= 0 ? BitsOf<F16>::exponent : BitsOf<T>::exponent; };
+    auto look_for_spoiled = [&](int2 w, int stage) __attribute__((always_inline)) {
+        if (!ragged(w)) return;
+        const uint32_t low = exponent(w), high = low << 16;
+        const uint4* const brought = reinterpret_cast<const uint4*>(v_lds[stage] + wave * kLoads * 1024) + lane;
         bool found = false;
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const uint4 x = mine[i * kWaves * kWave];
+        for (int i = 0; i < kLoads; ++i) {
+            const uint4 x = brought[i * kWave];
             const uint32_t x4[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) found = found || (x4[c] & kLow) == kLow || (x4[c] & kHigh) == kHigh;
+            for (int c = 0; c < 4; ++c) found = found || (x4[c] & low) == low || (x4[c] & high) == high;
         }
-        if (!__syncthreads_or(found)) return 0;
+        if (__any(found)) spoiled[stage] = 1;
+    };
+    // (together; the bits of the keys that have such values)
+    auto clear_spoiled = [&](int2 w, int stage) __attribute__((always_inline)) -> unsigned long long {
+        const uint32_t low = exponent(w), high = low << 16;
+        constexpr int kPieces = kTileBytes / 16 / (kWaves * kWave);
+        uint4* const mine = reinterpret_cast<uint4*>(v_lds[stage]) + tid;
+        __syncthreads();
+        if (tid == 0) spoiled[stage] = 0;
         if (tid < 2) spoiled_keys[tid] = 0;
         __syncthreads();
 #pragma clang loop unroll(disable)
@@ -472,8 +527,8 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
             bool here = false;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                if ((x4[c] & kLow) == kLow) x4[c] &= 0xffff0000u, here = true;
-                if ((x4[c] & kHigh) == kHigh) x4[c] &= 0x0000ffffu, here = true;
+                if ((x4[c] & low) == low) x4[c] &= 0xffff0000u, here = true;
+                if ((x4[c] & high) == high) x4[c] &= 0x0000ffffu, here = true;
             }
             if (here) {
                 const int key = (tid + at) / 16;
@@ -486,8 +541,9 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
                (unsigned)__builtin_amdgcn_readfirstlane(spoiled_keys[0]);
     };
     // Those values, from where they came from, to the rows that do see their keys: weight times value in fp32.
-    auto add_spoiled = [&](int2 w, int stage, unsigned long long bits, float off, unsigned long long keys) __attribute__((always_inline)) {
-        const bool drafted = w.y < 0, codes = QUANT && !drafted;
+    auto add_spoiled = [&](auto kind, int2 w, int stage, unsigned long long bits, float off, unsigned long long keys) __attribute__((always_inline)) {
+        constexpr bool codes = decltype(kind)::value;
+        const bool drafted = w.y < 0;
         for (keys &= (NB == 2 ? ~0ull : 0xffffffffull << (32 * kg)); keys; keys &= keys - 1) {
             const int key = __builtin_ctzll(keys), from = min(key, live_rows(w) - 1);
             float score = 0.f;
@@ -500,9 +556,11 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
             }
             score = halves_sum(score);
             const bool on = bits >> key & 1ull;
-            const float p = __builtin_amdgcn_exp2f(codes ? __builtin_fmaf(score, k_scale[QUANT ? stage : 0][0][QUANT ? key : 0],
-                                                                          __builtin_fmaf(k_scale[QUANT ? stage : 0][1][QUANT ? key : 0], q_sum, off))
-                                                         : __builtin_fmaf(score, a.lp.sm_scale_log2, off));
+            if constexpr (codes)
+                score = __builtin_fmaf(score, k_scale[stage][0][key], __builtin_fmaf(k_scale[stage][1][key], q_sum, off));
+            else
+                score = __builtin_fmaf(score, a.lp.sm_scale_log2, off);
+            const float p = __builtin_amdgcn_exp2f(score);
             const unsigned char* const page = v_base + (size_t)w.y * page_bytes;
             const unsigned char* const src =
                 drafted ? (const unsigned char*)a.v_new + new_offset + ((size_t)w.x * kTile + from) * new_row_bytes
@@ -512,17 +570,16 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
 #pragma unroll
                 for (int g4 = 0; g4 < 4; ++g4) {
                     const int c = 4 * db + g4;  // eight channels, of which the lane has four
-                    uint2 x;
-                    if (codes) {
-                        uint2 raw = make_uint2(0u, 0u);
-                        if constexpr (BITS == 8) raw = *reinterpret_cast<const uint2*>(src + c * 8);
-                        if constexpr (BITS == 4) raw.x = *reinterpret_cast<const uint32_t*>(src + c * 4);
-                        const uint4 eight = dequantise8<T, QUANT ? BITS : 8>(raw, reinterpret_cast<const uint32_t*>(page + kTile * kHeadDim * BITS / 8)[from]);
-                        x = half ? make_uint2(eight.z, eight.w) : make_uint2(eight.x, eight.y);
+                    float v4[4];
+                    if constexpr (codes) {
+                        const uint32_t scale_zero = reinterpret_cast<const uint32_t*>(page + kTile * kCodeBytes)[from];
+                        const uint4 eight = dequantise8<F16, BITS>(two_words(*reinterpret_cast<const Codes*>(src + c * BITS)), halved(scale_zero));
+                        const uint2 x = half ? make_uint2(eight.z, eight.w) : make_uint2(eight.x, eight.y);
+                        v4[0] = Elem<F16>::lo(x.x), v4[1] = Elem<F16>::hi(x.x), v4[2] = Elem<F16>::lo(x.y), v4[3] = Elem<F16>::hi(x.y);
                     } else {
-                        x = *reinterpret_cast<const uint2*>(src + c * 16 + 8 * half);
+                        const uint2 x = *reinterpret_cast<const uint2*>(src + c * 16 + 8 * half);
+                        v4[0] = Elem<T>::lo(x.x), v4[1] = Elem<T>::hi(x.x), v4[2] = Elem<T>::lo(x.y), v4[3] = Elem<T>::hi(x.y);
                     }
-                    const float v4[4] = {Elem<T>::lo(x.x), Elem<T>::hi(x.x), Elem<T>::lo(x.y), Elem<T>::hi(x.y)};
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (on && !(fabsf(v4[i]) < INFINITY)) acc[db][4 * g4 + i] += p * v4[i];
@@ -531,22 +588,27 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
         }
     };
 
-    auto work_on = [&](int2 w, int stage, bool ragged, unsigned long long spoiled) __attribute__((always_inline)) {
+    // (kind: std::true_type for a quantised page)
+    auto work_on = [&](auto kind, int2 w, int stage, bool part, unsigned long long keys) __attribute__((always_inline)) {
+        constexpr bool codes = decltype(kind)::value;
         const int live = live_rows(w);
         if (live <= 0 || !wave_has_rows) return;
-        const bool codes = QUANT && w.y >= 0;
         unsigned long long bits = ~0ull;
-        if (ragged) {
+        if (part) {
             bits = seen(w, live);
             if (!__any(bits != 0)) return;
         }
-        const unsigned char *ks = k_lds[stage] + kg * NB * 32 * kRowBytes, *vs = v_lds[stage] + kg * NB * 32 * kRowBytes;
-        float16_t sc[NB] = {};
+        const unsigned char *ks = k_lds[stage], *vs = v_lds[stage];
+        // (one block of keys: two chains of products, which do not wait for each other, instead of one)
+        constexpr int kChains = 2 / NB;
+        float16_t sc[NB], chain[NB * kChains] = {};
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
-            for (int kb = 0; kb < NB; ++kb)
-                sc[kb] = Mfma<T>::run(*reinterpret_cast<const uint4*>(ks + kb * 32 * kRowBytes + koff[kk]), qreg[kk], sc[kb]);
+            for (int kb = 0; kb < NB; ++kb) {
+                float16_t& sum = chain[kb * kChains + kk % kChains];
+                sum = Mfma<T>::run(*reinterpret_cast<const uint4*>(ks + kb * 32 * kRowBytes + koff[kk]), qreg[kk], sum);
+            }
         // schedule: operand reads run four ahead of the products that consume them, and no further (registers)
         __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
@@ -555,18 +617,27 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            sc[kb] = chain[kb * kChains];
+            if constexpr (kChains == 2) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[kb][i] += chain[kb * kChains + 1][i];
+            }
+        }
         // Exponents, relative to the row's reference (0 before it has one).  The reference is not the maximum so far but one that follows it at
         // a distance of up to kSlack: weights up to 2^kSlack do no harm in any of the types, and outputs are rescaled a few times a list
         // instead of in most steps.
         const bool unset = m_run == -INFINITY;
-        float off = unset ? 0.f : -m_run;
-        if (codes) {
+        const float doubled = codes ? 1.f : 0.f;  // weights of quantised values (see store_staged)
+        float off = (unset ? 0.f : -m_run) + doubled;
+        if constexpr (codes) {
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
                 for (int g4 = 0; g4 < 4; ++g4) {
-                    const int key = QUANT ? (kg * NB + kb) * 32 + 8 * g4 + 4 * half : 0;
-                    const float4 z = *reinterpret_cast<const float4*>(&k_scale[QUANT ? stage : 0][0][key]), o = *reinterpret_cast<const float4*>(&k_scale[QUANT ? stage : 0][1][key]);
+                    const int key = (kg * NB + kb) * 32 + 8 * g4 + 4 * half;
+                    const float4 z = *reinterpret_cast<const float4*>(&k_scale[stage][0][key]), o = *reinterpret_cast<const float4*>(&k_scale[stage][1][key]);
                     const float z4[4] = {z.x, z.y, z.z, z.w}, o4[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sc[kb][4 * g4 + i] = __builtin_fmaf(sc[kb][4 * g4 + i], z4[i], __builtin_fmaf(o4[i], q_sum, off));
@@ -577,7 +648,7 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[kb][i] = __builtin_fmaf(sc[kb][i], a.lp.sm_scale_log2, off);
         }
-        if (ragged) {
+        if (part) {
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb) {
                 const unsigned mine = (unsigned)(bits >> (32 * (kg * NB + kb))) >> (4 * half);
@@ -591,7 +662,7 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
-        top = halves_max(top);
+        top = halves_max(top) - doubled;
         const bool moves = unset ? top > -INFINITY : top > kSlack;
         if (__builtin_expect(__any(moves), 0)) {
             const float delta = moves ? top : 0.f, alpha = unset ? 0.f : __builtin_amdgcn_exp2f(-delta);
@@ -605,8 +676,9 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[kb][i] -= delta;
             if (moves) m_run = unset ? delta : m_run + delta;
-            off = m_run == -INFINITY ? 0.f : -m_run;
+            off = (m_run == -INFINITY ? 0.f : -m_run) + doubled;
         }
+        using V = typename std::conditional<codes, F16, T>::type;  // of the values in LDS
         uint4 pb[NB][2];
         float sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -617,11 +689,11 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
                 p[i] = __builtin_amdgcn_exp2f(sc[kb][i]);
                 sum[i % 2] += p[i];  // unrounded; the second product takes them in the layer's type, which is what its operands are
             }
-            pb[kb][0] = pack8<T>(p);
-            pb[kb][1] = pack8<T>(p + 8);
+            pb[kb][0] = pack8<V>(p);
+            pb[kb][1] = pack8<V>(p + 8);
         }
-        l_run += sum[0] + sum[1];
-        auto values = [&](int step, int db) {  // V^T operand: channel 32 db + n of the lane's eight keys of the step's sixteen
+        l_run += (sum[0] + sum[1]) * (codes ? 0.5f : 1.f);
+        auto values = [&](int step, int db) __attribute__((always_inline)) {  // V^T operand: channel 32 db + n of the lane's eight keys of the step's sixteen
             const uint2 lo = lds_read_transposed(vs + (4 * step) * 1024 + voff[db]);
             const uint2 hi = lds_read_transposed(vs + (4 * step + 2) * 1024 + voff[db]);
             return make_uint4(lo.x, lo.y, hi.x, hi.y);
@@ -629,7 +701,7 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
 #pragma unroll
         for (int step = 0; step < 2 * NB; ++step)
 #pragma unroll
-            for (int db = 0; db < 4; ++db) acc[db] = Mfma<T>::run(values(step, db), pb[step / 2][step % 2], acc[db]);
+            for (int db = 0; db < 4; ++db) acc[db] = Mfma<V>::run(values(step, db), pb[step / 2][step % 2], acc[db]);
         __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAhead, 0);
 #pragma unroll
         for (int i = 0; i < 8 * NB - kAhead; ++i) {
@@ -637,10 +709,11 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
-        if (__builtin_expect(spoiled != 0, 0)) add_spoiled(w, stage, bits, off, spoiled);
+        if (__builtin_expect(keys != 0, 0)) add_spoiled(kind, w, stage, bits, off, keys);
     };
 
     // ---- walk
+    if (tid < 2) spoiled[tid] = 0;
     {
         const int tile = (int)wave_max((float)own_tile);
         if (lane == 0) deepest[wave] = tile;
@@ -655,86 +728,82 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
         q_sum = halves_sum(q_sum);
     }
 
-    auto step = [&](int2 w, int stage) __attribute__((always_inline)) {
-        const int live = live_rows(w);
-        const bool ragged = live > 0 && (live < kTile || w.y < 0 || (streaming && w.x >= a.lp.sink_pages && w.x <= deepest_tile - a.lp.local_pages));
-        work_on(w, stage, ragged, ragged ? clear_spoiled(w, stage) : 0ull);
+    auto step = [&](auto kind, int2 w, int stage) __attribute__((always_inline)) {
+        const bool part = ragged(w);
+        unsigned long long keys = 0;
+        if (part && __builtin_expect(uniform(spoiled[stage]) != 0, 0)) keys = clear_spoiled(w, stage);
+        work_on(kind, w, stage, part, keys);
     };
-    auto find_deepest = [&] {  // past a barrier
+    auto find_deepest = [&]() __attribute__((always_inline)) {  // past a barrier
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) deepest_tile = max(deepest_tile, deepest[i]);
         deepest_tile = uniform(deepest_tile);
     };
     const int2 nothing = make_int2(s.pages, 0);
     // entry e of the list; asked for in order
-    auto next_entry = [&](int e) {
+    auto next_entry = [&](int e) __attribute__((always_inline)) {
         if (e >= e1) return nothing;
         const int i = (e - e0) % kWave;
         if (i == 0 && e > e0) stretch = look_up(e);
         return make_int2(__builtin_amdgcn_readlane(stretch.x, i), __builtin_amdgcn_readlane(stretch.y, i));
     };
-    if constexpr (!QUANT) {
-        // Tiles of up to kStages - 1 steps are on their way.  Loads arrive in order, kPerStep a step and wave: those of step e are there once no
-        // more than those of the steps behind it are missing.
-        constexpr int kPerStep = 2 * kLoads;
-        int2 w[kStages];
-#pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) {
-            w[i] = next_entry(e0 + i);
-            if (e0 + i < e1) fetch(w[i], k_lds[i], v_lds[i]);
-        }
+    // Entry e is worked on, e + 1 on its way into LDS and, of quantised pages, e + 2 on its way into registers.  The entries of quantised pages come
+    // first, and then, as all entries of 16-bit caches do, drafted tokens.
+    const int coded = QUANT ? max(e0, min(history, e1)) : e0;  // the first entry of 16-bit rows
+    int2 w0 = next_entry(e0), w1 = nothing, w2 = nothing;
+    if constexpr (QUANT) w1 = next_entry(e0 + 1);
+    if (e0 < coded) {
+        fetch_codes(w0);
+        store_staged(0);
+        if (e0 + 1 < coded) fetch_codes(w1);
+    } else if (e0 < e1) {
+        fetch(w0, k_lds[0], v_lds[0]);
+    }
+    __syncthreads();
+    find_deepest();
+    pin_queries();
+    if constexpr (QUANT) {
+        if (e0 < coded) look_for_spoiled(w0, 0);
         __syncthreads();
-        find_deepest();
-        pin_queries();
-        for (int e = e0; e < e1; e += kStages) {
-#pragma unroll
-            for (int i = 0; i < kStages; ++i) {
-                const int now = e + i;
-                if (now >= e1) break;
-                if (kStages == 4 && now + 2 < e1)
-                    wait_loads<2 * kPerStep>();
-                else if (kStages == 4 && now + 1 < e1)
-                    wait_loads<kPerStep>();
-                else
-                    wait_loads<0>();
-                __syncthreads();  // the tiles of this step are there, and those of the step before are done with
-                constexpr int kBehind = kStages - 1;
-                w[(i + kBehind) % kStages] = next_entry(now + kBehind);
-                if (now + kBehind < e1) fetch(w[(i + kBehind) % kStages], k_lds[(i + kBehind) % kStages], v_lds[(i + kBehind) % kStages]);
-                step(w[i], i);
-            }
-        }
-        __syncthreads();
-    } else {
-        // entry e is worked on, e + 1 on its way into LDS, e + 2 on its way into registers
-        auto fetch_drafted = [&](int2 w, int stage) {
-            if (w.y < 0) fetch(w, k_lds[stage], v_lds[stage]);
-        };
-        int2 w0 = next_entry(e0), w1 = next_entry(e0 + 1);
-        if (e0 < e1) {
-            fetch_drafted(w0, 0);
-            fetch_codes(w0);
-            store_staged(0);
-        }
-        pin_queries();
-        wait_loads<0>();
-        if (e0 + 1 < e1) fetch_codes(w1);
-        __syncthreads();
-        find_deepest();
-        for (int e = e0; e < e1; ++e) {
-            const int stage = (e - e0) & 1;
-            const int2 w2 = next_entry(e + 2);
-            if (e + 1 < e1) {
-                fetch_drafted(w1, stage ^ 1);
+        auto turn = [&](int e, int stage) __attribute__((always_inline)) {
+            w2 = next_entry(e + 2);
+            if (e + 1 < coded)
                 store_staged(stage ^ 1);
-            }
-            if (e + 2 < e1) fetch_codes(w2);
-            step(w0, stage);
-            if (w1.y < 0) wait_loads<0>();
+            else if (e + 1 < e1)
+                fetch(w1, k_lds[stage ^ 1], v_lds[stage ^ 1]);
+            if (e + 2 < coded) fetch_codes(w2);
+            step(std::true_type{}, w0, stage);
+            if (e + 1 < coded) look_for_spoiled(w1, stage ^ 1);
             w0 = w1;
             w1 = w2;
             __syncthreads();
+        };
+        for (int e = e0; e < coded; e += 2) {
+            turn(e, 0);
+            if (e + 1 < coded) turn(e + 1, 1);
         }
+    }
+    {
+        auto turn = [&](int e, int stage) __attribute__((always_inline)) {
+            dma_wait();
+            look_for_spoiled(w0, stage);
+            __syncthreads();  // the tiles of this step are there, and those of the step before are done with
+            if constexpr (!QUANT) w1 = next_entry(e + 1);
+            if (e + 1 < e1) fetch(w1, k_lds[stage ^ 1], v_lds[stage ^ 1]);
+            step(std::false_type{}, w0, stage);
+            w0 = w1;
+            if constexpr (QUANT) w1 = next_entry(e + 2);
+        };
+        if constexpr (QUANT) {  // one or two steps
+#pragma clang loop unroll(disable)
+            for (int e = coded; e < e1; ++e) turn(e, (e - e0) & 1);
+        } else {
+            for (int e = coded; e < e1; e += 2) {
+                turn(e, 0);
+                if (e + 1 < e1) turn(e + 1, 1);
+            }
+        }
+        __syncthreads();
     }
 
     // ---- the two halves of the keys meet in LDS (the tiles are done with: the loop ended on a barrier)
@@ -779,8 +848,7 @@ __global__ __launch_bounds__((TreeShape<BITS, RG>::kWaves * kWave), 2) void draf
         if (half == 0) t.partial_ml[block * 32 + n] = make_float2(m, l);
         return;
     }
-    // 8 KiB for the wave's rows: two waves to a tile of V, four tiles where there are eight waves
-    unsigned char* const room = (rg < 4 ? v_lds[rg / 2] : k_lds[rg / 2 - 2]) + rg % 2 * (kTileBytes / 2);
+    unsigned char* const room = v_lds[rg / 2] + rg % 2 * (kTileBytes / 2);  // 8 KiB for the wave's rows
     store_rows<T>(a, acc, l == 0.f ? 0.f : 1.f / l, room, s, hk, row0);
     store_lse(a, m, l, s, hk, row0);
 }
@@ -873,35 +941,28 @@ __global__ __launch_bounds__(kFoldThreads) void fold_trees_kernel(TreeArgs a, Tr
 namespace {
 
 struct TreeSizes {
-    int RG, row_tiles, target, exact, fine, streams;
+    int RG, row_tiles, target, exact, streams;
     long long grid, folds;  // workgroups of the two kernels
     size_t pieces_bytes, ml_bytes, partial_bytes;
 };
 
-template <int BITS> int resident_workgroups(int RG) {
-    return RG == 1 ? TreeShape<BITS, 1>::kResident : RG == 2 ? TreeShape<BITS, 2>::kResident
-           : RG == 4 ? TreeShape<BITS, 4>::kResident : TreeShape<BITS, 8>::kResident;
-}
-
-TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride, bool quantised) {
+TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride) {
     TreeSizes z = {};
     const long long rows = (long long)max_new * lp.group;
-    z.RG = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+    z.RG = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     const int R = 32 * z.RG;
     z.row_tiles = (int)((rows + R - 1) / R);
     z.streams = __builtin_popcountll(lp.streaming_mask);
     // row tiles of all sequences: a part of one each, and no more than the tokens there are
     const long long tiles = std::min((long long)batch * z.row_tiles, (long long)total_new * lp.group / R + batch), lists = tiles * lp.Hkv;
-    const int resident = num_compute_units() * (quantised ? resident_workgroups<8>(z.RG) : resident_workgroups<16>(z.RG));
+    const int resident = 2 * num_compute_units();  // workgroups that run at once: 64 KiB of LDS each
     // list entries as far as the host knows: pages of the table, or of a selection (and those since, which are few)
     const int drafts = ceil_div(max_new, kTile), dense = sel_stride > 0 ? std::min(max_pages, sel_stride + 1) : max_pages;
     const int stream = std::min(max_pages, lp.sink_pages + lp.local_pages);
     const long long shortest = tiles * ((lp.Hkv - z.streams) * (long long)(dense + drafts) + z.streams * (long long)(stream + drafts)) / kLeastPiece;
     z.target = lists >= 8LL * resident || std::max(dense, stream) + drafts <= kLeastPiece ? 0 : (int)std::min<long long>(shortest, resident);
     z.exact = z.target > 0 && 2 * lists <= z.target;
-    // pieces: one for every list, and of `target` times what make_plan makes of a workgroup's share
-    z.fine = z.target > 0 && shortest * kLeastPiece / z.target >= kWholeSpan;
-    z.grid = z.target == 0 ? (long long)batch * lp.Hkv * z.row_tiles : (z.fine ? 5LL : 1LL) * z.target + lists;
+    z.grid = z.target == 0 ? (long long)batch * lp.Hkv * z.row_tiles : z.target + lists;
     const long long cycle = 8LL * z.row_tiles;  // see the kernel
     z.grid = (z.grid + cycle - 1) / cycle * cycle;
     z.folds = z.target == 0 ? 0 : (long long)batch * lp.Hkv * z.row_tiles * z.RG * 4;
@@ -914,12 +975,11 @@ TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_ne
 }
 
 template <class T, int BITS> hipError_t launch_tree(const TreeArgs& a, void* workspace, hipStream_t stream) {
-    const TreeSizes z = tree_sizes(a.lp, a.kv.batch, a.total_new, a.max_new, a.kv.max_pages, a.sel_stride, BITS != 16);
+    const TreeSizes z = tree_sizes(a.lp, a.kv.batch, a.total_new, a.max_new, a.kv.max_pages, a.sel_stride);
     if (z.grid > 0x7fffffffLL || z.folds > 0x7fffffffLL) return hipErrorInvalidValue;
     TreeLaunch t = {};
     t.target = z.target;
     t.exact = z.exact;
-    t.fine = z.fine;
     t.row_tiles = z.row_tiles;
     t.streams = z.streams;
     t.slots = z.target ? (int)z.grid : 0;
@@ -932,14 +992,13 @@ template <class T, int BITS> hipError_t launch_tree(const TreeArgs& a, void* wor
     const dim3 grid((unsigned)z.grid), folds((unsigned)z.folds);
 #define LSERVE_TREE(RG)                                                                                                              \
     case RG:                                                                                                                         \
-        hipLaunchKernelGGL((draft_tree_kernel<T, BITS, RG>), grid, dim3(TreeShape<BITS, RG>::kWaves * kWave), 0, stream, a, t);     \
+        hipLaunchKernelGGL((draft_tree_kernel<T, BITS, RG>), grid, dim3(tree_waves(RG) * kWave), 0, stream, a, t);     \
         if (z.folds) hipLaunchKernelGGL((fold_trees_kernel<T, RG>), folds, dim3(kFoldThreads), 0, stream, a, t);                     \
         break
     switch (z.RG) {
         LSERVE_TREE(1);
         LSERVE_TREE(2);
         LSERVE_TREE(4);
-        LSERVE_TREE(8);
     }
 #undef LSERVE_TREE
     return hipGetLastError();
@@ -959,12 +1018,8 @@ template <class T> hipError_t launch_bits(const TreeArgs& a, void* workspace, hi
 }  // namespace
 
 size_t tree_workspace_bytes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride) {
-    size_t most = 0;  // one size for pages of every kind
-    for (const bool quantised : {false, true}) {
-        const TreeSizes z = tree_sizes(lp, batch, total_new, max_new, max_pages, sel_stride, quantised);
-        most = std::max(most, z.pieces_bytes + z.ml_bytes + z.partial_bytes);
-    }
-    return most;
+    const TreeSizes z = tree_sizes(lp, batch, total_new, max_new, max_pages, sel_stride);
+    return z.pieces_bytes + z.ml_bytes + z.partial_bytes;
 }
 
 hipError_t preload_tree_kernels() {
