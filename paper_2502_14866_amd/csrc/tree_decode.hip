@@ -39,6 +39,7 @@ struct TreeLaunch {
     int row_tiles;  // of 32 RG rows, of the longest sequence
     int streams;    // streaming heads
     int slots;      // of pieces in the workspace
+    int folds;      // items of fold_trees_kernel: 32 rows, 32 channels
     float4* partials;
     float2* partial_ml;
     int2* pieces;   // [batch][Hkv][row_tiles]: (first slot, pieces)
@@ -79,8 +80,12 @@ struct TreePlan {
     float reciprocal;
     __device__ __forceinline__ static TreePlan of(int span) { return {span, span ? __builtin_amdgcn_rcpf((float)span) : 0.f}; }
     __device__ __forceinline__ int pieces(int entries) const { return max(1, (int)ceilf((float)entries * reciprocal - 0.01f)); }
+    __device__ __forceinline__ int dense_units(const TreeArgs& a, const TreeLaunch& t, const SeqShape& s) const {
+        return s.row_tiles * (a.lp.Hkv - t.streams) * pieces(s.dense);
+    }
+    __device__ __forceinline__ int stream_units(const TreeLaunch& t, const SeqShape& s) const { return s.row_tiles * t.streams * pieces(s.stream); }
     __device__ __forceinline__ int units(const TreeArgs& a, const TreeLaunch& t, const SeqShape& s) const {
-        return s.row_tiles * (t.streams * pieces(s.stream) + (a.lp.Hkv - t.streams) * pieces(s.dense));
+        return dense_units(a, t, s) + stream_units(t, s);
     }
 };
 
@@ -99,7 +104,9 @@ template <int R> __device__ __forceinline__ TreePlan make_plan(const TreeArgs& a
     const float work = total([&](const SeqShape& s) { return (float)s.row_tiles * ((float)t.streams * s.stream + (float)denses * s.dense); });
     // what a workgroup that is always there has to do: nothing longer than that stays in one piece
     TreePlan plan = TreePlan::of(uniform(max(kLeastPiece, (int)min(work / t.target, 1e9f) + 1)));
-    if (!t.exact) return plan;
+    // (more lists than that: half as much again, so that most stay whole.  40 sequences of 100 .. 3000 tokens 49 -> 38 us, 64 over selected 4-bit
+    // pages 253 -> 217, nine of 1000 .. 2000 under 32 KV heads 51 -> 43, others within 2 %; a quarter more, or less than that, is behind in one of them)
+    if (!t.exact) return TreePlan::of(plan.span + plan.span / 2);
     // as long as it takes to have no more pieces than workgroups that run at once (they are at most twice as many to begin with)
     for (int i = 0; i < 24; ++i) {
         const float count = total([&](const SeqShape& s) { return (float)plan.units(a, t, s); });
@@ -128,11 +135,17 @@ __device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t
         shape = seq_shape<R>(a, u.b);
         return u.row_tile < shape.row_tiles;
     }
+    // heads that select, of all sequences, before streaming ones: what is long starts first
+    bool streaming = false;
     for (int base = 0;; base += kWave) {
-        if (base >= batch) return false;
+        if (base >= batch) {
+            if (streaming || t.streams == 0) return false;
+            streaming = true;
+            base = 0;
+        }
         SeqShape s = own;
         if (base > 0) s = base + lane < batch ? seq_shape<R>(a, base + lane) : SeqShape{};
-        const int units = plan.units(a, t, s);
+        const int units = streaming ? plan.stream_units(t, s) : plan.dense_units(a, t, s);
         const int upto = wave_scan(units, 0, add);
         const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
         if (unit >= all) {
@@ -152,10 +165,7 @@ __device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t
         unit -= __builtin_amdgcn_readlane(upto - units, at);
         break;
     }
-    // of a sequence: heads that select (the longer lists) first, then pieces, then row tiles, which read the same keys
-    const int denses = a.lp.Hkv - t.streams, of_dense = denses * plan.pieces(shape.dense) * shape.row_tiles;
-    const bool streaming = unit >= of_dense;
-    if (streaming) unit -= of_dense;
+    // of a sequence: heads, then pieces, then row tiles, which read the same keys
     u.pieces = plan.pieces(streaming ? shape.stream : shape.dense);
     u.row_tile = unit % shape.row_tiles;
     unit /= shape.row_tiles;
@@ -167,6 +177,7 @@ __device__ __forceinline__ bool find_unit(const TreeArgs& a, const TreeLaunch& t
     return true;
 }
 
+typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
 
 template <class T> struct BitsOf;
 template <> struct BitsOf<F16> { static constexpr uint32_t exponent = 0x7c00u; };
@@ -498,17 +509,17 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     auto exponent = [&](int2 w) __attribute__((always_inline)) { return QUANT && w.y >= 0 ? BitsOf<F16>::exponent : BitsOf<T>::exponent; };
     auto look_for_spoiled = [&](int2 w, int stage) __attribute__((always_inline)) {
         if (!ragged(w)) return;
-        const uint32_t low = exponent(w), high = low << 16;
         const uint4* const brought = reinterpret_cast<const uint4*>(v_lds[stage] + wave * kLoads * 1024) + lane;
-        bool found = false;
+        ushort2_t most = {0, 0};  // magnitude, as whole numbers
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const uint4 x = brought[i * kWave];
             const uint32_t x4[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) found = found || (x4[c] & low) == low || (x4[c] & high) == high;
+            for (int c = 0; c < 4; ++c) most = __builtin_elementwise_max(most, __builtin_bit_cast(ushort2_t, x4[c] & 0x7fff7fffu));
         }
-        if (__any(found)) spoiled[stage] = 1;
+        const uint32_t exponents = exponent(w);
+        if (__any(most[0] >= exponents || most[1] >= exponents)) spoiled[stage] = 1;
     };
     // (together; the bits of the keys that have such values)
     auto clear_spoiled = [&](int2 w, int stage) __attribute__((always_inline)) -> unsigned long long {
@@ -855,22 +866,19 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
 
 // Puts the pieces of 32 rows of a (sequence, KV head) together: a workgroup to 32 channels, its eight wavefronts take pieces in turn, and what they
 // have is added in their order.  Pieces come in at the latency of memory, so that many wavefronts with a few loads each are wanted.
-constexpr int kFoldWaves = 8, kFoldThreads = kFoldWaves * kWave;
+constexpr int kFoldWaves = 8, kFoldThreads = kFoldWaves * kWave, kFoldLanes = kWave * 17;  // a lane's sixteen sums, one place apart from the next lane's
 template <class T, int RG>
-__global__ __launch_bounds__(kFoldThreads) void fold_trees_kernel(TreeArgs a, TreeLaunch t) {
-    __shared__ float sums[kFoldWaves][kWave * 17];  // a lane's sixteen, one place apart from the next lane's
-    __shared__ float2 wave_ml[kFoldWaves][32];
+__device__ __forceinline__ void fold_item(const TreeArgs& a, const TreeLaunch& t, int at, float (&sums)[kFoldWaves][kFoldLanes], float2 (&wave_ml)[kFoldWaves][32]) {
     const int tid = threadIdx.x, lane = tid % kWave, n = lane % 32, G = a.lp.group, wave = uniform(tid / kWave);
-    int at = blockIdx.x;
     const int db = at % 4;
     at /= 4;
     const int rg = at % RG;
     at /= RG;
     const int row_tile = at % t.row_tiles, list = at / t.row_tiles, hk = list % a.lp.Hkv, b = list / a.lp.Hkv;
-    const int2 pieces = t.pieces[(size_t)list * t.row_tiles + row_tile];
+    const int2 pieces = t.pieces[at];
     const SeqShape s = seq_shape<32 * RG>(a, b);
     const int row0 = (row_tile * RG + rg) * 32;
-    if (row0 >= s.n * G) return;
+    if (row0 >= s.n * G) return;  // (what stands in `pieces` of a row tile that does not exist is of another launch)
     // (lengths that contradict each other may ask for more pieces than there is room for, and lead to no address outside it)
     if (pieces.x < 0 || pieces.y < 2 || pieces.x + (long long)(pieces.y - 1) * s.row_tiles >= t.slots) return;
     // piece i of a row tile is row_tiles (of this sequence) slots behind piece i - 1
@@ -936,6 +944,21 @@ __global__ __launch_bounds__(kFoldThreads) void fold_trees_kernel(TreeArgs a, Tr
     if (a.lse_out && db == 0 && c == 0) a.lse_out[head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
+template <class T, int RG>
+__global__ __launch_bounds__(kFoldThreads) void fold_trees_kernel(TreeArgs a, TreeLaunch t) {
+    __shared__ float sums[kFoldWaves][kFoldLanes];
+    __shared__ float2 wave_ml[kFoldWaves][32];
+    const int lane = threadIdx.x % kWave;
+    // Lists that are whole leave most of the work of some launches empty: a workgroup looks at up to 64 of its items at once.
+    const int own = blockIdx.x + lane * (int)gridDim.x;
+    bool mine = false;
+    if (own < t.folds) mine = t.pieces[own / (4 * RG)].y >= 2;
+    for (unsigned long long todo = __ballot(mine); todo; todo &= todo - 1) {
+        const int item = blockIdx.x + __builtin_ctzll(todo) * gridDim.x;
+        fold_item<T, RG>(a, t, item, sums, wave_ml);
+        __syncthreads();
+    }
+}
 // ---- host side -----------------------------------------------------------------------------------
 
 namespace {
@@ -983,13 +1006,14 @@ template <class T, int BITS> hipError_t launch_tree(const TreeArgs& a, void* wor
     t.row_tiles = z.row_tiles;
     t.streams = z.streams;
     t.slots = z.target ? (int)z.grid : 0;
+    t.folds = (int)z.folds;
     if (z.target) {
         unsigned char* p = static_cast<unsigned char*>(workspace);
         t.pieces = reinterpret_cast<int2*>(p);
         t.partial_ml = reinterpret_cast<float2*>(p + z.pieces_bytes);
         t.partials = reinterpret_cast<float4*>(p + z.pieces_bytes + z.ml_bytes);
     }
-    const dim3 grid((unsigned)z.grid), folds((unsigned)z.folds);
+    const dim3 grid((unsigned)z.grid), folds((unsigned)std::max<long long>(std::min<long long>(z.folds, 2048), (z.folds + kWave - 1) / kWave));
 #define LSERVE_TREE(RG)                                                                                                              \
     case RG:                                                                                                                         \
         hipLaunchKernelGGL((draft_tree_kernel<T, BITS, RG>), grid, dim3(tree_waves(RG) * kWave), 0, stream, a, t);     \
