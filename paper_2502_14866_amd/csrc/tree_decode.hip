@@ -221,6 +221,30 @@ template <class T, int BITS> __device__ __forceinline__ uint4 codes8(uint2 codes
 
 __device__ __forceinline__ uint2 two_words(uint2 x) { return x; }
 __device__ __forceinline__ uint2 two_words(uint32_t x) { return make_uint2(x, 0u); }
+// Values of an fp16 layer's quantised pages.  Rounded to fp16 in LDS, next to weights rounded to fp16, they would make the second error of that size;
+// so LDS has (code - kMiddle) 2^e there, which is exact, with 2^e the power of two in the row's scale (as far as fp16 has it), and what is left of the
+// scale, in [1, 2) as a rule, meets the weight in fp32 before that is rounded.  The middle of the codes and the zero go into a sum of the row's own.
+template <int BITS> struct ValueCodes {
+    static constexpr int kMiddle = 1 << (BITS - 1);
+    static __device__ __forceinline__ uint32_t power(uint32_t scale_zero) {  // 2^e as fp16
+        const uint32_t e = scale_zero & 0x7c00u;
+        return min(max(e, 0x0400u), 0x5c00u);  // 2^-14 .. 2^8: a code times that is a number of fp16
+    }
+    static __device__ __forceinline__ uint4 operands(uint2 codes, uint32_t scale_zero) {
+        const uint32_t e = power(scale_zero);
+        const half2_t factor = __builtin_bit_cast(half2_t, e | e << 16), middle = {(_Float16)(-1024.f - kMiddle), (_Float16)(-1024.f - kMiddle)};
+        uint32_t lo = codes.x, hi = codes.y;  // channels 0..3 and 4..7, one byte each
+        if constexpr (BITS == 4) {
+            hi = (codes.x >> 4) & 0x0f0f0f0fu;
+            lo = codes.x & 0x0f0f0f0fu;
+        }
+        auto pair = [&](uint32_t word, uint32_t select) {  // 0x6400 and a code are 1024 + code
+            const half2_t c = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, word, select)) + middle;
+            return __builtin_bit_cast(uint32_t, c * factor);
+        };
+        return make_uint4(pair(lo, 0x04010400u), pair(lo, 0x04030402u), pair(hi, 0x04010400u), pair(hi, 0x04030402u));
+    }
+};
 __device__ __forceinline__ uint32_t halved(uint32_t two) {  // of fp16
     const half2_t h = {(_Float16)0.5f, (_Float16)0.5f};
     return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, two) * h);
@@ -268,6 +292,8 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     __shared__ __attribute__((aligned(1024))) unsigned char k_lds[2][kTileBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char v_lds[2][kTileBytes];
     __shared__ __attribute__((aligned(16))) float k_scale[QUANT ? 2 : 1][2][QUANT ? kTile : 4];  // of the keys of a stage, times the softmax scale: scale, zero
+    constexpr bool kExact = QUANT && std::is_same<T, F16>::value;  // see ValueCodes
+    __shared__ __attribute__((aligned(16))) float v_scale[kExact ? 2 : 1][2][kExact ? kTile : 4];  // of the values: what is left of the scale, middle and zero
     __shared__ float2 fold_ml[RG][32];
     __shared__ unsigned spoiled_keys[2];
     __shared__ int spoiled[2];  // does a tile that some row does not see whole hold values that are not numbers?
@@ -396,7 +422,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     using Codes = typename std::conditional<BITS == 8, uint2, uint32_t>::type;
     struct Staged {
         Codes k[kLoads], v[kLoads];
-        uint32_t vz[kLoads], kz;
+        uint32_t vz[kLoads], kz, vz_all;
         bool on;
     } staged;
     staged.on = false;
@@ -432,11 +458,12 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
                 }
             }
             if (wave == 0) staged.kz = *reinterpret_cast<const uint32_t*>(kp + (kTile * kCodeBytes + (unsigned)min(lane, live - 1) * 4));
+            if (kExact && wave == 1) staged.vz_all = *reinterpret_cast<const uint32_t*>(vp + (kTile * kCodeBytes + (unsigned)min(lane, live - 1) * 4));
         }
     };
     // Keys go into LDS as their codes, exactly, and meet scale and zero as scores in fp32 (rounded keys would cost the log-sum-exp three
-    // digits).  Values go there as fp16 numbers, under bf16 layers too: they come from fp16 scales and zeros, and 11 bits at three instructions for
-    // two of them are better than 8 at six.  Half of each, so that none passes 65504; the weights they meet are doubled.
+    // digits).  Values of a bf16 layer go there as fp16 numbers: they come from fp16 scales and zeros, and 11 bits at three instructions for two of
+    // them are better than 8 at six.  Half of each, so that none passes 65504; the weights they meet are doubled.  Those of an fp16 layer: see ValueCodes.
     auto store_staged = [&](int stage) __attribute__((always_inline)) {
         if constexpr (QUANT) {
             if (!staged.on) return;
@@ -444,12 +471,20 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
             for (int i = 0; i < kLoads; ++i) {
                 const unsigned to = (wave * kLoads + i) * 1024 + lane * 16;
                 *reinterpret_cast<uint4*>(k_lds[stage] + to) = codes8<T, BITS>(two_words(staged.k[i]));
-                *reinterpret_cast<uint4*>(v_lds[stage] + to) = dequantise8<F16, BITS>(two_words(staged.v[i]), halved(staged.vz[i]));
+                if constexpr (kExact)
+                    *reinterpret_cast<uint4*>(v_lds[stage] + to) = ValueCodes<BITS>::operands(two_words(staged.v[i]), staged.vz[i]);
+                else
+                    *reinterpret_cast<uint4*>(v_lds[stage] + to) = dequantise8<F16, BITS>(two_words(staged.v[i]), halved(staged.vz[i]));
             }
             if (wave == 0) {
                 const float scale = Elem<F16>::lo(staged.kz), zero = Elem<F16>::hi(staged.kz);
                 k_scale[stage][0][lane] = scale / KeyCodes<T, BITS>::unit * a.lp.sm_scale_log2;
                 k_scale[stage][1][lane] = (zero - KeyCodes<T, BITS>::offset * scale) * a.lp.sm_scale_log2;
+            }
+            if (kExact && wave == 1) {
+                const float scale = Elem<F16>::lo(staged.vz_all), zero = Elem<F16>::hi(staged.vz_all);
+                v_scale[kExact ? stage : 0][0][lane] = scale / Elem<F16>::lo(ValueCodes<BITS>::power(staged.vz_all));
+                v_scale[kExact ? stage : 0][1][lane] = zero + scale * ValueCodes<BITS>::kMiddle;
             }
         }
     };
@@ -458,7 +493,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
 
     // ---- softmax state and outputs of the lane's row (its keys: those of its half)
     float16_t acc[4] = {};
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run = -INFINITY, l_run = 0.f, o_run = 0.f;  // (o_run: what all channels get, see ValueCodes)
     int koff[8], voff[4];
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) koff[kk] = (kg * NB * 32 + n) * kRowBytes + k_chunk_pos(n, kk * 2 + half) * 16;
@@ -507,7 +542,8 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
         return live > 0 && (live < kTile || w.y < 0 || (streaming && w.x >= a.lp.sink_pages && w.x <= deepest_tile - a.lp.local_pages));
     };
     auto exponent = [&](int2 w) __attribute__((always_inline)) { return QUANT && w.y >= 0 ? BitsOf<F16>::exponent : BitsOf<T>::exponent; };
-    auto look_for_spoiled = [&](int2 w, int stage) __attribute__((always_inline)) {
+    auto look_for_spoiled = [&](auto kind, int2 w, int stage) __attribute__((always_inline)) {
+        if (kExact && decltype(kind)::value) return;  // codes are numbers
         if (!ragged(w)) return;
         const uint4* const brought = reinterpret_cast<const uint4*>(v_lds[stage] + wave * kLoads * 1024) + lane;
         ushort2_t most = {0, 0};  // magnitude, as whole numbers
@@ -640,7 +676,8 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
         // a distance of up to kSlack: weights up to 2^kSlack do no harm in any of the types, and outputs are rescaled a few times a list
         // instead of in most steps.
         const bool unset = m_run == -INFINITY;
-        const float doubled = codes ? 1.f : 0.f;  // weights of quantised values (see store_staged)
+        constexpr bool exact = codes && kExact;
+        const float doubled = codes && !exact ? 1.f : 0.f;  // weights of quantised values (see store_staged)
         float off = (unset ? 0.f : -m_run) + doubled;
         if constexpr (codes) {
 #pragma unroll
@@ -678,6 +715,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
         if (__builtin_expect(__any(moves), 0)) {
             const float delta = moves ? top : 0.f, alpha = unset ? 0.f : __builtin_amdgcn_exp2f(-delta);
             l_run *= alpha;
+            if constexpr (kExact) o_run *= alpha;
 #pragma unroll
             for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -700,10 +738,31 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
                 p[i] = __builtin_amdgcn_exp2f(sc[kb][i]);
                 sum[i % 2] += p[i];  // unrounded; the second product takes them in the layer's type, which is what its operands are
             }
+            if constexpr (exact) {
+#pragma unroll
+                for (int g4 = 0; g4 < 4; ++g4) {
+                    const int key = (kg * NB + kb) * 32 + 8 * g4 + 4 * half;
+                    const float4 z = *reinterpret_cast<const float4*>(&v_scale[stage][0][key]), o = *reinterpret_cast<const float4*>(&v_scale[stage][1][key]);
+                    float z4[4] = {z.x, z.y, z.z, z.w}, o4[4] = {o.x, o.y, o.z, o.w};
+                    if (__builtin_expect(part, 0)) {  // a key that is not seen may have a scale or zero that is not a number
+                        asm volatile("");
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            z4[i] = p[4 * g4 + i] == 0.f ? 0.f : z4[i];
+                            o4[i] = p[4 * g4 + i] == 0.f ? 0.f : o4[i];
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        o_run = __builtin_fmaf(p[4 * g4 + i], o4[i], o_run);
+                        p[4 * g4 + i] *= z4[i];
+                    }
+                }
+            }
             pb[kb][0] = pack8<V>(p);
             pb[kb][1] = pack8<V>(p + 8);
         }
-        l_run += (sum[0] + sum[1]) * (codes ? 0.5f : 1.f);
+        l_run += (sum[0] + sum[1]) * (codes && !exact ? 0.5f : 1.f);
         auto values = [&](int step, int db) __attribute__((always_inline)) {  // V^T operand: channel 32 db + n of the lane's eight keys of the step's sixteen
             const uint2 lo = lds_read_transposed(vs + (4 * step) * 1024 + voff[db]);
             const uint2 hi = lds_read_transposed(vs + (4 * step + 2) * 1024 + voff[db]);
@@ -720,7 +779,9 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
-        if (__builtin_expect(keys != 0, 0)) add_spoiled(kind, w, stage, bits, off, keys);
+        if constexpr (!exact) {
+            if (__builtin_expect(keys != 0, 0)) add_spoiled(kind, w, stage, bits, off, keys);
+        }
     };
 
     // ---- walk
@@ -742,7 +803,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     auto step = [&](auto kind, int2 w, int stage) __attribute__((always_inline)) {
         const bool part = ragged(w);
         unsigned long long keys = 0;
-        if (part && __builtin_expect(uniform(spoiled[stage]) != 0, 0)) keys = clear_spoiled(w, stage);
+        if (!(kExact && decltype(kind)::value) && part && __builtin_expect(uniform(spoiled[stage]) != 0, 0)) keys = clear_spoiled(w, stage);
         work_on(kind, w, stage, part, keys);
     };
     auto find_deepest = [&]() __attribute__((always_inline)) {  // past a barrier
@@ -774,7 +835,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     find_deepest();
     pin_queries();
     if constexpr (QUANT) {
-        if (e0 < coded) look_for_spoiled(w0, 0);
+        if (e0 < coded) look_for_spoiled(std::true_type{}, w0, 0);
         __syncthreads();
         auto turn = [&](int e, int stage) __attribute__((always_inline)) {
             w2 = next_entry(e + 2);
@@ -784,7 +845,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
                 fetch(w1, k_lds[stage ^ 1], v_lds[stage ^ 1]);
             if (e + 2 < coded) fetch_codes(w2);
             step(std::true_type{}, w0, stage);
-            if (e + 1 < coded) look_for_spoiled(w1, stage ^ 1);
+            if (e + 1 < coded) look_for_spoiled(std::true_type{}, w1, stage ^ 1);
             w0 = w1;
             w1 = w2;
             __syncthreads();
@@ -797,7 +858,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     {
         auto turn = [&](int e, int stage) __attribute__((always_inline)) {
             dma_wait();
-            look_for_spoiled(w0, stage);
+            look_for_spoiled(std::false_type{}, w0, stage);
             __syncthreads();  // the tiles of this step are there, and those of the step before are done with
             if constexpr (!QUANT) w1 = next_entry(e + 1);
             if (e + 1 < e1) fetch(w1, k_lds[stage ^ 1], v_lds[stage ^ 1]);
@@ -819,6 +880,13 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
 
     // ---- the two halves of the keys meet in LDS (the tiles are done with: the loop ended on a barrier)
     float l = halves_sum(l_run), m = m_run;
+    if constexpr (kExact) {
+        const float o = halves_sum(o_run);
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[db][i] += o;
+    }
     if constexpr (KG == 2) {
         float4* const room = reinterpret_cast<float4*>(k_lds[rg]);
         if (kg == 1) {
