@@ -1,5 +1,5 @@
-"""Binding of liblserve.so: argument marshalling only, every step runs in the HIP kernels.  The three calls of a decode step are
-marshalled natively (csrc/py_calls.cpp), the others by ctypes."""
+"""Binding of liblserve.so: argument marshalling only, every step runs in the HIP kernels.  The calls of a decode step and
+those on new tokens are marshalled natively (csrc/py_calls.cpp), the others by ctypes."""
 from __future__ import annotations
 
 import contextlib
@@ -200,6 +200,86 @@ class _CtypesCalls:
                                                    _ptr(workspace), ws_bytes, stream)
 
 
+    @staticmethod
+    def extend(desc, kv, new_lens, free_pages, cu_new, new_seq_lens, pages_taken, positions, slots, ring_slots, total_new, stream):
+        d, batch, i32, i64 = _CAttnDesc.from_address(desc), kv.page_table.shape[0], torch.int32, torch.int64
+        _checked("lserve_extend_tables", (kv.page_table, i32, 0), (kv.seq_lens, i32, batch), (kv.ring_table, i32, 0), (new_lens, i32, batch),
+                 (free_pages, i32, 0), (cu_new, i32, batch + 1), (new_seq_lens, i32, batch), (pages_taken, i32, 1),
+                 (positions, i32, total_new), (slots, i64, total_new), (ring_slots, i64, total_new))
+        if ring_slots is not None and kv.ring_table is not None and d.page_size > 0:
+            ring = -(-d.sink_tokens // d.page_size) - (-d.local_tokens // d.page_size)
+            if kv.ring_table.numel() < batch * ring:
+                raise ValueError(f"lserve_extend_tables: a ring table of {kv.ring_table.numel()} entries for {batch} sequences of {ring}")
+        return load_library().lserve_extend_tables(
+            d, kv.c(), _ptr(new_lens), _ptr(free_pages), 0 if free_pages is None else free_pages.numel(), total_new, _ptr(cu_new),
+            _ptr(new_seq_lens), _ptr(pages_taken), _ptr(positions), _ptr(slots), _ptr(ring_slots), stream)
+
+    @staticmethod
+    def masks(parents, cu_new, seq_lens, max_new_per_seq, tree_mask, positions, stream):
+        total, batch = (0 if parents is None else parents.numel()), (0 if cu_new is None else cu_new.numel() - 1)
+        words = 0 if tree_mask is None else tree_mask.shape[-1]
+        _checked("lserve_tree_masks", (parents, torch.int32, 1), (cu_new, torch.int32, 2), (seq_lens, torch.int32, batch),
+                 (tree_mask, torch.int64, total * words), (positions, torch.int32, total))
+        return load_library().lserve_tree_masks(_ptr(parents), _ptr(cu_new), _ptr(seq_lens), batch, total, max_new_per_seq, words,
+                                                _ptr(tree_mask), _ptr(positions), stream)
+
+    @staticmethod
+    def rotary(desc, rotary, inv_freq, q, k, positions, q_out, k_out, stream):
+        d, r = _CAttnDesc.from_address(desc), _CRotaryDesc.from_address(rotary)
+        total, dim, hq, hkv, dt = (0 if positions is None else positions.numel()), d.head_dim, d.num_q_heads, d.num_kv_heads, _dtype(d)
+        (q_at, q_stride), (k_at, k_stride) = _rows(q, hq, dim, "q"), _rows(k, hkv, dim, "k")
+        _checked("lserve_rotary", (positions, torch.int32, 1), (inv_freq, torch.float64, r.rotary_dim // 2 if r.rotary_dim <= dim else 0), (q, dt, total * hq * dim),
+                 (q_out, dt, total * hq * dim), (k, dt, total * hkv * dim), (k_out, dt, total * hkv * dim))
+        return load_library().lserve_rotary(d, r, q_at, k_at, _ptr(positions), total, q_stride, k_stride, _ptr(q_out), _ptr(k_out), stream)
+
+    @staticmethod
+    def tree(desc, kv, q, k_new, v_new, cu_new, max_new_per_seq, out, lse_out, tree_mask, positions, sel_pages, sel_count, sel_seq_len,
+             workspace, stream):
+        d, batch, i32 = _CAttnDesc.from_address(desc), kv.page_table.shape[0], torch.int32
+        total, dim, hq, hkv, dt = (0 if q is None else q.shape[0]), d.head_dim, d.num_q_heads, d.num_kv_heads, _dtype(d)
+        words = 0 if tree_mask is None else tree_mask.shape[-1]
+        stride = 0 if sel_pages is None else sel_pages.shape[-1]
+        _checked("lserve_sparse_decode_tree", (q, dt, total * hq * dim), (k_new, dt, total * hkv * dim), (v_new, dt, total * hkv * dim),
+                 (out, dt, total * hq * dim), (lse_out, torch.float32, total * hq), (cu_new, i32, batch + 1), (kv.seq_lens, i32, batch),
+                 (kv.page_table, i32, 0), (kv.k_pool, (dt, torch.uint8), 0), (tree_mask, torch.int64, total * words), (positions, i32, total),
+                 (sel_pages, i32, batch * hkv * stride), (sel_count, i32, batch * hkv), (sel_seq_len, i32, batch))
+        return load_library().lserve_sparse_decode_tree(
+            d, kv.c(), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(cu_new), _ptr(tree_mask), words, _ptr(positions), _ptr(sel_pages),
+            _ptr(sel_count), _ptr(sel_seq_len), stride, total, max_new_per_seq, _ptr(out), _ptr(lse_out), _ptr(workspace),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), stream)
+
+
+def _dtype(desc: "_CAttnDesc") -> torch.dtype:
+    return torch.bfloat16 if desc.dtype == 1 else torch.float16
+
+
+def _checked(where: str, *args) -> None:
+    """(tensor or None, type or types, least number of elements) each: what the library cannot see from an address."""
+    device = None
+    for t, kinds, least in args:
+        if t is None:
+            continue
+        if t.dtype not in (kinds if isinstance(kinds, tuple) else (kinds,)):
+            raise ValueError(f"{where}: a tensor of {t.dtype} where {kinds} is taken")
+        if t.numel() < least:
+            raise ValueError(f"{where}: a tensor of {t.numel()} elements where {least} are read or written")
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError(f"{where}: tensors on {device} and {t.device}")
+    if device is not None and device.type == "cuda" and device.index != torch.cuda.current_device():
+        raise ValueError(f"{where}: tensors on {device} while device {torch.cuda.current_device()} is current")
+
+
+def _rows(t: Optional[torch.Tensor], heads: int, dim: int, what: str) -> tuple:
+    """(address, elements between two rows) of [total][heads][dim] whose rows may lie apart."""
+    if t is None:
+        return None, 0
+    if t.dim() != 3 or t.shape[1:] != (heads, dim) or t.stride(2) != 1 or t.stride(1) != dim:
+        raise ValueError(f"lserve_rotary: {what} is [total][{heads}][{dim}], heads next to each other")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
 def _native():
     """The native calls, bound to the loaded library; without the extension (only the library was built, or it was built with another
     torch or Python) the same by ctypes, some five microseconds a call slower."""
@@ -213,6 +293,9 @@ def _native():
                 raise ImportError(f"_calls was built with torch {calls.torch_version}, this is {torch.__version__}")
             calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value
                          for f in (lib.lserve_append_kv, lib.lserve_select_pages, lib.lserve_sparse_decode)))
+            if hasattr(lib, "lserve_extend_tables"):  # what stands in for the library may have the decode step's calls alone
+                calls.bind_new(*(ctypes.cast(f, ctypes.c_void_p).value
+                                 for f in (lib.lserve_extend_tables, lib.lserve_tree_masks, lib.lserve_rotary, lib.lserve_sparse_decode_tree)))
         except ImportError as e:
             warnings.warn(f"the binding's native calls are missing ({e}): decode steps are marshalled by ctypes; build them with "
                           "`python -m paper_2502_14866_amd.build` (or __graft_entry__.build())", RuntimeWarning, stacklevel=3)
@@ -534,24 +617,6 @@ def lserve_probe_mask_walk(desc: AttnDesc, batch: int, total_tokens: int, max_se
     return walk.value
 
 
-def _checked(where: str, *args) -> None:
-    """(tensor or None, type or types, least number of elements) each: what the library cannot see from an address."""
-    device = None
-    for t, kinds, least in args:
-        if t is None:
-            continue
-        if t.dtype not in (kinds if isinstance(kinds, tuple) else (kinds,)):
-            raise ValueError(f"{where}: a tensor of {t.dtype} where {kinds} is taken")
-        if t.numel() < least:
-            raise ValueError(f"{where}: a tensor of {t.numel()} elements where {least} are read or written")
-        if device is None:
-            device = t.device
-        elif t.device != device:
-            raise ValueError(f"{where}: tensors on {device} and {t.device}")
-    if device is not None and device.type == "cuda" and device.index != torch.cuda.current_device():
-        raise ValueError(f"{where}: tensors on {device} while device {torch.cuda.current_device()} is current")
-
-
 def lserve_extend_tables(desc: AttnDesc, kv: PagedKV, new_lens: torch.Tensor, free_pages: Optional[torch.Tensor], cu_new: torch.Tensor,
                          new_seq_lens: torch.Tensor, pages_taken: torch.Tensor, positions: Optional[torch.Tensor] = None,
                          slots: Optional[torch.Tensor] = None, ring_slots: Optional[torch.Tensor] = None, stream=None,
@@ -563,17 +628,8 @@ def lserve_extend_tables(desc: AttnDesc, kv: PagedKV, new_lens: torch.Tensor, fr
         if given is None:
             raise ValueError("lserve_extend_tables: total_new, where no positions or slots are asked for")
         total_new = given.numel()
-    batch, i32, i64 = kv.page_table.shape[0], torch.int32, torch.int64
-    _checked("lserve_extend_tables", (kv.page_table, i32, 0), (kv.seq_lens, i32, batch), (kv.ring_table, i32, 0), (new_lens, i32, batch),
-             (free_pages, i32, 0), (cu_new, i32, batch + 1), (new_seq_lens, i32, batch), (pages_taken, i32, 1),
-             (positions, i32, total_new), (slots, i64, total_new), (ring_slots, i64, total_new))
-    if ring_slots is not None and kv.ring_table is not None:
-        ring = -(-desc.sink_tokens // desc.page_size) - (-desc.local_tokens // desc.page_size)
-        if kv.ring_table.numel() < batch * ring:
-            raise ValueError(f"lserve_extend_tables: a ring table of {kv.ring_table.numel()} entries for {batch} sequences of {ring}")
-    _check(load_library().lserve_extend_tables(
-        desc.c(), kv.c(), _ptr(new_lens), _ptr(free_pages), 0 if free_pages is None else free_pages.numel(), total_new, _ptr(cu_new),
-        _ptr(new_seq_lens), _ptr(pages_taken), _ptr(positions), _ptr(slots), _ptr(ring_slots), _stream(stream)), "lserve_extend_tables")
+    _check((_calls or _native()).extend(desc._address, kv, new_lens, free_pages, cu_new, new_seq_lens, pages_taken, positions, slots,
+                                        ring_slots, total_new, _stream(stream)), "lserve_extend_tables")
 
 
 _SCALINGS = ("none", "linear", "wavelength", "ramp")
@@ -621,38 +677,22 @@ class RotaryDesc:
     def c(self):
         return ctypes.byref(self._c)
 
-
-def _rows(t: Optional[torch.Tensor], heads: int, dim: int, what: str) -> tuple:
-    """(address, elements between two rows) of [total][heads][dim] whose rows may lie apart."""
-    if t is None:
-        return None, 0
-    if t.dim() != 3 or t.shape[1:] != (heads, dim) or t.stride(2) != 1 or t.stride(1) != dim:
-        raise ValueError(f"lserve_rotary: {what} is [total][{heads}][{dim}], heads next to each other")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim
+    @property
+    def _address(self):
+        return ctypes.addressof(self._c)
 
 
 def lserve_rotary(desc: AttnDesc, rotary: RotaryDesc, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor,
                   q_out: Optional[torch.Tensor], k_out: Optional[torch.Tensor], stream=None) -> None:
     """q and k may be cut out of the rows of a fused projection (any distance between rows that is a multiple of eight elements)."""
-    total = positions.numel()
-    dim, hq, hkv = desc.head_dim, desc.num_q_heads, desc.num_kv_heads
-    q_at, q_stride = _rows(q, hq, dim, "q")
-    k_at, k_stride = _rows(k, hkv, dim, "k")
-    _checked("lserve_rotary", (positions, torch.int32, 1), (rotary.inv_freq, torch.float64, rotary.rotary_dim // 2),
-             (q, desc.dtype, total * hq * dim), (q_out, desc.dtype, total * hq * dim),
-             (k, desc.dtype, total * hkv * dim), (k_out, desc.dtype, total * hkv * dim))
-    _check(load_library().lserve_rotary(desc.c(), rotary.c(), q_at, k_at, _ptr(positions), total, q_stride, k_stride, _ptr(q_out),
-                                        _ptr(k_out), _stream(stream)), "lserve_rotary")
+    _check((_calls or _native()).rotary(desc._address, rotary._address, rotary.inv_freq, q, k, positions, q_out, k_out, _stream(stream)),
+           "lserve_rotary")
 
 
 def lserve_tree_masks(parents: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor, max_new_per_seq: int,
                       tree_mask: torch.Tensor, positions: torch.Tensor, stream=None) -> None:
     """tree_mask: int64 [total_new][words], 64 drafted tokens to a word."""
-    total, batch, words = parents.numel(), cu_new.numel() - 1, tree_mask.shape[-1]
-    _checked("lserve_tree_masks", (parents, torch.int32, 1), (cu_new, torch.int32, 2), (seq_lens, torch.int32, batch),
-             (tree_mask, torch.int64, total * words), (positions, torch.int32, total))
-    _check(load_library().lserve_tree_masks(_ptr(parents), _ptr(cu_new), _ptr(seq_lens), batch, total, max_new_per_seq, words,
-                                            _ptr(tree_mask), _ptr(positions), _stream(stream)), "lserve_tree_masks")
+    _check((_calls or _native()).masks(parents, cu_new, seq_lens, max_new_per_seq, tree_mask, positions, _stream(stream)), "lserve_tree_masks")
 
 
 def lserve_tree_workspace_bytes(desc: AttnDesc, batch: int, total_new: int, max_new_per_seq: int, max_pages_per_seq: int,
@@ -667,15 +707,5 @@ def lserve_sparse_decode_tree(desc: AttnDesc, kv: PagedKV, q: torch.Tensor, k_ne
                               sel_seq_len: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """tree_mask: int64 [total_new][words], 64 drafted tokens to a word; without it and positions the drafted tokens are a chain.
     Without sel_pages, sel_count and sel_seq_len selecting heads attend the whole history."""
-    total, batch, i32 = q.shape[0], kv.page_table.shape[0], torch.int32
-    dim, hq, hkv, dt = desc.head_dim, desc.num_q_heads, desc.num_kv_heads, desc.dtype
-    words = 0 if tree_mask is None else tree_mask.shape[-1]
-    stride = 0 if sel_pages is None else sel_pages.shape[-1]
-    _checked("lserve_sparse_decode_tree", (q, dt, total * hq * dim), (k_new, dt, total * hkv * dim), (v_new, dt, total * hkv * dim),
-             (out, dt, total * hq * dim), (lse_out, torch.float32, total * hq), (cu_new, i32, batch + 1), (kv.seq_lens, i32, batch),
-             (kv.page_table, i32, 0), (kv.k_pool, (dt, torch.uint8), 0), (tree_mask, torch.int64, total * words), (positions, i32, total),
-             (sel_pages, i32, batch * hkv * stride), (sel_count, i32, batch * hkv), (sel_seq_len, i32, batch))
-    _check(load_library().lserve_sparse_decode_tree(
-        desc.c(), kv.c(), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(cu_new), _ptr(tree_mask), words, _ptr(positions), _ptr(sel_pages),
-        _ptr(sel_count), _ptr(sel_seq_len), stride, total, max_new_per_seq, _ptr(out), _ptr(lse_out), _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "lserve_sparse_decode_tree")
+    _check((_calls or _native()).tree(desc._address, kv, q, k_new, v_new, cu_new, max_new_per_seq, out, lse_out, tree_mask, positions,
+                                      sel_pages, sel_count, sel_seq_len, workspace, _stream(stream)), "lserve_sparse_decode_tree")

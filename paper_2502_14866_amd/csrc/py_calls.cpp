@@ -1,11 +1,14 @@
-// The calls of a decode step, marshalled natively.  A step of a small batch is some ten microseconds of GPU work a call, and
+// The calls of a decode step and those on new tokens, marshalled natively.  A step of a small batch is some ten microseconds of GPU work a call, and
 // through ctypes a call was five microseconds of Python before its launch: the struct of the cache built field by field, an
 // address and a check per tensor, twelve arguments converted.  Arguments are the binding's own objects; what is passed on
 // is what ctypes passed on (see binding.py), and the return value is the library's.  The library is not linked: its entry points are
 // handed over by address (bind), since the binding may load another build of it.
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <c10/core/impl/VirtualGuardImpl.h>
+
 #include <exception>
+#include <initializer_list>
 
 #include "../../include/lserve.h"
 
@@ -14,6 +17,10 @@ namespace {
 decltype(&lserve_append_kv) append_kv;
 decltype(&lserve_select_pages) select_pages;
 decltype(&lserve_sparse_decode) sparse_decode;
+decltype(&lserve_extend_tables) extend_tables;
+decltype(&lserve_tree_masks) tree_masks;
+decltype(&lserve_rotary) rotary;
+decltype(&lserve_sparse_decode_tree) sparse_decode_tree;
 
 struct PythonError {};  // the interpreter's error is set
 
@@ -35,6 +42,34 @@ template <class P = void> P* address(const at::Tensor* t) {
     return static_cast<P*>(t->data_ptr());
 }
 template <class P = void> P* address(PyObject* o) { return address<P>(tensor_or_null(o)); }
+
+// What the library cannot see from an address: a tensor's type, how many elements of it are read or written, its device.
+struct Wanted {
+    const at::Tensor* t;
+    at::ScalarType type;
+    int64_t least;
+};
+[[noreturn]] void refuse(const char* where, const std::string& why) {
+    PyErr_Format(PyExc_ValueError, "%s: %s", where, why.c_str());
+    throw PythonError();
+}
+void check(const char* where, std::initializer_list<Wanted> wanted) {
+    const at::Tensor* first = nullptr;
+    for (const Wanted& w : wanted) {
+        if (!w.t) continue;
+        if (w.t->scalar_type() != w.type) refuse(where, std::string("a tensor of ") + c10::toString(w.t->scalar_type()) + " where " + c10::toString(w.type) + " is taken");
+        if (w.t->numel() < w.least)
+            refuse(where, "a tensor of " + std::to_string(w.t->numel()) + " elements where " + std::to_string(w.least) + " are read or written");
+        if (first && w.t->device() != first->device()) refuse(where, "tensors on " + first->device().str() + " and " + w.t->device().str());
+        if (!first) first = w.t;
+    }
+    if (first && first->device().is_cuda()) {
+        const c10::Device now = c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice();
+        if (first->device() != now) refuse(where, "tensors on " + first->device().str() + " while device " + now.str() + " is current");
+    }
+}
+constexpr at::ScalarType kInt = at::kInt, kLong = at::kLong, kFloat = at::kFloat, kDouble = at::kDouble;
+at::ScalarType type_of(const lserve_attn_desc* d) { return d->dtype == LSERVE_DTYPE_BF16 ? at::kBFloat16 : at::kHalf; }
 
 // (the low bits, as ctypes takes them)
 unsigned long long number(PyObject* o) {
@@ -151,6 +186,125 @@ PyObject* py_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+struct HeldKV {  // the tensors of a PagedKV that are checked
+    Attribute table_o, lens_o, ring_o, pool_o;
+    const at::Tensor *table, *lens, *ring, *pool;
+    explicit HeldKV(PyObject* kv)
+        : table_o(kv, names[kPageTable]), lens_o(kv, names[kSeqLens]), ring_o(kv, names[kRingTable]), pool_o(kv, names[kKPool]),
+          table(tensor_or_null(table_o.o)), lens(tensor_or_null(lens_o.o)), ring(tensor_or_null(ring_o.o)), pool(tensor_or_null(pool_o.o)) {}
+};
+
+PyObject* py_extend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 12, [&] {
+        const char* where = "lserve_extend_tables";
+        const lserve_attn_desc* desc = description(a[0]);
+        const lserve_paged_kv kv = paged(a[1]);
+        const HeldKV held(a[1]);
+        const at::Tensor *fresh = tensor_or_null(a[2]), *pages = tensor_or_null(a[3]), *cu = tensor_or_null(a[4]), *lens = tensor_or_null(a[5]),
+                         *taken = tensor_or_null(a[6]), *pos = tensor_or_null(a[7]), *slots = tensor_or_null(a[8]), *ring = tensor_or_null(a[9]);
+        const int64_t batch = kv.batch, total = PyLong_AsLongLong(a[10]);
+        if (total == -1 && PyErr_Occurred()) throw PythonError();
+        check(where, {{held.table, kInt, 0}, {held.lens, kInt, batch}, {held.ring, kInt, 0}, {fresh, kInt, batch}, {pages, kInt, 0},
+                      {cu, kInt, batch + 1}, {lens, kInt, batch}, {taken, kInt, 1}, {pos, kInt, total}, {slots, kLong, total}, {ring, kLong, total}});
+        if (ring && held.ring && desc->page_size > 0) {
+            const int64_t slots_of_ring = (desc->sink_tokens + desc->page_size - 1) / desc->page_size + (desc->local_tokens + desc->page_size - 1) / desc->page_size;
+            if (held.ring->numel() < batch * slots_of_ring)
+                refuse(where, "a ring table of " + std::to_string(held.ring->numel()) + " entries for " + std::to_string(batch) + " sequences of " +
+                                  std::to_string(slots_of_ring));
+        }
+        const int32_t* p_fresh = address<int32_t>(fresh);
+        const int32_t *p_pages = address<int32_t>(pages), num_free = pages ? (int32_t)pages->numel() : 0;
+        int32_t *p_cu = address<int32_t>(cu), *p_lens = address<int32_t>(lens), *p_taken = address<int32_t>(taken), *p_pos = address<int32_t>(pos);
+        int64_t *p_slots = address<int64_t>(slots), *p_ring = address<int64_t>(ring);
+        void* stream = stream_handle(a[11]);
+        const WithoutLock w;
+        return extend_tables(desc, &kv, p_fresh, p_pages, num_free, (int32_t)total, p_cu, p_lens, p_taken, p_pos, p_slots, p_ring, stream);
+    });
+}
+
+PyObject* py_masks(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 7, [&] {
+        const at::Tensor *parents = tensor_or_null(a[0]), *cu = tensor_or_null(a[1]), *lens = tensor_or_null(a[2]), *mask = tensor_or_null(a[4]),
+                         *pos = tensor_or_null(a[5]);
+        const int64_t total = parents ? parents->numel() : 0, batch = cu ? cu->numel() - 1 : 0, words = mask && mask->dim() ? mask->size(-1) : 0;
+        check("lserve_tree_masks", {{parents, kInt, 1}, {cu, kInt, 2}, {lens, kInt, batch}, {mask, kLong, total * words}, {pos, kInt, total}});
+        const int32_t *p_parents = address<int32_t>(parents), *p_cu = address<int32_t>(cu), *p_lens = address<int32_t>(lens), longest = number32(a[3]);
+        uint64_t* p_mask = address<uint64_t>(mask);
+        int32_t* p_pos = address<int32_t>(pos);
+        void* stream = stream_handle(a[6]);
+        const WithoutLock w;
+        return tree_masks(p_parents, p_cu, p_lens, (int32_t)batch, (int32_t)total, longest, (int32_t)words, p_mask, p_pos, stream);
+    });
+}
+
+// Address of [total][heads][dim] whose rows may lie apart, and how far.
+const void* rows(const at::Tensor* t, int64_t heads, int64_t dim, const char* what, int64_t* stride) {
+    *stride = 0;
+    if (!t) return nullptr;
+    if (t->dim() != 3 || t->size(1) != heads || t->size(2) != dim || t->stride(2) != 1 || t->stride(1) != dim)
+        refuse("lserve_rotary", std::string(what) + " is [total][" + std::to_string(heads) + "][" + std::to_string(dim) + "], heads next to each other");
+    *stride = t->size(0) > 1 ? t->stride(0) : heads * dim;
+    return t->data_ptr();
+}
+
+PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 9, [&] {
+        const lserve_attn_desc* desc = description(a[0]);
+        const lserve_rotary_desc* rot = reinterpret_cast<const lserve_rotary_desc*>((uintptr_t)number(a[1]));
+        const at::Tensor *freq = tensor_or_null(a[2]), *q = tensor_or_null(a[3]), *k = tensor_or_null(a[4]), *pos = tensor_or_null(a[5]),
+                         *qo = tensor_or_null(a[6]), *ko = tensor_or_null(a[7]);
+        const int64_t dim = desc->head_dim, hq = desc->num_q_heads, hkv = desc->num_kv_heads, total = pos ? pos->numel() : 0;
+        int64_t q_stride, k_stride;
+        const void *p_q = rows(q, hq, dim, "q", &q_stride), *p_k = rows(k, hkv, dim, "k", &k_stride);
+        const at::ScalarType t = type_of(desc);
+        check("lserve_rotary", {{pos, kInt, 1}, {freq, kDouble, rot->rotary_dim <= dim ? rot->rotary_dim / 2 : 0}, {q, t, total * hq * dim}, {qo, t, total * hq * dim},
+                                {k, t, total * hkv * dim}, {ko, t, total * hkv * dim}});
+        const int32_t* p_pos = address<int32_t>(pos);
+        void *p_qo = address(qo), *p_ko = address(ko), *stream = stream_handle(a[8]);
+        const WithoutLock w;
+        return rotary(desc, rot, p_q, p_k, p_pos, (int32_t)total, q_stride, k_stride, p_qo, p_ko, stream);
+    });
+}
+
+PyObject* py_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 16, [&] {
+        const char* where = "lserve_sparse_decode_tree";
+        const lserve_attn_desc* desc = description(a[0]);
+        const lserve_paged_kv kv = paged(a[1]);
+        const HeldKV held(a[1]);
+        const at::Tensor *q = tensor_or_null(a[2]), *k = tensor_or_null(a[3]), *v = tensor_or_null(a[4]), *cu = tensor_or_null(a[5]),
+                         *out = tensor_or_null(a[7]), *lse = tensor_or_null(a[8]), *mask = tensor_or_null(a[9]), *pos = tensor_or_null(a[10]),
+                         *sel = tensor_or_null(a[11]), *count = tensor_or_null(a[12]), *len = tensor_or_null(a[13]), *ws = tensor_or_null(a[14]);
+        const int64_t dim = desc->head_dim, hq = desc->num_q_heads, hkv = desc->num_kv_heads, batch = kv.batch, total = q && q->dim() ? q->size(0) : 0;
+        const int64_t words = mask && mask->dim() ? mask->size(-1) : 0, stride = sel && sel->dim() ? sel->size(-1) : 0;
+        const at::ScalarType t = type_of(desc);
+        check(where, {{q, t, total * hq * dim}, {k, t, total * hkv * dim}, {v, t, total * hkv * dim}, {out, t, total * hq * dim}, {lse, kFloat, total * hq},
+                      {cu, kInt, batch + 1}, {held.lens, kInt, batch}, {held.table, kInt, 0},
+                      {held.pool, held.pool && held.pool->scalar_type() == at::kByte ? at::kByte : t, 0}, {mask, kLong, total * words},
+                      {pos, kInt, total}, {sel, kInt, batch * hkv * stride}, {count, kInt, batch * hkv}, {len, kInt, batch}});
+        const void *p_q = address(q), *p_k = address(k), *p_v = address(v);
+        const int32_t *p_cu = address<int32_t>(cu), longest = number32(a[6]), *p_pos = address<int32_t>(pos), *p_sel = address<int32_t>(sel),
+                      *p_count = address<int32_t>(count), *p_len = address<int32_t>(len);
+        const uint64_t* p_mask = address<uint64_t>(mask);
+        void *p_out = address(out), *p_ws = address(ws), *stream = stream_handle(a[15]);
+        float* p_lse = address<float>(lse);
+        const size_t bytes = ws ? ws->nbytes() : 0;
+        const WithoutLock w;
+        return sparse_decode_tree(desc, &kv, p_q, p_k, p_v, p_cu, p_mask, (int32_t)words, p_pos, p_sel, p_count, p_len, (int32_t)stride, (int32_t)total,
+                                  longest, p_out, p_lse, p_ws, bytes, stream);
+    });
+}
+
+PyObject* py_bind_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 4, [&] {
+        extend_tables = reinterpret_cast<decltype(extend_tables)>((uintptr_t)number(a[0]));
+        tree_masks = reinterpret_cast<decltype(tree_masks)>((uintptr_t)number(a[1]));
+        rotary = reinterpret_cast<decltype(rotary)>((uintptr_t)number(a[2]));
+        sparse_decode_tree = reinterpret_cast<decltype(sparse_decode_tree)>((uintptr_t)number(a[3]));
+        return 0;
+    });
+}
+
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 3, [&] {
         append_kv = reinterpret_cast<decltype(append_kv)>((uintptr_t)number(a[0]));
@@ -167,8 +321,15 @@ PyMethodDef methods[] = {
     {"select", LSERVE_FASTCALL(py_select),
      "desc address, kv, q, budget_tokens, stats_valid_len, sel_pages, sel_count, sel_seq_len, scores_out, workspace, stream"},
     {"decode", LSERVE_FASTCALL(py_decode), "desc address, kv, q, sel_pages, sel_count, sel_seq_len, out, lse_out, workspace, stream"},
+    {"bind_new", LSERVE_FASTCALL(py_bind_new), "addresses of lserve_extend_tables, lserve_tree_masks, lserve_rotary, lserve_sparse_decode_tree"},
+    {"extend", LSERVE_FASTCALL(py_extend),
+     "desc address, kv, new_lens, free_pages, cu_new, new_seq_lens, pages_taken, positions, slots, ring_slots, total_new, stream"},
+    {"masks", LSERVE_FASTCALL(py_masks), "parents, cu_new, seq_lens, max_new_per_seq, tree_mask, positions, stream"},
+    {"rotary", LSERVE_FASTCALL(py_rotary), "desc address, rotary address, inv_freq, q, k, positions, q_out, k_out, stream"},
+    {"tree", LSERVE_FASTCALL(py_tree),
+     "desc address, kv, q, k_new, v_new, cu_new, max_new_per_seq, out, lse_out, tree_mask, positions, sel_pages, sel_count, sel_seq_len, workspace, stream"},
     {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "native marshalling of the decode step's calls", -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "native marshalling of the calls of a decode step and on new tokens", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
