@@ -106,6 +106,32 @@ class DecodeSession:
                                self.out, self.lse, self.ws_decode)
         return self.out
 
+    def extend(self, new_lens: torch.Tensor, free_pages: Optional[torch.Tensor], cu_new: torch.Tensor, new_seq_lens: torch.Tensor,
+               pages_taken: torch.Tensor, positions: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+               ring_slots: Optional[torch.Tensor] = None, total_new: Optional[int] = None) -> None:
+        """Give every sequence the pages that new_lens more tokens need, and find where each of them goes (lserve_extend_tables)."""
+        B.lserve_extend_tables(self.desc, self.kv, new_lens, free_pages, cu_new, new_seq_lens, pages_taken, positions, slots, ring_slots,
+                               total_new=total_new)
+
+    def decode_tree(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cu_new: torch.Tensor, max_new_per_seq: int,
+                    tree_mask: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                    lse_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of drafted tokens behind the current lengths, whose K/V are in no page yet: over the pages of the last selection and
+        what was appended since, or over every page before the first one.  Those that are accepted are appended afterwards.
+
+        The output and the workspace are new tensors each time, so that a captured call keeps its own."""
+        if self.steps_since_selection is None:
+            sel = {}
+        else:
+            sel = dict(sel_pages=self.sel_pages, sel_count=self.sel_count, sel_seq_len=self.sel_seq_len)
+        batch, max_pages = self.kv.page_table.shape
+        out = torch.empty_like(q)
+        need = B.lserve_tree_workspace_bytes(self.desc, batch, q.shape[0], max_new_per_seq, max_pages, self.K if sel else 0)
+        workspace = torch.empty((max(need, 16),), dtype=torch.uint8, device=q.device)
+        B.lserve_sparse_decode_tree(self.desc, self.kv, q, k_new, v_new, cu_new, max_new_per_seq, out, lse_out, tree_mask=tree_mask,
+                                    positions=positions, workspace=workspace, **sel)
+        return out
+
     def step(self, q: torch.Tensor, seq_lens: torch.Tensor, prev_seq_lens: torch.Tensor,
              run_decode: bool = True) -> torch.Tensor:
         """One decode step.
