@@ -494,14 +494,9 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     // ---- softmax state and outputs of the lane's row (its keys: those of its half)
     float16_t acc[4] = {};
     float m_run = -INFINITY, l_run = 0.f, o_run = 0.f;  // (o_run: what all channels get, see ValueCodes)
-    int koff[8], voff[4];
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) koff[kk] = (kg * NB * 32 + n) * kRowBytes + k_chunk_pos(n, kk * 2 + half) * 16;
-#pragma unroll
-    for (int db = 0; db < 4; ++db) {
-        const int s16 = lane % 16, rr = s16 / 4, chunk = 4 * db + 2 * (n / 16) + (s16 % 4) / 2;
-        voff[db] = kg * NB * 32 * kRowBytes + half * 1024 + rr * kRowBytes + v_chunk_pos(rr, chunk) * 16 + 8 * (s16 % 2);
-    }
+    // Chunk kk of a key's row is at k_place ^ 32 kk and channels 32 db and on of a value's at v_place ^ 64 db.
+    const int k_place = (kg * NB * 32 + n) * kRowBytes + k_chunk_pos(n, half) * 16;
+    const int v_place = kg * NB * 32 * kRowBytes + half * 1024 + lane % 16 / 4 * kRowBytes + v_chunk_pos(lane % 16 / 4, 2 * (n / 16) + lane % 4 / 2) * 16 + 8 * (lane % 2);
 
     // keys of the entry that the lane's row sees, one bit each
     auto seen = [&](int2 w, int live) __attribute__((always_inline)) {
@@ -646,6 +641,10 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
             if (!__any(bits != 0)) return;
         }
         const unsigned char *ks = k_lds[stage], *vs = v_lds[stage];
+        int k_at = k_place;
+        // Where registers are short the eight places of a step are worked out in the step (64 x 16k tokens of 8 bits, 30 drafted: 204 us with the places
+        // kept and 33 other registers in scratch, 177 us with 25).
+        if constexpr (QUANT && RG == 4) asm volatile("" : "+v"(k_at));
         // (one block of keys: two chains of products, which do not wait for each other, instead of one)
         constexpr int kChains = 2 / NB;
         float16_t sc[NB], chain[NB * kChains] = {};
@@ -654,7 +653,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb) {
                 float16_t& sum = chain[kb * kChains + kk % kChains];
-                sum = Mfma<T>::run(*reinterpret_cast<const uint4*>(ks + kb * 32 * kRowBytes + koff[kk]), qreg[kk], sum);
+                sum = Mfma<T>::run(*reinterpret_cast<const uint4*>(ks + kb * 32 * kRowBytes + (k_at ^ 32 * kk)), qreg[kk], sum);
             }
         // schedule: operand reads run four ahead of the products that consume them, and no further (registers)
         __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
@@ -764,8 +763,8 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
         }
         l_run += (sum[0] + sum[1]) * (codes && !exact ? 0.5f : 1.f);
         auto values = [&](int step, int db) __attribute__((always_inline)) {  // V^T operand: channel 32 db + n of the lane's eight keys of the step's sixteen
-            const uint2 lo = lds_read_transposed(vs + (4 * step) * 1024 + voff[db]);
-            const uint2 hi = lds_read_transposed(vs + (4 * step + 2) * 1024 + voff[db]);
+            const uint2 lo = lds_read_transposed(vs + (4 * step) * 1024 + (v_place ^ 64 * db));
+            const uint2 hi = lds_read_transposed(vs + (4 * step + 2) * 1024 + (v_place ^ 64 * db));
             return make_uint4(lo.x, lo.y, hi.x, hi.y);
         };
 #pragma unroll
