@@ -1036,10 +1036,13 @@ struct TreeSizes {
     size_t pieces_bytes, ml_bytes, partial_bytes;
 };
 
-TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride) {
+TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride, bool quantised) {
     TreeSizes z = {};
+    // As few rows as the longest tree has (two and three times as many as it takes: 40 sequences of 100 .. 3000 tokens 36 -> 50 us with RG = 1 for 64
+    // rows, 36 -> 41 with RG = 4).  Quantised pages take four wavefronts to unpack, whoever has rows: 16 x 12k tokens of 8 bits under 32 rows 82 -> 76 us
+    // with RG = 2, 4 x 100k of 4 bits 134 -> 125, 64 x 500 .. 4000 of 8 bits 83 -> 76; 8 x 30k, of which 4096 selected, of 4 bits 27 -> 28.
     const long long rows = (long long)max_new * lp.group;
-    z.RG = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    z.RG = rows <= 32 && !quantised ? 1 : rows <= 64 ? 2 : 4;
     const int R = 32 * z.RG;
     z.row_tiles = (int)((rows + R - 1) / R);
     z.streams = __builtin_popcountll(lp.streaming_mask);
@@ -1065,7 +1068,7 @@ TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_ne
 }
 
 template <class T, int BITS> hipError_t launch_tree(const TreeArgs& a, void* workspace, hipStream_t stream) {
-    const TreeSizes z = tree_sizes(a.lp, a.kv.batch, a.total_new, a.max_new, a.kv.max_pages, a.sel_stride);
+    const TreeSizes z = tree_sizes(a.lp, a.kv.batch, a.total_new, a.max_new, a.kv.max_pages, a.sel_stride, BITS != 16);
     if (z.grid > 0x7fffffffLL || z.folds > 0x7fffffffLL) return hipErrorInvalidValue;
     TreeLaunch t = {};
     t.target = z.target;
@@ -1081,17 +1084,17 @@ template <class T, int BITS> hipError_t launch_tree(const TreeArgs& a, void* wor
         t.partials = reinterpret_cast<float4*>(p + z.pieces_bytes + z.ml_bytes);
     }
     const dim3 grid((unsigned)z.grid), folds((unsigned)std::max<long long>(std::min<long long>(z.folds, 2048), (z.folds + kWave - 1) / kWave));
-#define LSERVE_TREE(RG)                                                                                                              \
-    case RG:                                                                                                                         \
-        hipLaunchKernelGGL((draft_tree_kernel<T, BITS, RG>), grid, dim3(tree_waves(RG) * kWave), 0, stream, a, t);     \
-        if (z.folds) hipLaunchKernelGGL((fold_trees_kernel<T, RG>), folds, dim3(kFoldThreads), 0, stream, a, t);                     \
-        break
-    switch (z.RG) {
-        LSERVE_TREE(1);
-        LSERVE_TREE(2);
-        LSERVE_TREE(4);
-    }
-#undef LSERVE_TREE
+    auto launch = [&](auto blocks) {
+        constexpr int RG = decltype(blocks)::value;
+        hipLaunchKernelGGL((draft_tree_kernel<T, BITS, RG>), grid, dim3(tree_waves(RG) * kWave), 0, stream, a, t);
+        if (z.folds) hipLaunchKernelGGL((fold_trees_kernel<T, RG>), folds, dim3(kFoldThreads), 0, stream, a, t);
+    };
+    if (z.RG == 4)
+        launch(std::integral_constant<int, 4>{});
+    else if (z.RG == 2)
+        launch(std::integral_constant<int, 2>{});
+    else if constexpr (BITS == 16)
+        launch(std::integral_constant<int, 1>{});
     return hipGetLastError();
 }
 
@@ -1109,8 +1112,12 @@ template <class T> hipError_t launch_bits(const TreeArgs& a, void* workspace, hi
 }  // namespace
 
 size_t tree_workspace_bytes(const LayerParams& lp, int batch, int total_new, int max_new, int max_pages, int sel_stride) {
-    const TreeSizes z = tree_sizes(lp, batch, total_new, max_new, max_pages, sel_stride);
-    return z.pieces_bytes + z.ml_bytes + z.partial_bytes;
+    size_t most = 0;
+    for (bool quantised : {false, true}) {  // whichever the call comes with
+        const TreeSizes z = tree_sizes(lp, batch, total_new, max_new, max_pages, sel_stride, quantised);
+        most = std::max(most, z.pieces_bytes + z.ml_bytes + z.partial_bytes);
+    }
+    return most;
 }
 
 hipError_t preload_tree_kernels() {
