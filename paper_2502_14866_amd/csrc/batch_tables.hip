@@ -19,6 +19,8 @@ constexpr int kTokensPerThread = 4, kTableTokens = kTableThreads * kTokensPerThr
 // first of its tokens among its own; a maximum over the marks then tells every token its sequence.  The page of a token comes from the table
 // where it was there before and from the free list where it is new: the table entries other workgroups write are not read.  Workgroup 0
 // also writes what there is per sequence.
+// Bound: latency, of a launch and three loads that wait for each other (lengths, then a table entry or a free page).  64 sequences of one new token
+// 4.0 us; 500 prompts of 16 .. 8192 new tokens, 655 thousand in 640 workgroups and 13 MB, 8.6 us.
 __global__ __launch_bounds__(kTableThreads) void extend_tables_kernel(ExtendArgs a) {
     __shared__ int4 marks[kTableTokens];  // at the first token of a sequence: (sequence, its first token, pages handed out before, length)
     __shared__ int owner[kTableTokens];   // index of the mark, or -1
@@ -143,6 +145,7 @@ __global__ __launch_bounds__(kTableThreads) void extend_tables_kernel(ExtendArgs
 // Ancestors by doubling: before round r a node knows those of fewer than 2^r steps, and the 2^r-th of them, whose own set it takes over.  A workgroup
 // to a sequence, a thread to a node, WORDS words of the set in its registers; the sets meet in LDS, read by all before they are
 // written by any.  Rounds end when no node has an ancestor left (drafted trees are a handful of levels deep: two or three rounds).
+// Bound: latency.  16 trees of 32 tokens 3.0 us, 256 trees of up to 200 4.6 us.
 template <int WORDS>
 __global__ __launch_bounds__(WORDS * 64) void tree_masks_kernel(const int* __restrict__ parents, const int* __restrict__ cu_new,
                                                                 const int* __restrict__ seq_lens, int total_new, int max_new, int mask_words,

@@ -1,7 +1,9 @@
 // Rotary positions of queries and keys: of every head the first R channels are R / 2 pairs (a, b), and a token at position t has them
 // turned by the angle t f_i of the pair,
 //   a' = scale (a cos - b sin),  b' = scale (b cos + a sin),
-// the other channels passing as they are.  Bound: HBM, every row read once and written once.
+// the other channels passing as they are.  Bound: HBM, every row read once and written once.  65536 tokens of 40 heads, 1.34 GB, 244 us = 5.5 TB/s (a
+// copy of 1 GiB runs at 5.1); 9217 out of a fused projection, half of the channels turning, 40 us = 4.7 TB/s, 30 where the rows are in the last
+// cache still; 16 tokens 3.0 us, which is a launch, a position, an angle and a row one after the other.
 //
 // The angle is taken in 64 bits: in 32 a position of 10^6 would be off by 0.06 radians.  Its whole turns are dropped there (t f_i / 2 pi less the
 // nearest whole number, exact), and sine and cosine of the rest, once per token and pair and not once per head, are 32-bit ones, three
