@@ -497,7 +497,7 @@ int lserve_rotary_frequencies(const lserve_rotary_scaling *scaling, double *inv_
  * sequence) of the one that token j follows, or -1 where it follows the last token of the history; parents come before
  * their children (an entry that is not in [0, j) counts as -1).
  *   seq_lens         device [batch]: S_b, tokens of history
- *   max_new_per_seq  host bound of n_b, 1 .. 1024 (tokens past it are left alone)
+ *   max_new_per_seq  host bound of n_b, 1 .. 1024 and no more than total_new (tokens past it are left alone)
  *   mask_words       64-bit words of a row of tree_mask, max_new_per_seq / 64 rounded up or more
  *   tree_mask        device [total_new][mask_words] out: bit i % 64 of word i / 64 of row cu_new[b] + j is set iff i is j or an
  *                    ancestor of j
@@ -524,7 +524,7 @@ int lserve_tree_masks(const int32_t *parents, const int32_t *cu_new, const int32
  *                   scale + zero in fp32; values of a bf16 layer rounded to fp16, those of an fp16 layer not rounded).  stats are not used
  *   q               device [total_new][H][D]; k_new, v_new device [total_new][Hkv][D]
  *   cu_new          device [batch + 1] (batch = kv->batch), cu_new[0] = 0, n_b >= 0; rows from cu_new[batch] on are left alone
- *   max_new_per_seq host bound of n_b, 1 .. 1024
+ *   max_new_per_seq host bound of n_b, 1 .. 1024 and no more than total_new
  *   tree_mask       device [total_new][mask_words] (64 tokens to a word, max_new_per_seq / 64 rounded up words or more); positions device
  *                   [total_new]; both or neither
  *   sel_pages, sel_count, sel_seq_len, sel_stride: as in lserve_sparse_decode, or all three NULL (sel_stride is then 0)
