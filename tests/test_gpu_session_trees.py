@@ -17,24 +17,37 @@ def _i32(x):
     return torch.tensor(x + [0] * 4, dtype=torch.int32, device=DEV)[:len(x)]
 
 
+def _numbers(pages, bits):
+    """[pages][heads][bytes] -> [tokens][heads][D] in 64 bits."""
+    size = NP * D * bits // 8
+    code = pages[..., :size]
+    if bits == 4:
+        code = code.reshape(-1, 4)
+        code = torch.stack([code & 15, code >> 4], 1)
+    sz = pages[..., size:].contiguous().view(torch.float16).view(pages.shape[0], -1, NP, 2).double()
+    x = code.reshape(pages.shape[0], -1, NP, D).double() * sz[..., :1] + sz[..., 1:]
+    return x.transpose(1, 2).reshape(-1, x.shape[1], D)
+
+
 class Server:
     """A session, its free pages and, on the host, every token that the cache should hold."""
 
-    def __init__(self, batch, dtype, two_way, seed=0, width=12):
+    def __init__(self, batch, dtype, two_way, seed=0, width=12, bits=16):
         import paper_2502_14866_amd as L
         from paper_2502_14866_amd.session import DecodeSession
 
         L.load_library()
-        self.L, self.dtype, self.two_way, self.batch = L, dtype, two_way, batch
+        self.L, self.dtype, self.two_way, self.batch, self.bits = L, dtype, two_way, batch, bits
         self.g = torch.Generator().manual_seed(seed)
         pages = batch * width
-        zeros = lambda n, h: torch.zeros((n, h, NP, D), dtype=dtype, device=DEV)  # noqa: E731
+        shape, kind = ((NP, D), dtype) if bits == 16 else ((NP * D * bits // 8 + 256,), torch.uint8)
+        zeros = lambda n, h: torch.zeros((n, h) + shape, dtype=kind, device=DEV)  # noqa: E731
         heads = 1 if two_way else 2
         ring = SINK // NP + LOCAL // NP
         bounded = dict(k_pool_stream=zeros(batch * ring, 1), v_pool_stream=zeros(batch * ring, 1),
                        ring_table=torch.randperm(batch * ring, generator=self.g).to(torch.int32).view(batch, ring).to(DEV)) if two_way else {}
         self.s = DecodeSession(zeros(pages, heads), zeros(pages, heads), torch.full((batch, width), -1, dtype=torch.int32, device=DEV), HQ, [1, 0],
-                                 SINK, LOCAL, 128, **bounded)
+                                 SINK, LOCAL, 128, kv_bits=bits, dtype=dtype, **bounded)
         self.free = torch.randperm(pages, generator=self.g).to(torch.int32).to(DEV)
         self.rotary = L.RotaryDesc(rotary_dim=64)
         self.lens = [0] * batch
@@ -66,11 +79,14 @@ class Server:
         for b, n in enumerate(self.lens):  # the head of every token, page after page
             for w, pool in (("k", self.s.kv.k_pool), ("v", self.s.kv.v_pool)):
                 at = [int(p) for p in self.s.kv.page_table[b, :-(-n // NP)]]
+                if self.bits != 16:  # what the codes stand for
+                    self.rows[w][b] = _numbers(pool[at].cpu(), self.bits)[:n]
+                    continue
                 assert torch.equal(pool[at, -1].reshape(-1, D)[:n].cpu(), self.rows[w][b][:, 1])
 
     def expect(self, trees, q, k, v, pos, selected):
         p = Problem.__new__(Problem)
-        p.lens, p.trees, p.hq, p.hkv, p.dtype, p.bits, p.flags = list(self.lens), trees, HQ, HKV, self.dtype, 16, [1, 0]
+        p.lens, p.trees, p.hq, p.hkv, p.dtype, p.bits, p.flags = list(self.lens), trees, HQ, HKV, self.dtype, self.bits, [1, 0]
         p.s, p.w = SINK // NP, LOCAL // NP
         p.counts = [len(t) for t in trees]
         p.most = max(p.counts)
@@ -127,6 +143,24 @@ def test_prompts_drafts_and_what_is_accepted(dtype, two_way):
         paths = [_path(t, s.g) for t in trees]
         if turn == 1:
             paths[0] = []  # nothing of one tree
+        rows = torch.tensor([int(x.cu[b]) + j for b, p in enumerate(paths) for j in p], device=DEV)
+        s.grow([len(p) for p in paths], x.kr[rows], x.v[rows])
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_over_quantised_pages(dtype, bits):
+    s = Server(2, dtype, False, seed=3, bits=bits)
+    s.grow([210, 64])
+    for turn in range(3):
+        trees = [random_tree(n, s.g) for n in ((12, 5), (3, 40), (1, 30))[turn]]
+        x = s.drafts(trees)
+        if turn == 1:
+            s.s.select(x.q[[int(c) for c in x.cu[:-1]]].contiguous())
+        out = x.step()
+        torch.cuda.synchronize()
+        s.expect(trees, x.qr, x.kr, x.v, x.pos.tolist(), turn > 0).check(out, x.lse)
+        paths = [_path(t, s.g) for t in trees]
         rows = torch.tensor([int(x.cu[b]) + j for b, p in enumerate(paths) for j in p], device=DEV)
         s.grow([len(p) for p in paths], x.kr[rows], x.v[rows])
 
