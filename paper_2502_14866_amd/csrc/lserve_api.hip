@@ -466,7 +466,20 @@ int lserve_extend_tables(const lserve_attn_desc* desc, const lserve_paged_kv* kv
     if (kv->batch > 65535) return LSERVE_ERR_UNSUPPORTED;
     if (!new_lens || num_free < 0 || (num_free > 0 && !free_pages) || total_new < 0 || !cu_new || !new_seq_lens || !pages_taken)
         return LSERVE_ERR_INVALID_ARG;
-    if (new_seq_lens == kv->seq_lens || (ring_slots && !kv->ring_table)) return LSERVE_ERR_INVALID_ARG;
+    if (ring_slots && !kv->ring_table) return LSERVE_ERR_INVALID_ARG;
+    // what one workgroup writes others still read the lengths and the free list for
+    auto meet = [](const int32_t* a, long long n, const int32_t* b, long long m) { return a < b + m && b < a + n; };
+    const struct {
+        const int32_t* at;
+        long long n;
+    } in[] = {{kv->seq_lens, kv->batch}, {new_lens, kv->batch}, {free_pages, num_free}},
+      out[] = {{cu_new, kv->batch + 1LL}, {new_seq_lens, kv->batch}, {pages_taken, 1}};
+    for (const auto& o : out) {
+        for (const auto& i : in)
+            if (meet(o.at, o.n, i.at, i.n)) return LSERVE_ERR_INVALID_ARG;
+        for (const auto& other : out)
+            if (&other != &o && meet(o.at, o.n, other.at, other.n)) return LSERVE_ERR_INVALID_ARG;
+    }
     if (!aligned16(kv->page_table) || !aligned16(kv->seq_lens) || !aligned16(kv->ring_table) || !aligned16(new_lens) ||
         (reinterpret_cast<uintptr_t>(free_pages) & 3u) != 0 || !aligned16(cu_new) || !aligned16(new_seq_lens) || !aligned16(pages_taken) || !aligned16(positions) ||
         !aligned16(slots) || !aligned16(ring_slots))
