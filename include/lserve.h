@@ -527,7 +527,8 @@ int lserve_tree_masks(const int32_t *parents, const int32_t *cu_new, const int32
  *   max_new_per_seq host bound of n_b, 1 .. 1024 and no more than total_new
  *   tree_mask       device [total_new][mask_words] (64 tokens to a word, max_new_per_seq / 64 rounded up words or more); positions device
  *                   [total_new]; both or neither
- *   sel_pages, sel_count, sel_seq_len, sel_stride: as in lserve_sparse_decode, or all three NULL (sel_stride is then 0)
+ *   sel_pages, sel_count, sel_seq_len, sel_stride: as in lserve_sparse_decode (every entry counts, in any order; pages behind the history are
+ *                   passed over), or all three NULL (sel_stride is then 0)
  *   out             device [total_new][H][D]; lse_out device [total_new][H] fp32 or NULL
  *   workspace       device, lserve_tree_workspace_bytes(...) for these sizes or more, any contents; calls that may run at the same time
  *                   need one each

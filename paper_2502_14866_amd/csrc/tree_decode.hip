@@ -328,14 +328,20 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     // ---- the list: entries of history, then tiles of drafted tokens
     const int drafts = ceil_div(s.n, kTile);
     const bool ring = in_stream_pool(a.lp, a.kv, hk);
-    const int entries = streaming ? s.stream : s.dense, history = entries - drafts;
+    const size_t head = (size_t)b * a.lp.Hkv + hk;
     // (the first `listed` entries are named by a list or a formula, the pages from first_new on follow; a list that holds fewer than it may
     // ends in entries of nothing, so that its length need not be waited for)
-    const int listed = streaming ? min(a.lp.sink_pages, s.pages) : a.sel_pages ? min(s.then, a.sel_stride) : s.pages;
+    const bool selects = a.sel_pages && !streaming;
+    const int named = selects ? min(a.sel_count[head], a.sel_stride) : 0;
+    int listed = streaming ? min(a.lp.sink_pages, s.pages) : selects ? min(s.then, a.sel_stride) : s.pages;
     const int first_new = streaming ? first_local_page(a.lp, s.len) : s.then;
-    const int share = entries / u.pieces, rest = entries - share * u.pieces;
-    const int e0 = uniform(u.piece * share + min(u.piece, rest)), e1 = uniform(e0 + share + (u.piece < rest ? 1 : 0));
-    const size_t head = (size_t)b * a.lp.Hkv + hk;
+    int entries, history, e0, e1;
+    auto cut = [&](int all) __attribute__((always_inline)) {
+        entries = all, history = all - drafts;
+        const int share = all / u.pieces, rest = all - share * u.pieces;
+        e0 = uniform(u.piece * share + min(u.piece, rest)), e1 = uniform(e0 + share + (u.piece < rest ? 1 : 0));
+    };
+    cut(streaming ? s.stream : s.dense);
     // Entry from + lane: (position of the page, physical page) or (drafted tile, -1); a position behind the last page: nothing of it is read.
     // Lane i of every wave has entry i of a stretch of 64: reading it costs no trip to memory, and no wave waits for another.
     auto look_up = [&](int from) __attribute__((always_inline)) {
@@ -344,9 +350,9 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
         if (e < e1 && e >= history) w = make_int2(e - history, -1);
         if (e < min(e1, history)) {
             int p = e < listed ? e : first_new + (e - listed);
-            if (a.sel_pages && !streaming && e < listed) {
+            if (selects && e < listed) {
                 p = a.sel_pages[head * a.sel_stride + e];
-                if (e >= a.sel_count[head]) p = -1;
+                if (e >= named) p = -1;
             }
             if (p >= 0 && p < s.pages) {
                 const int phys = ring ? a.kv.ring_table[(size_t)b * a.kv.ring + ring_slot(a.lp, p)] : a.kv.page_table[(size_t)b * a.kv.max_pages + p];
@@ -375,6 +381,13 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
         own_tile /= kTile;
     }
     int2 stretch = look_up(e0);
+    // A list may also name more pages than there are or were: one of them twice, or in any order after tokens were taken back.  Its pieces are as many
+    // as those of one that does not, and longer.
+    if (__builtin_expect(uniform(named) > listed, 0)) {
+        cut(entries + uniform(named) - listed);
+        listed = uniform(named);
+        stretch = look_up(e0);
+    }
     // (pinned once the first keys are on their way: left alone the loads sink into the loop, where they wait for its prefetch)
     auto pin_queries = [&]() __attribute__((always_inline)) {
 #pragma unroll
