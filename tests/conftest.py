@@ -23,6 +23,19 @@ def pytest_collection_modifyitems(config, items):
             item.add_marker(skip)
 
 
+@pytest.fixture(autouse=True)
+def _both_routes_of_the_binding_get_the_same_tensors(request):
+    """test_new_calls_native.py compares what two routes hand over, addresses among them; one of these lies inside a tensor and has no name there,
+    so the comparison held only where the allocator happened to place the second route's tensors where the first one's had been."""
+    if not request.node.nodeid.split("::")[0].endswith("test_new_calls_native.py"):
+        yield
+        return
+    made = request.module._tensors()
+    with pytest.MonkeyPatch.context() as m:  # (its own: the test undoes what it has patched itself half way)
+        m.setattr(request.module, "_tensors", lambda: dict(made))
+        yield
+
+
 _observed = []  # (test id, what, kind, max abs, max row-relative)
 
 
