@@ -805,8 +805,8 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     // ---- walk
     if (tid < 2) spoiled[tid] = 0;
     {
-        const int tile = (int)wave_max((float)own_tile);
-        if (lane == 0) deepest[wave] = tile;
+        const int tile = wave_scan(own_tile, 0, larger);  // (as whole numbers: tiles go up to 2^25)
+        if (lane == kWave - 1) deepest[wave] = tile;
     }
     if constexpr (QUANT) {
 #pragma unroll
