@@ -520,8 +520,8 @@ int lserve_tree_masks(const int32_t *parents, const int32_t *cu_new, const int32
  * tree_mask = positions = NULL: a chain, token j at position S_b + j after token j - 1.  A token that attends nothing gets out = 0 and
  * lse = -inf.  What a token does not attend, be it not a number, leaves no trace in its result.
  *
- *   kv              N_P = 64; one pool or the two-way cache, pages of 16-bit rows or quantised (kv_bits 8 or 4: keys enter as code *
- *                   scale + zero in fp32; values of a bf16 layer rounded to fp16, those of an fp16 layer not rounded).  stats are not used
+ *   kv              N_P = 64; one pool or the two-way cache, pages of 16-bit rows or quantised (kv_bits 8 or 4: keys and values are
+ *                   code * scale + zero, not rounded).  stats are not used
  *   q               device [total_new][H][D]; k_new, v_new device [total_new][Hkv][D]
  *   cu_new          device [batch + 1] (batch = kv->batch), cu_new[0] = 0, n_b >= 0; rows from cu_new[batch] on are left alone
  *   max_new_per_seq host bound of n_b, 1 .. 1024 and no more than total_new

@@ -227,9 +227,11 @@ template <class T, int BITS> __device__ __forceinline__ uint4 codes8(uint2 codes
 
 __device__ __forceinline__ uint2 two_words(uint2 x) { return x; }
 __device__ __forceinline__ uint2 two_words(uint32_t x) { return make_uint2(x, 0u); }
-// Values of an fp16 layer's quantised pages.  Rounded to fp16 in LDS, next to weights rounded to fp16, they would make the second error of that size;
-// so LDS has (code - kMiddle) 2^e there, which is exact, with 2^e the power of two in the row's scale (as far as fp16 has it), and what is left of the
-// scale, in [1, 2) as a rule, meets the weight in fp32 before that is rounded.  The middle of the codes and the zero go into a sum of the row's own.
+// Values of quantised pages.  As fp16 numbers in LDS, next to weights rounded to fp16, they would make the second error of that size, and fp16 has not
+// the range of a scale times a code: tiny rows would lose their scale, loud ones of a bf16 layer become infinite.  So LDS has (code - kMiddle) 2^e,
+// which is exact, with 2^e the power of two in the row's scale (as far as fp16 has it), and what is left of the scale, in [1, 2) as a rule, meets the
+// weight in fp32 before that is rounded.  The middle of the codes and the zero go into a sum of the row's own.  (Under a bf16 layer, against values
+// rounded to fp16, which a fused multiply and add makes: 64 x 16k in 4-bit pages 193 -> 209 us, 4 x 100k 121 -> 125, in 8-bit pages 217 -> 231 and 144 -> 146.)
 template <int BITS> struct ValueCodes {
     static constexpr int kMiddle = 1 << (BITS - 1);
     static __device__ __forceinline__ uint32_t power(uint32_t scale_zero) {  // 2^e as fp16
@@ -251,10 +253,6 @@ template <int BITS> struct ValueCodes {
         return make_uint4(pair(lo, 0x04010400u), pair(lo, 0x04030402u), pair(hi, 0x04010400u), pair(hi, 0x04030402u));
     }
 };
-__device__ __forceinline__ uint32_t halved(uint32_t two) {  // of fp16
-    const half2_t h = {(_Float16)0.5f, (_Float16)0.5f};
-    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, two) * h);
-}
 
 // A block of 32 output rows, O^T in the lanes ((n, half) holds channels 32 db + 8 (i / 4) + 4 half + i % 4 of row n), out through 8 KiB of LDS so
 // that sixteen lanes store a row.
@@ -298,8 +296,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     __shared__ __attribute__((aligned(1024))) unsigned char k_lds[2][kTileBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char v_lds[2][kTileBytes];
     __shared__ __attribute__((aligned(16))) float k_scale[QUANT ? 2 : 1][2][QUANT ? kTile : 4];  // of the keys of a stage, times the softmax scale: scale, zero
-    constexpr bool kExact = QUANT && std::is_same<T, F16>::value;  // see ValueCodes
-    __shared__ __attribute__((aligned(16))) float v_scale[kExact ? 2 : 1][2][kExact ? kTile : 4];  // of the values: what is left of the scale, middle and zero
+    __shared__ __attribute__((aligned(16))) float v_scale[QUANT ? 2 : 1][2][QUANT ? kTile : 4];  // of the values: what is left of the scale, middle and zero
     __shared__ float2 fold_ml[RG][32];
     __shared__ unsigned spoiled_keys[2];
     __shared__ int spoiled[2];  // does a tile that some row does not see whole hold values that are not numbers?
@@ -477,12 +474,11 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
                 }
             }
             if (wave == 0) staged.kz = *reinterpret_cast<const uint32_t*>(kp + (kTile * kCodeBytes + (unsigned)min(lane, live - 1) * 4));
-            if (kExact && wave == 1) staged.vz_all = *reinterpret_cast<const uint32_t*>(vp + (kTile * kCodeBytes + (unsigned)min(lane, live - 1) * 4));
+            if (wave == 1) staged.vz_all = *reinterpret_cast<const uint32_t*>(vp + (kTile * kCodeBytes + (unsigned)min(lane, live - 1) * 4));
         }
     };
     // Keys go into LDS as their codes, exactly, and meet scale and zero as scores in fp32 (rounded keys would cost the log-sum-exp three
-    // digits).  Values of a bf16 layer go there as fp16 numbers: they come from fp16 scales and zeros, and 11 bits at three instructions for two of
-    // them are better than 8 at six.  Half of each, so that none passes 65504; the weights they meet are doubled.  Those of an fp16 layer: see ValueCodes.
+    // digits).  Values: see ValueCodes.
     auto store_staged = [&](int stage) __attribute__((always_inline)) {
         if constexpr (QUANT) {
             if (!staged.on) return;
@@ -490,20 +486,17 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
             for (int i = 0; i < kLoads; ++i) {
                 const unsigned to = (wave * kLoads + i) * 1024 + lane * 16;
                 *reinterpret_cast<uint4*>(k_lds[stage] + to) = codes8<T, BITS>(two_words(staged.k[i]));
-                if constexpr (kExact)
-                    *reinterpret_cast<uint4*>(v_lds[stage] + to) = ValueCodes<BITS>::operands(two_words(staged.v[i]), staged.vz[i]);
-                else
-                    *reinterpret_cast<uint4*>(v_lds[stage] + to) = dequantise8<F16, BITS>(two_words(staged.v[i]), halved(staged.vz[i]));
+                *reinterpret_cast<uint4*>(v_lds[stage] + to) = ValueCodes<BITS>::operands(two_words(staged.v[i]), staged.vz[i]);
             }
             if (wave == 0) {
                 const float scale = Elem<F16>::lo(staged.kz), zero = Elem<F16>::hi(staged.kz);
                 k_scale[stage][0][lane] = scale / KeyCodes<T, BITS>::unit * a.lp.sm_scale_log2;
                 k_scale[stage][1][lane] = (zero - KeyCodes<T, BITS>::offset * scale) * a.lp.sm_scale_log2;
             }
-            if (kExact && wave == 1) {
+            if (wave == 1) {
                 const float scale = Elem<F16>::lo(staged.vz_all), zero = Elem<F16>::hi(staged.vz_all);
-                v_scale[kExact ? stage : 0][0][lane] = scale / Elem<F16>::lo(ValueCodes<BITS>::power(staged.vz_all));
-                v_scale[kExact ? stage : 0][1][lane] = zero + scale * ValueCodes<BITS>::kMiddle;
+                v_scale[stage][0][lane] = scale / Elem<F16>::lo(ValueCodes<BITS>::power(staged.vz_all));
+                v_scale[stage][1][lane] = zero + scale * ValueCodes<BITS>::kMiddle;
             }
         }
     };
@@ -555,9 +548,8 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
         const int live = live_rows(w);
         return live > 0 && (live < kTile || w.y < 0 || (streaming && w.x >= a.lp.sink_pages && w.x <= deepest_tile - a.lp.local_pages));
     };
-    auto exponent = [&](int2 w) __attribute__((always_inline)) { return QUANT && w.y >= 0 ? BitsOf<F16>::exponent : BitsOf<T>::exponent; };
-    auto look_for_spoiled = [&](auto kind, int2 w, int stage) __attribute__((always_inline)) {
-        if (kExact && decltype(kind)::value) return;  // codes are numbers
+    // (Codes are numbers, and scales and zeros that are not are kept from weights of zero: this is for rows of 16 bits.)
+    auto look_for_spoiled = [&](int2 w, int stage) __attribute__((always_inline)) {
         if (!ragged(w)) return;
         const uint4* const brought = reinterpret_cast<const uint4*>(v_lds[stage] + wave * kLoads * 1024) + lane;
         ushort2_t most = {0, 0};  // magnitude, as whole numbers
@@ -568,12 +560,12 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
 #pragma unroll
             for (int c = 0; c < 4; ++c) most = __builtin_elementwise_max(most, __builtin_bit_cast(ushort2_t, x4[c] & 0x7fff7fffu));
         }
-        const uint32_t exponents = exponent(w);
+        constexpr uint32_t exponents = BitsOf<T>::exponent;
         if (__any(most[0] >= exponents || most[1] >= exponents)) spoiled[stage] = 1;
     };
     // (together; the bits of the keys that have such values)
-    auto clear_spoiled = [&](int2 w, int stage) __attribute__((always_inline)) -> unsigned long long {
-        const uint32_t low = exponent(w), high = low << 16;
+    auto clear_spoiled = [&](int stage) __attribute__((always_inline)) -> unsigned long long {
+        constexpr uint32_t low = BitsOf<T>::exponent, high = low << 16;
         constexpr int kPieces = kTileBytes / 16 / (kWaves * kWave);
         uint4* const mine = reinterpret_cast<uint4*>(v_lds[stage]) + tid;
         __syncthreads();
@@ -602,8 +594,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
                (unsigned)__builtin_amdgcn_readfirstlane(spoiled_keys[0]);
     };
     // Those values, from where they came from, to the rows that do see their keys: weight times value in fp32.
-    auto add_spoiled = [&](auto kind, int2 w, int stage, unsigned long long bits, float off, unsigned long long keys) __attribute__((always_inline)) {
-        constexpr bool codes = decltype(kind)::value;
+    auto add_spoiled = [&](int2 w, int stage, unsigned long long bits, float off, unsigned long long keys) __attribute__((always_inline)) {
         const bool drafted = w.y < 0;
         for (keys &= (NB == 2 ? ~0ull : 0xffffffffull << (32 * kg)); keys; keys &= keys - 1) {
             const int key = __builtin_ctzll(keys), from = min(key, live_rows(w) - 1);
@@ -617,30 +608,16 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
             }
             score = halves_sum(score);
             const bool on = bits >> key & 1ull;
-            if constexpr (codes)
-                score = __builtin_fmaf(score, k_scale[stage][0][key], __builtin_fmaf(k_scale[stage][1][key], q_sum, off));
-            else
-                score = __builtin_fmaf(score, a.lp.sm_scale_log2, off);
-            const float p = __builtin_amdgcn_exp2f(score);
-            const unsigned char* const page = v_base + (size_t)w.y * page_bytes;
-            const unsigned char* const src =
-                drafted ? (const unsigned char*)a.v_new + new_offset + ((size_t)w.x * kTile + from) * new_row_bytes
-                        : page + from * (kHeadDim * BITS / 8);
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(score, a.lp.sm_scale_log2, off));
+            const unsigned char* const src = drafted ? (const unsigned char*)a.v_new + new_offset + ((size_t)w.x * kTile + from) * new_row_bytes
+                                                     : v_base + (size_t)w.y * page_bytes + from * kRowBytes;
 #pragma unroll
             for (int db = 0; db < 4; ++db)
 #pragma unroll
                 for (int g4 = 0; g4 < 4; ++g4) {
                     const int c = 4 * db + g4;  // eight channels, of which the lane has four
-                    float v4[4];
-                    if constexpr (codes) {
-                        const uint32_t scale_zero = reinterpret_cast<const uint32_t*>(page + kTile * kCodeBytes)[from];
-                        const uint4 eight = dequantise8<F16, BITS>(two_words(*reinterpret_cast<const Codes*>(src + c * BITS)), halved(scale_zero));
-                        const uint2 x = half ? make_uint2(eight.z, eight.w) : make_uint2(eight.x, eight.y);
-                        v4[0] = Elem<F16>::lo(x.x), v4[1] = Elem<F16>::hi(x.x), v4[2] = Elem<F16>::lo(x.y), v4[3] = Elem<F16>::hi(x.y);
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2*>(src + c * 16 + 8 * half);
-                        v4[0] = Elem<T>::lo(x.x), v4[1] = Elem<T>::hi(x.x), v4[2] = Elem<T>::lo(x.y), v4[3] = Elem<T>::hi(x.y);
-                    }
+                    const uint2 x = *reinterpret_cast<const uint2*>(src + c * 16 + 8 * half);
+                    const float v4[4] = {Elem<T>::lo(x.x), Elem<T>::hi(x.x), Elem<T>::lo(x.y), Elem<T>::hi(x.y)};
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (on && !(fabsf(v4[i]) < INFINITY)) acc[db][4 * g4 + i] += p * v4[i];
@@ -694,9 +671,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
         // a distance of up to kSlack: weights up to 2^kSlack do no harm in any of the types, and outputs are rescaled a few times a list
         // instead of in most steps.
         const bool unset = m_run == -INFINITY;
-        constexpr bool exact = codes && kExact;
-        const float doubled = codes && !exact ? 1.f : 0.f;  // weights of quantised values (see store_staged)
-        float off = (unset ? 0.f : -m_run) + doubled;
+        float off = unset ? 0.f : -m_run;
         if constexpr (codes) {
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb)
@@ -728,12 +703,12 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
-        top = halves_max(top) - doubled;
+        top = halves_max(top);
         const bool moves = unset ? top > -INFINITY : top > kSlack;
         if (__builtin_expect(__any(moves), 0)) {
             const float delta = moves ? top : 0.f, alpha = unset ? 0.f : __builtin_amdgcn_exp2f(-delta);
             l_run *= alpha;
-            if constexpr (kExact) o_run *= alpha;
+            if constexpr (QUANT) o_run *= alpha;
 #pragma unroll
             for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -743,7 +718,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[kb][i] -= delta;
             if (moves) m_run = unset ? delta : m_run + delta;
-            off = (m_run == -INFINITY ? 0.f : -m_run) + doubled;
+            off = m_run == -INFINITY ? 0.f : -m_run;
         }
         using V = typename std::conditional<codes, F16, T>::type;  // of the values in LDS
         uint4 pb[NB][2];
@@ -756,7 +731,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
                 p[i] = __builtin_amdgcn_exp2f(sc[kb][i]);
                 sum[i % 2] += p[i];  // unrounded; the second product takes them in the layer's type, which is what its operands are
             }
-            if constexpr (exact) {
+            if constexpr (codes) {
 #pragma unroll
                 for (int g4 = 0; g4 < 4; ++g4) {
                     const int key = (kg * NB + kb) * 32 + 8 * g4 + 4 * half;
@@ -780,7 +755,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
             pb[kb][0] = pack8<V>(p);
             pb[kb][1] = pack8<V>(p + 8);
         }
-        l_run += (sum[0] + sum[1]) * (codes && !exact ? 0.5f : 1.f);
+        l_run += sum[0] + sum[1];
         auto values = [&](int step, int db) __attribute__((always_inline)) {  // V^T operand: channel 32 db + n of the lane's eight keys of the step's sixteen
             const uint2 lo = lds_read_transposed(vs + (4 * step) * 1024 + (v_place ^ 64 * db));
             const uint2 hi = lds_read_transposed(vs + (4 * step + 2) * 1024 + (v_place ^ 64 * db));
@@ -797,8 +772,8 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
-        if constexpr (!exact) {
-            if (__builtin_expect(keys != 0, 0)) add_spoiled(kind, w, stage, bits, off, keys);
+        if constexpr (!codes) {
+            if (__builtin_expect(keys != 0, 0)) add_spoiled(w, stage, bits, off, keys);
         }
     };
 
@@ -821,7 +796,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     auto step = [&](auto kind, int2 w, int stage) __attribute__((always_inline)) {
         const bool part = ragged(w);
         unsigned long long keys = 0;
-        if (!(kExact && decltype(kind)::value) && part && __builtin_expect(uniform(spoiled[stage]) != 0, 0)) keys = clear_spoiled(w, stage);
+        if (!decltype(kind)::value && part && __builtin_expect(uniform(spoiled[stage]) != 0, 0)) keys = clear_spoiled(stage);
         work_on(kind, w, stage, part, keys);
     };
     auto find_deepest = [&]() __attribute__((always_inline)) {  // past a barrier
@@ -853,8 +828,6 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     find_deepest();
     pin_queries();
     if constexpr (QUANT) {
-        if (e0 < coded) look_for_spoiled(std::true_type{}, w0, 0);
-        __syncthreads();
         auto turn = [&](int e, int stage) __attribute__((always_inline)) {
             w2 = next_entry(e + 2);
             if (e + 1 < coded)
@@ -863,7 +836,6 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
                 fetch(w1, k_lds[stage ^ 1], v_lds[stage ^ 1]);
             if (e + 2 < coded) fetch_codes(w2);
             step(std::true_type{}, w0, stage);
-            if (e + 1 < coded) look_for_spoiled(std::true_type{}, w1, stage ^ 1);
             w0 = w1;
             w1 = w2;
             __syncthreads();
@@ -876,7 +848,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     {
         auto turn = [&](int e, int stage) __attribute__((always_inline)) {
             dma_wait();
-            look_for_spoiled(std::false_type{}, w0, stage);
+            look_for_spoiled(w0, stage);
             __syncthreads();  // the tiles of this step are there, and those of the step before are done with
             if constexpr (!QUANT) w1 = next_entry(e + 1);
             if (e + 1 < e1) fetch(w1, k_lds[stage ^ 1], v_lds[stage ^ 1]);
@@ -898,7 +870,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
 
     // ---- the two halves of the keys meet in LDS (the tiles are done with: the loop ended on a barrier)
     float l = halves_sum(l_run), m = m_run;
-    if constexpr (kExact) {
+    if constexpr (QUANT) {
         const float o = halves_sum(o_run);
 #pragma unroll
         for (int db = 0; db < 4; ++db)
