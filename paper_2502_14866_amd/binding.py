@@ -206,10 +206,8 @@ class _CtypesCalls:
         _checked("lserve_extend_tables", (kv.page_table, i32, 0), (kv.seq_lens, i32, batch), (kv.ring_table, i32, 0), (new_lens, i32, batch),
                  (free_pages, i32, 0), (cu_new, i32, batch + 1), (new_seq_lens, i32, batch), (pages_taken, i32, 1),
                  (positions, i32, total_new), (slots, i64, total_new), (ring_slots, i64, total_new))
-        if ring_slots is not None and kv.ring_table is not None and d.page_size > 0:
-            ring = -(-d.sink_tokens // d.page_size) - (-d.local_tokens // d.page_size)
-            if kv.ring_table.numel() < batch * ring:
-                raise ValueError(f"lserve_extend_tables: a ring table of {kv.ring_table.numel()} entries for {batch} sequences of {ring}")
+        if ring_slots is not None and kv.ring_table is not None and kv.ring_table.numel() < batch * _ring(d):
+            raise ValueError(f"lserve_extend_tables: a ring table of {kv.ring_table.numel()} entries for {batch} sequences of {_ring(d)}")
         return load_library().lserve_extend_tables(
             d, kv.c(), _ptr(new_lens), _ptr(free_pages), 0 if free_pages is None else free_pages.numel(), total_new, _ptr(cu_new),
             _ptr(new_seq_lens), _ptr(pages_taken), _ptr(positions), _ptr(slots), _ptr(ring_slots), stream)
@@ -239,9 +237,15 @@ class _CtypesCalls:
         total, dim, hq, hkv, dt = (0 if q is None else q.shape[0]), d.head_dim, d.num_q_heads, d.num_kv_heads, _dtype(d)
         words = 0 if tree_mask is None else tree_mask.shape[-1]
         stride = 0 if sel_pages is None else sel_pages.shape[-1]
+        kind, slab = _slab(d, kv.kv_bits)
+        streams = sum(d.kv_head_is_streaming[:hkv]) if kv.k_pool_stream is not None else 0
+        kv.c()
+        pool, bounded = kv._c.num_pages * (kv.pool_heads or hkv) * slab, kv._c.num_pages_stream * streams * slab
         _checked("lserve_sparse_decode_tree", (q, dt, total * hq * dim), (k_new, dt, total * hkv * dim), (v_new, dt, total * hkv * dim),
                  (out, dt, total * hq * dim), (lse_out, torch.float32, total * hq), (cu_new, i32, batch + 1), (kv.seq_lens, i32, batch),
-                 (kv.page_table, i32, 0), (kv.k_pool, (dt, torch.uint8), 0), (tree_mask, torch.int64, total * words), (positions, i32, total),
+                 (kv.page_table, i32, 0), (kv.k_pool, kind, pool), (kv.v_pool, kind, pool), (kv.k_pool_stream, kind, bounded),
+                 (kv.v_pool_stream, kind, bounded), (kv.ring_table, i32, batch * _ring(d) if kv.k_pool_stream is not None else 0),
+                 (tree_mask, torch.int64, total * words), (positions, i32, total),
                  (sel_pages, i32, batch * hkv * stride), (sel_count, i32, batch * hkv), (sel_seq_len, i32, batch))
         return load_library().lserve_sparse_decode_tree(
             d, kv.c(), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(cu_new), _ptr(tree_mask), words, _ptr(positions), _ptr(sel_pages),
@@ -251,6 +255,18 @@ class _CtypesCalls:
 
 def _dtype(desc: "_CAttnDesc") -> torch.dtype:
     return torch.bfloat16 if desc.dtype == 1 else torch.float16
+
+
+def _ring(desc: "_CAttnDesc") -> int:
+    """Entries of a sequence in the ring table of the two-way cache."""
+    return -(-desc.sink_tokens // desc.page_size) - (-desc.local_tokens // desc.page_size) if desc.page_size > 0 else 0
+
+
+def _slab(desc: "_CAttnDesc", bits: int) -> tuple:
+    """(type, elements) of one head's rows in a page; with a number of bits that the library refuses, any type and none."""
+    if bits in (0, 16):
+        return _dtype(desc), max(0, desc.page_size * desc.head_dim)
+    return (torch.uint8, 8 * desc.head_dim * bits + 256) if bits in (8, 4) else ((_dtype(desc), torch.uint8), 0)
 
 
 def _checked(where: str, *args) -> None:

@@ -123,6 +123,7 @@ struct TreeArgs {
     const unsigned long long* tree_mask; // [total_new][mask_words]
     const int *sel_pages, *sel_count, *sel_seq_len;  // all null: every page
     int mask_words, sel_stride, total_new, max_new;
+    int stream_pages;                    // of the streaming heads' pool, where there is one
     uint16_t* out;
     float* lse_out;
 };

@@ -619,6 +619,7 @@ int lserve_sparse_decode_tree(const lserve_attn_desc* desc, const lserve_paged_k
     a.sel_stride = sel_stride;
     a.total_new = total_new;
     a.max_new = max_new_per_seq;
+    a.stream_pages = kv->num_pages_stream;
     a.out = (uint16_t*)out;
     a.lse_out = lse_out;
     const hipError_t e = launch_sparse_decode_tree(desc->dtype, a, workspace, (hipStream_t)stream);

@@ -186,32 +186,34 @@ PyObject* py_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-struct HeldKV {  // the tensors of a PagedKV that are checked
-    Attribute table_o, lens_o, ring_o, pool_o;
-    const at::Tensor *table, *lens, *ring, *pool;
-    explicit HeldKV(PyObject* kv)
-        : table_o(kv, names[kPageTable]), lens_o(kv, names[kSeqLens]), ring_o(kv, names[kRingTable]), pool_o(kv, names[kKPool]),
-          table(tensor_or_null(table_o.o)), lens(tensor_or_null(lens_o.o)), ring(tensor_or_null(ring_o.o)), pool(tensor_or_null(pool_o.o)) {}
+struct Held {  // a tensor of a PagedKV that is checked
+    Attribute o;
+    const at::Tensor* t;
+    Held(PyObject* kv, int name) : o(kv, names[name]), t(tensor_or_null(o.o)) {}
 };
+
+// Entries of a sequence in the ring table of the two-way cache.
+int64_t ring_of(const lserve_attn_desc* d) {
+    if (d->page_size <= 0) return 0;
+    const int64_t page = d->page_size;
+    return (d->sink_tokens + page - 1) / page + (d->local_tokens + page - 1) / page;
+}
 
 PyObject* py_extend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 12, [&] {
         const char* where = "lserve_extend_tables";
         const lserve_attn_desc* desc = description(a[0]);
         const lserve_paged_kv kv = paged(a[1]);
-        const HeldKV held(a[1]);
+        const Held table(a[1], kPageTable), now(a[1], kSeqLens), ring_table(a[1], kRingTable);
         const at::Tensor *fresh = tensor_or_null(a[2]), *pages = tensor_or_null(a[3]), *cu = tensor_or_null(a[4]), *lens = tensor_or_null(a[5]),
                          *taken = tensor_or_null(a[6]), *pos = tensor_or_null(a[7]), *slots = tensor_or_null(a[8]), *ring = tensor_or_null(a[9]);
         const int64_t batch = kv.batch, total = PyLong_AsLongLong(a[10]);
         if (total == -1 && PyErr_Occurred()) throw PythonError();
-        check(where, {{held.table, kInt, 0}, {held.lens, kInt, batch}, {held.ring, kInt, 0}, {fresh, kInt, batch}, {pages, kInt, 0},
+        check(where, {{table.t, kInt, 0}, {now.t, kInt, batch}, {ring_table.t, kInt, 0}, {fresh, kInt, batch}, {pages, kInt, 0},
                       {cu, kInt, batch + 1}, {lens, kInt, batch}, {taken, kInt, 1}, {pos, kInt, total}, {slots, kLong, total}, {ring, kLong, total}});
-        if (ring && held.ring && desc->page_size > 0) {
-            const int64_t slots_of_ring = (desc->sink_tokens + desc->page_size - 1) / desc->page_size + (desc->local_tokens + desc->page_size - 1) / desc->page_size;
-            if (held.ring->numel() < batch * slots_of_ring)
-                refuse(where, "a ring table of " + std::to_string(held.ring->numel()) + " entries for " + std::to_string(batch) + " sequences of " +
-                                  std::to_string(slots_of_ring));
-        }
+        if (ring && ring_table.t && ring_table.t->numel() < batch * ring_of(desc))
+            refuse(where, "a ring table of " + std::to_string(ring_table.t->numel()) + " entries for " + std::to_string(batch) + " sequences of " +
+                              std::to_string(ring_of(desc)));
         const int32_t* p_fresh = address<int32_t>(fresh);
         const int32_t *p_pages = address<int32_t>(pages), num_free = pages ? (int32_t)pages->numel() : 0;
         int32_t *p_cu = address<int32_t>(cu), *p_lens = address<int32_t>(lens), *p_taken = address<int32_t>(taken), *p_pos = address<int32_t>(pos);
@@ -271,16 +273,25 @@ PyObject* py_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const char* where = "lserve_sparse_decode_tree";
         const lserve_attn_desc* desc = description(a[0]);
         const lserve_paged_kv kv = paged(a[1]);
-        const HeldKV held(a[1]);
+        const Held table(a[1], kPageTable), now(a[1], kSeqLens), ring_table(a[1], kRingTable), k_pool(a[1], kKPool), v_pool(a[1], kVPool),
+            k_stream(a[1], kKStream), v_stream(a[1], kVStream);
         const at::Tensor *q = tensor_or_null(a[2]), *k = tensor_or_null(a[3]), *v = tensor_or_null(a[4]), *cu = tensor_or_null(a[5]),
                          *out = tensor_or_null(a[7]), *lse = tensor_or_null(a[8]), *mask = tensor_or_null(a[9]), *pos = tensor_or_null(a[10]),
                          *sel = tensor_or_null(a[11]), *count = tensor_or_null(a[12]), *len = tensor_or_null(a[13]), *ws = tensor_or_null(a[14]);
         const int64_t dim = desc->head_dim, hq = desc->num_q_heads, hkv = desc->num_kv_heads, batch = kv.batch, total = q && q->dim() ? q->size(0) : 0;
         const int64_t words = mask && mask->dim() ? mask->size(-1) : 0, stride = sel && sel->dim() ? sel->size(-1) : 0;
         const at::ScalarType t = type_of(desc);
+        // of one head's rows in a page; a number of bits that is neither is the library's to refuse
+        const bool rows16 = kv.kv_bits == 0 || kv.kv_bits == 16, codes = kv.kv_bits == 8 || kv.kv_bits == 4;
+        const int64_t slab = rows16 ? desc->page_size * dim : codes ? 8 * dim * kv.kv_bits + 256 : 0;
+        auto kind = [&](const Held& pool) { return rows16 ? t : codes || (pool.t && pool.t->scalar_type() == at::kByte) ? at::kByte : t; };
+        int64_t streams = 0;
+        for (int64_t h = 0; k_stream.t && h < hkv; ++h) streams += desc->kv_head_is_streaming[h] != 0;
+        const int64_t pool = kv.num_pages * (kv.pool_heads ? kv.pool_heads : hkv) * slab, bounded = kv.num_pages_stream * streams * slab;
         check(where, {{q, t, total * hq * dim}, {k, t, total * hkv * dim}, {v, t, total * hkv * dim}, {out, t, total * hq * dim}, {lse, kFloat, total * hq},
-                      {cu, kInt, batch + 1}, {held.lens, kInt, batch}, {held.table, kInt, 0},
-                      {held.pool, held.pool && held.pool->scalar_type() == at::kByte ? at::kByte : t, 0}, {mask, kLong, total * words},
+                      {cu, kInt, batch + 1}, {now.t, kInt, batch}, {table.t, kInt, 0}, {k_pool.t, kind(k_pool), pool}, {v_pool.t, kind(v_pool), pool},
+                      {k_stream.t, kind(k_stream), bounded}, {v_stream.t, kind(v_stream), bounded},
+                      {ring_table.t, kInt, k_stream.t ? batch * ring_of(desc) : 0}, {mask, kLong, total * words},
                       {pos, kInt, total}, {sel, kInt, batch * hkv * stride}, {count, kInt, batch * hkv}, {len, kInt, batch}});
         const void *p_q = address(q), *p_k = address(k), *p_v = address(v);
         const int32_t *p_cu = address<int32_t>(cu), longest = number32(a[6]), *p_pos = address<int32_t>(pos), *p_sel = address<int32_t>(sel),

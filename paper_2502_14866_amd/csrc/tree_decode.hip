@@ -325,6 +325,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
     // ---- the list: entries of history, then tiles of drafted tokens
     const int drafts = ceil_div(s.n, kTile);
     const bool ring = in_stream_pool(a.lp, a.kv, hk);
+    const int last_page = uniform((ring ? a.stream_pages : a.kv.num_pages) - 1);  // (one number of the walk: two and a choice there cost 6 % over 4-bit pages)
     const size_t head = (size_t)b * a.lp.Hkv + hk;
     // (the first `listed` entries are named by a list or a formula, the pages from first_new on follow; a list that holds fewer than it may
     // ends in entries of nothing, so that its length need not be waited for)
@@ -353,7 +354,7 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
             }
             if (p >= 0 && p < s.pages) {
                 const int phys = ring ? a.kv.ring_table[(size_t)b * a.kv.ring + ring_slot(a.lp, p)] : a.kv.page_table[(size_t)b * a.kv.max_pages + p];
-                w = make_int2(p, ring ? max(phys, 0) : min(max(phys, 0), a.kv.num_pages - 1));
+                w = make_int2(p, min(max(phys, 0), last_page));
             }
         }
         return w;
