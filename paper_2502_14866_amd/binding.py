@@ -246,7 +246,8 @@ class _CtypesCalls:
                  (kv.page_table, i32, 0), (kv.k_pool, kind, pool), (kv.v_pool, kind, pool), (kv.k_pool_stream, kind, bounded),
                  (kv.v_pool_stream, kind, bounded), (kv.ring_table, i32, batch * _ring(d) if kv.k_pool_stream is not None else 0),
                  (tree_mask, torch.int64, total * words), (positions, i32, total),
-                 (sel_pages, i32, batch * hkv * stride), (sel_count, i32, batch * hkv), (sel_seq_len, i32, batch))
+                 (sel_pages, i32, batch * hkv * stride), (sel_count, i32, batch * hkv), (sel_seq_len, i32, batch),
+                 (workspace, () if workspace is None else workspace.dtype, 0))
         return load_library().lserve_sparse_decode_tree(
             d, kv.c(), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(cu_new), _ptr(tree_mask), words, _ptr(positions), _ptr(sel_pages),
             _ptr(sel_count), _ptr(sel_seq_len), stride, total, max_new_per_seq, _ptr(out), _ptr(lse_out), _ptr(workspace),

@@ -292,7 +292,7 @@ PyObject* py_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
                       {cu, kInt, batch + 1}, {now.t, kInt, batch}, {table.t, kInt, 0}, {k_pool.t, kind(k_pool), pool}, {v_pool.t, kind(v_pool), pool},
                       {k_stream.t, kind(k_stream), bounded}, {v_stream.t, kind(v_stream), bounded},
                       {ring_table.t, kInt, k_stream.t ? batch * ring_of(desc) : 0}, {mask, kLong, total * words},
-                      {pos, kInt, total}, {sel, kInt, batch * hkv * stride}, {count, kInt, batch * hkv}, {len, kInt, batch}});
+                      {pos, kInt, total}, {sel, kInt, batch * hkv * stride}, {count, kInt, batch * hkv}, {len, kInt, batch}, {ws, ws ? ws->scalar_type() : t, 0}});
         const void *p_q = address(q), *p_k = address(k), *p_v = address(v);
         const int32_t *p_cu = address<int32_t>(cu), longest = number32(a[6]), *p_pos = address<int32_t>(pos), *p_sel = address<int32_t>(sel),
                       *p_count = address<int32_t>(count), *p_len = address<int32_t>(len);

@@ -46,3 +46,28 @@ def test_which_calls_refuse_what(monkeypatch, route, name, wrong, refusing):
                 refused.add(i)
             assert len(seen) == before + (i not in refused)
     assert refused == refusing
+
+
+@pytest.mark.parametrize("route", ["native", "ctypes"])
+@pytest.mark.parametrize("name,refusing", [("ws", {TREE}), ("ring", {EXTEND, EXTEND_NO_SLOTS, TREE, TREE_ALL}), ("vs", {TREE, TREE_ALL}),
+                                           ("freq", {ROTARY, ROTARY_KEYS}), ("parents", {MASKS}), ("free", {EXTEND})])
+def test_tensors_on_another_device(monkeypatch, route, name, refusing):
+    t, refused = _tensors(), set()
+    if name == "freq":  # (its address is taken when the description is made)
+        calls = _calls(t)
+        _rotary_of(calls[ROTARY]).inv_freq = t[name].to("meta")
+    else:
+        calls = _calls({**t, name: t[name].to("meta")})
+    with _stand_in(monkeypatch, route) as seen:
+        for i, call in enumerate(calls):
+            before = len(seen)
+            try:
+                call()
+            except ValueError:
+                refused.add(i)
+            assert len(seen) == before + (i not in refused)
+    assert refused == refusing
+
+
+def _rotary_of(call):
+    return next(c.cell_contents for c in call.__closure__ if type(c.cell_contents).__name__ == "RotaryDesc")
