@@ -434,7 +434,8 @@ int lserve_sparse_decode_noalloc(const lserve_attn_desc *desc, const lserve_page
  *                  their table entries become -1
  *   total_new      host: new tokens of the batch or more (the call works on this many; with fewer the rest is left undone)
  *   cu_new         device [batch + 1] out: running sum of n_b, as lserve_append_kv takes it (with start_pos = kv->seq_lens)
- *   new_seq_lens   device [batch] out: S_b + n_b; outputs overlap neither kv->seq_lens, new_lens, free_pages nor each other
+ *   new_seq_lens   device [batch] out: S_b + n_b; outputs, the page table among them, overlap neither kv->seq_lens, new_lens, free_pages,
+ *                  ring_table nor each other
  *   pages_taken    device [1] out: pages the batch needs; more than num_free: the list was too short, and -1 is what
  *                  table entries and slots without a page hold: not to be handed to the other calls
  *   positions      device [total_new] out or NULL: position of every new token in its sequence

@@ -39,6 +39,16 @@ void* g_scratch_ptr[kMaxDevices] = {};  // device address of `scratch`, per devi
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// An array of a call, if it is given.
+struct Range {
+    const void* at;
+    long long bytes;
+};
+bool meet(const Range& a, const Range& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return a.at && b.at && a.bytes > 0 && b.bytes > 0 && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+
 int fail_hip(hipError_t e) {
     g_last_hip_error = (int)e;
     return LSERVE_ERR_HIP;
@@ -467,18 +477,17 @@ int lserve_extend_tables(const lserve_attn_desc* desc, const lserve_paged_kv* kv
     if (!new_lens || num_free < 0 || (num_free > 0 && !free_pages) || total_new < 0 || !cu_new || !new_seq_lens || !pages_taken)
         return LSERVE_ERR_INVALID_ARG;
     if (ring_slots && !kv->ring_table) return LSERVE_ERR_INVALID_ARG;
-    // what one workgroup writes others still read the lengths and the free list for
-    auto meet = [](const int32_t* a, long long n, const int32_t* b, long long m) { return a < b + m && b < a + n; };
-    const struct {
-        const int32_t* at;
-        long long n;
-    } in[] = {{kv->seq_lens, kv->batch}, {new_lens, kv->batch}, {free_pages, num_free}},
-      out[] = {{cu_new, kv->batch + 1LL}, {new_seq_lens, kv->batch}, {pages_taken, 1}};
-    for (const auto& o : out) {
-        for (const auto& i : in)
-            if (meet(o.at, o.n, i.at, i.n)) return LSERVE_ERR_INVALID_ARG;
-        for (const auto& other : out)
-            if (&other != &o && meet(o.at, o.n, other.at, other.n)) return LSERVE_ERR_INVALID_ARG;
+    // what one workgroup writes others still read the lengths, the free list and the tables for
+    const long long batch = kv->batch, total = total_new;
+    const Range in[] = {{kv->seq_lens, batch * 4}, {new_lens, batch * 4}, {free_pages, num_free * 4LL},
+                        {ring_slots ? kv->ring_table : nullptr, batch * (lp.sink_pages + lp.local_pages) * 4}};
+    const Range out[] = {{cu_new, (batch + 1) * 4}, {new_seq_lens, batch * 4}, {pages_taken, 4}, {kv->page_table, batch * kv->max_pages_per_seq * 4},
+                         {positions, total * 4}, {slots, total * 8}, {ring_slots, total * 8}};
+    for (const Range& o : out) {
+        for (const Range& i : in)
+            if (meet(o, i)) return LSERVE_ERR_INVALID_ARG;
+        for (const Range& other : out)
+            if (&other != &o && meet(o, other)) return LSERVE_ERR_INVALID_ARG;
     }
     if (!aligned16(kv->page_table) || !aligned16(kv->seq_lens) || !aligned16(kv->ring_table) || !aligned16(new_lens) ||
         (reinterpret_cast<uintptr_t>(free_pages) & 3u) != 0 || !aligned16(cu_new) || !aligned16(new_seq_lens) || !aligned16(pages_taken) || !aligned16(positions) ||
