@@ -530,7 +530,8 @@ int lserve_tree_masks(const int32_t *parents, const int32_t *cu_new, const int32
  *                   [total_new]; both or neither
  *   sel_pages, sel_count, sel_seq_len, sel_stride: as in lserve_sparse_decode (every entry counts, in any order; pages behind the history are
  *                   passed over), or all three NULL (sel_stride is then 0)
- *   out             device [total_new][H][D]; lse_out device [total_new][H] fp32 or NULL
+ *   out             device [total_new][H][D]; lse_out device [total_new][H] fp32 or NULL; neither these nor the workspace overlap each
+ *                   other or what the call reads
  *   workspace       device, lserve_tree_workspace_bytes(...) for these sizes or more, any contents; calls that may run at the same time
  *                   need one each
  */

@@ -615,6 +615,19 @@ int lserve_sparse_decode_tree(const lserve_attn_desc* desc, const lserve_paged_k
     if (max_new_per_seq > kMaxTreeNodes) return LSERVE_ERR_UNSUPPORTED;
     const size_t need = tree_workspace_bytes(a.lp, a.kv.batch, total_new, max_new_per_seq, a.kv.max_pages, sel_stride);
     if (need > 0 && (!workspace || workspace_bytes < need)) return LSERVE_ERR_WORKSPACE;
+    // what one workgroup writes others still read their rows, keys and lists for
+    const long long batch = a.kv.batch, total = total_new, row = 2LL * kHeadDim, lists = batch * a.lp.Hkv * 4;
+    const Range in[] = {{q, total * a.lp.H * row}, {k_new, total * a.lp.Hkv * row}, {v_new, total * a.lp.Hkv * row}, {cu_new, (batch + 1) * 4},
+                        {tree_mask, total * mask_words * 8}, {positions, total * 4}, {sel_pages, lists * sel_stride}, {sel_count, lists},
+                        {sel_seq_len, batch * 4}, {kv->seq_lens, batch * 4}, {kv->page_table, batch * a.kv.max_pages * 4},
+                        {a.kv.k_stream ? kv->ring_table : nullptr, batch * a.kv.ring * 4}};
+    const Range written[] = {{out, total * a.lp.H * row}, {lse_out, total * a.lp.H * 4}, {workspace, (long long)need}};
+    for (const Range& o : written) {
+        for (const Range& i : in)
+            if (meet(o, i)) return LSERVE_ERR_INVALID_ARG;
+        for (const Range& other : written)
+            if (&other != &o && meet(o, other)) return LSERVE_ERR_INVALID_ARG;
+    }
     a.q = (const uint16_t*)q;
     a.k_new = (const uint16_t*)k_new;
     a.v_new = (const uint16_t*)v_new;
