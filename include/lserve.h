@@ -502,7 +502,8 @@ int lserve_rotary_frequencies(const lserve_rotary_scaling *scaling, double *inv_
  *   mask_words       64-bit words of a row of tree_mask, max_new_per_seq / 64 rounded up or more
  *   tree_mask        device [total_new][mask_words] out: bit i % 64 of word i / 64 of row cu_new[b] + j is set iff i is j or an
  *                    ancestor of j
- *   positions        device [total_new] out: S_b plus the number of ancestors of j
+ *   positions        device [total_new] out: S_b plus the number of ancestors of j; may be `parents` itself.  Outputs overlap neither
+ *                    each other nor what the call reads otherwise
  * Rows from cu_new[batch] on are left alone.  No workspace.
  */
 int lserve_tree_masks(const int32_t *parents, const int32_t *cu_new, const int32_t *seq_lens, int32_t batch, int32_t total_new,

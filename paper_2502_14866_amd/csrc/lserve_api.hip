@@ -588,6 +588,12 @@ int lserve_tree_masks(const int32_t* parents, const int32_t* cu_new, const int32
     if (batch > 65535 || max_new_per_seq > kMaxTreeNodes) return LSERVE_ERR_UNSUPPORTED;
     if (!aligned16(parents) || !aligned16(cu_new) || !aligned16(seq_lens) || !aligned16(tree_mask) || !aligned16(positions))
         return LSERVE_ERR_INVALID_ARG;
+    // (positions may take the parents' place: a workgroup has read all of its own before it writes any)
+    const Range in[] = {{positions == parents ? nullptr : parents, total_new * 4LL}, {cu_new, (batch + 1LL) * 4}, {seq_lens, batch * 4LL}};
+    const Range mask = {tree_mask, (long long)total_new * mask_words * 8}, at = {positions, total_new * 4LL};
+    for (const Range& i : in)
+        if (meet(mask, i) || meet(at, i)) return LSERVE_ERR_INVALID_ARG;
+    if (meet(mask, at)) return LSERVE_ERR_INVALID_ARG;
     const hipError_t e = launch_tree_masks(parents, cu_new, seq_lens, batch, total_new, max_new_per_seq, mask_words,
                                            (unsigned long long*)tree_mask, positions, (hipStream_t)stream);
     return e == hipSuccess ? LSERVE_OK : fail_hip(e);
