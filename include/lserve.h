@@ -467,8 +467,8 @@ typedef struct lserve_rotary_desc {
  *   q_stride     elements between the rows of two tokens: a multiple of 8, at least H * D (k_stride: Hkv * D); rows cut
  *                out of those of a fused projection are fine
  *   positions    device [total]; a token with a negative position is left out: its rows are not written
- *   q_out, k_out device [total][H][D], [total][Hkv][D]; may be q / k themselves where these are dense, and must
- *                not overlap them otherwise
+ *   q_out, k_out device [total][H][D], [total][Hkv][D]; q_out may be q itself and k_out k where these are dense; outputs that
+ *                overlap what is read otherwise, or each other, are refused
  * desc: num_q_heads, num_kv_heads, head_dim and dtype.  No workspace.
  */
 int lserve_rotary(const lserve_attn_desc *desc, const lserve_rotary_desc *rotary, const void *q, const void *k,

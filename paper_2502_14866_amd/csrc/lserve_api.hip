@@ -49,6 +49,19 @@ bool meet(const Range& a, const Range& b) {
     return a.at && b.at && a.bytes > 0 && b.bytes > 0 && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
 }
 
+// Rows of a call, `apart` bytes from one to the next.
+struct Rows {
+    const void* at;
+    long long bytes, apart, count;
+};
+bool meet(const Range& a, const Rows& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    if (!meet(a, Range{b.at, (b.count - 1) * b.apart + b.bytes})) return false;
+    // the first row that does not end in front of the array
+    const uintptr_t first = x < y + (uintptr_t)b.bytes ? 0 : (x - y - (uintptr_t)b.bytes) / (uintptr_t)b.apart + 1;
+    return first < (uintptr_t)b.count && y + first * (uintptr_t)b.apart < x + (uintptr_t)a.bytes;
+}
+
 int fail_hip(hipError_t e) {
     g_last_hip_error = (int)e;
     return LSERVE_ERR_HIP;
@@ -531,6 +544,13 @@ int lserve_rotary(const lserve_attn_desc* desc, const lserve_rotary_desc* rotary
     if (k && (k_stride < k_row || k_stride % 8 != 0 || (k_out == k && k_stride != k_row))) return LSERVE_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(positions) || !aligned16(rotary->inv_freq))
         return LSERVE_ERR_INVALID_ARG;
+    // (outputs are whole, inputs rows that may lie apart; in place a row is read before it is written)
+    const Rows q_in = {q, q_row * 2, q_stride * 2, total}, k_in = {k, k_row * 2, k_stride * 2, total};
+    const Range q_to = {q_out, total * q_row * 2}, k_to = {k_out, total * k_row * 2}, at = {positions, total * 4LL},
+                freq = {rotary->inv_freq, rotary->rotary_dim * 4LL};
+    for (const Range& o : {q_to, k_to})
+        if (meet(o, at) || meet(o, freq) || (o.at != q && meet(o, q_in)) || (o.at != k && meet(o, k_in))) return LSERVE_ERR_INVALID_ARG;
+    if (meet(q_to, k_to) || (q_out && q_out == k) || (k_out && k_out == q)) return LSERVE_ERR_INVALID_ARG;
     RotaryArgs a = {};
     a.q = q;
     a.k = k;
