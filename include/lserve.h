@@ -533,7 +533,7 @@ int lserve_tree_masks(const int32_t *parents, const int32_t *cu_new, const int32
  *                   passed over), or all three NULL (sel_stride is then 0)
  *   out             device [total_new][H][D]; lse_out device [total_new][H] fp32 or NULL; neither these nor the workspace overlap each
  *                   other or what the call reads
- *   workspace       device, lserve_tree_workspace_bytes(...) for these sizes or more, any contents; calls that may run at the same time
+ *   workspace       device, lserve_tree_workspace_bytes(...) of just these sizes, or more bytes; any contents; calls that may run at the same time
  *                   need one each
  */
 int lserve_sparse_decode_tree(const lserve_attn_desc *desc, const lserve_paged_kv *kv, const void *q, const void *k_new,
@@ -542,7 +542,10 @@ int lserve_sparse_decode_tree(const lserve_attn_desc *desc, const lserve_paged_k
                               const int32_t *sel_seq_len, int32_t sel_stride, int32_t total_new, int32_t max_new_per_seq, void *out,
                               float *lse_out, void *workspace, size_t workspace_bytes, void *stream);
 
-/* Workspace of lserve_sparse_decode_tree (0 on invalid arguments, or where none is needed). */
+/* Workspace of lserve_sparse_decode_tree for a call of just these sizes (0 on invalid arguments, or where none is needed).  Smaller calls may need
+ * more: with so many lists that none is cut it is 0 (512 sequences of 8 KV heads and a token each; 511 want 146 MiB).  A workspace that is
+ * kept for calls of many sizes is the largest over them; LSERVE_TREE_WORKSPACE_MOST is enough for all. */
+#define LSERVE_TREE_WORKSPACE_MOST (352u << 20)
 size_t lserve_tree_workspace_bytes(const lserve_attn_desc *desc, int32_t batch, int32_t total_new, int32_t max_new_per_seq,
                                    int32_t max_pages_per_seq, int32_t sel_stride);
 

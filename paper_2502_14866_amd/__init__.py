@@ -10,6 +10,7 @@ from .binding import (  # noqa: F401
     LSERVE_CALL_SELECT_PAGES,
     LSERVE_CALL_SPARSE_DECODE,
     LSERVE_CALL_SPARSE_PREFILL,
+    LSERVE_TREE_WORKSPACE_MOST,
     AttnDesc,
     LserveError,
     PagedKV,

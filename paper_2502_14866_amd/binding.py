@@ -21,6 +21,7 @@ LSERVE_CALL_BUILD_PAGE_STATS = 0
 LSERVE_CALL_SELECT_PAGES = 1
 LSERVE_CALL_SPARSE_PREFILL = 2
 LSERVE_CALL_SPARSE_DECODE = 3
+LSERVE_TREE_WORKSPACE_MOST = 352 << 20
 
 EXPORTED_SYMBOLS = (
     "lserve_build_page_stats",
@@ -714,6 +715,8 @@ def lserve_tree_masks(parents: torch.Tensor, cu_new: torch.Tensor, seq_lens: tor
 
 def lserve_tree_workspace_bytes(desc: AttnDesc, batch: int, total_new: int, max_new_per_seq: int, max_pages_per_seq: int,
                                 sel_stride: int = 0) -> int:
+    """For a call of just these sizes; smaller ones may need more (a workspace kept for many: the largest over them, or
+    LSERVE_TREE_WORKSPACE_MOST)."""
     return int(load_library().lserve_tree_workspace_bytes(desc.c(), batch, total_new, max_new_per_seq, max_pages_per_seq, sel_stride))
 
 
