@@ -646,6 +646,8 @@ def lserve_extend_tables(desc: AttnDesc, kv: PagedKV, new_lens: torch.Tensor, fr
         if given is None:
             raise ValueError("lserve_extend_tables: total_new, where no positions or slots are asked for")
         total_new = given.numel()
+    if total_new >= 2 ** 31:
+        raise ValueError(f"lserve_extend_tables: {total_new} new tokens, more than 32 bits count")
     _check((_calls or _native()).extend(desc._address, kv, new_lens, free_pages, cu_new, new_seq_lens, pages_taken, positions, slots,
                                         ring_slots, total_new, _stream(stream)), "lserve_extend_tables")
 

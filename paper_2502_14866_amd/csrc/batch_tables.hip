@@ -31,7 +31,7 @@ __global__ __launch_bounds__(kTableThreads) void extend_tables_kernel(ExtendArgs
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const int page = 1 << a.page_log2;
     const bool first_one = blockIdx.x == 0;
-    const int t0 = (int)blockIdx.x * kTableTokens, t1 = min(t0 + kTableTokens, a.total);
+    const int t0 = (int)blockIdx.x * kTableTokens, t1 = t0 + min(kTableTokens, a.total - t0);  // (in differences: the last tokens are next to 2^31)
     auto pages_of = [&](unsigned tokens) { return (int)min((tokens + page - 1) >> a.page_log2, (unsigned)a.max_pages); };
 #pragma unroll
     for (int i = 0; i < kTokensPerThread; ++i) owner[i * kTableThreads + tid] = -1;
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kTableThreads) void extend_tables_kernel(ExtendArgs
         }
     }
     const int t = t0 + tid * kTokensPerThread;
-    if (t + kTokensPerThread <= t1) {  // 16-byte stores: `t` is a multiple of four
+    if (t1 - t >= kTokensPerThread) {  // 16-byte stores: `t` is a multiple of four
         if (a.positions) *reinterpret_cast<int4*>(a.positions + t) = make_int4(position[0], position[1], position[2], position[3]);
 #pragma unroll
         for (int i = 0; i < kTokensPerThread; i += 2) {

@@ -41,3 +41,10 @@ def test_arrays_of_nothing_lie_anywhere():
         L.lserve_extend_tables(L.AttnDesc(4, 2, [1, 0]), kv, room[8:16], None, room[16:28], room[28:36], room[36:37], room[4:4], room[8:8].view(torch.int64),
                                total_new=0, stream=0)
     assert e.value.code == -4
+
+
+def test_more_tokens_than_a_count_holds():
+    kv = L.PagedKV(None, None, None, torch.zeros((8, 4), dtype=torch.int32), torch.zeros(8, dtype=torch.int32))
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError):
+        L.lserve_extend_tables(L.AttnDesc(4, 2, [1, 0]), kv, i32(8), None, i32(9), i32(8), i32(1), total_new=2 ** 32 + 1, stream=0)
