@@ -436,8 +436,10 @@ int lserve_sparse_decode_noalloc(const lserve_attn_desc *desc, const lserve_page
  *   cu_new         device [batch + 1] out: running sum of n_b, as lserve_append_kv takes it (with start_pos = kv->seq_lens)
  *   new_seq_lens   device [batch] out: S_b + n_b; outputs, the page table among them, overlap neither kv->seq_lens, new_lens, free_pages,
  *                  ring_table nor each other
- *   pages_taken    device [1] out: pages the batch needs; more than num_free: the list was too short, and -1 is what
- *                  table entries and slots without a page hold: not to be handed to the other calls
+ *   pages_taken    device [1] out: pages the batch needs, as far as the rows of the table go; more than num_free: the list was too
+ *                  short, and -1 is what table entries and slots without a page hold: not to be handed to the other calls.  A
+ *                  sequence that outgrows its row does not show here, but in new_seq_lens[b] > max_pages_per_seq * N_P (and in
+ *                  slots of -1)
  *   positions      device [total_new] out or NULL: position of every new token in its sequence
  *   slots          device [total_new] out or NULL: page * N_P + position % N_P; -1 without a page
  *   ring_slots     device [total_new] out or NULL: the same in the streaming heads' ring (ring_table), -1 for tokens whose page is
@@ -520,7 +522,9 @@ int lserve_tree_masks(const int32_t *parents, const int32_t *cu_new, const int32
  *   drafted tokens: those whose bit in row j of tree_mask is set (lserve_tree_masks sets its own and its ancestors'); of a
  *                   streaming head only those with tile(t_i) < s or tile(t_i) > tile(t_j) - w.
  * tree_mask = positions = NULL: a chain, token j at position S_b + j after token j - 1.  A token that attends nothing gets out = 0 and
- * lse = -inf.  What a token does not attend, be it not a number, leaves no trace in its result.
+ * lse = -inf.  What a token does not attend, be it not a number, leaves no trace in its result.  Scores, maxima and sums are fp32; unlike
+ * those of a decode step, weights are rounded for their product with the values, to the layer's type (fp16 over quantised pages): half a
+ * step of the type relative to each weight.
  *
  *   kv              N_P = 64; one pool or the two-way cache, pages of 16-bit rows or quantised (kv_bits 8 or 4: keys and values are
  *                   code * scale + zero, not rounded).  stats are not used

@@ -118,6 +118,8 @@ class DecodeSession:
                     lse_out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of drafted tokens behind the current lengths, whose K/V are in no page yet: over the pages of the last selection and
         what was appended since, or over every page before the first one.  Those that are accepted are appended afterwards.
+        This is no step of the reuse interval and selects nothing: a loop of drafted tokens alone calls `select` itself, when as many
+        tokens were accepted as it wants to share a selection, or the pages made since the last one go on growing.
 
         The output and the workspace are new tensors each time, so that a captured call keeps its own."""
         if self.steps_since_selection is None:
