@@ -14,11 +14,12 @@
 // workgroup works out the cut from the lengths of the batch (TreePlan).  Pieces leave (maximum, sum, outputs) in the workspace and
 // fold_trees_kernel puts them together in order.
 //
-// Measured, both kernels (a copy of 1 GiB runs at 5.1 TB/s, a product of 8192^3 at 1216 TFLOP/s): five tokens each on 4 x 256k, 2.15 GB, 370 us = 5.8
-// TB/s; 32 sequences of 4k .. 60k under 32 KV heads, 695 MB, 135 us = 5.1 TB/s; sixteen each on 16 x 32k, 4096 selected, 158 MB, 40 us, of which 6.6 are
-// the second kernel and some 8 the start (lengths, cut, page table, first tiles); one conversation of 4000 tokens 14.6 us, nothing but such
-// latencies; twenty to 64 each on 64 x 16k in 4-bit pages 210 us = 440 TFLOP/s: there the vector instructions (46 % of a SIMD's cycles: unpacking, exponentials,
-// packing) and the matrix ones (25 %) of two wavefronts to a SIMD add up with the barriers between; 64 x 8k under 512 rows of 16-bit pages 620.
+// Measured, calls back to back, both kernels and what is between them (a copy of 1 GiB runs at 5.1 TB/s, a product of 8192^3 at 1216 TFLOP/s): five tokens
+// each on 4 x 256k, 2.15 GB, 365 .. 381 us = 5.6 .. 5.9 TB/s; 32 sequences of 4k .. 60k under 32 KV heads, 695 MB, 133 .. 140 us = 5.0 .. 5.2 TB/s; sixteen
+// each on 16 x 32k, 4096 selected, 158 MB, 47 .. 49 us, of which 6.7 are the second kernel and some 8 the start (lengths, cut, page table, first tiles);
+// one conversation of 4000 tokens 14.8 us, nothing but such latencies; twenty to 64 each on 64 x 16k in 4-bit pages 209 .. 213 us = 435 .. 445 TFLOP/s: there
+// the vector instructions (50 % of a SIMD's cycles: unpacking, exponentials, packing) and the matrix ones (24 %) of two wavefronts to a SIMD add up with
+// the barriers between; the same in 8-bit pages 215 .. 231.
 #include <algorithm>
 
 #include "kernels.h"
@@ -639,8 +640,8 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
         }
         const unsigned char *ks = k_lds[stage], *vs = v_lds[stage];
         int k_at = k_place;
-        // Where registers are short the eight places of a step are worked out in the step (64 x 16k tokens of 8 bits, 30 drafted: 204 us with the places
-        // kept and 33 other registers in scratch, 177 us with 25).
+        // Where registers are short the eight places of a step are worked out in the step (64 x 16k tokens of 8 bits, 30 drafted: 191 us with the places
+        // kept and 35 other registers in scratch, 186 us with 28; of 4 bits under 32 rows each the same).
         if constexpr (QUANT && RG == 4) asm volatile("" : "+v"(k_at));
         // (one block of keys: two chains of products, which do not wait for each other, instead of one)
         constexpr int kChains = 2 / NB;
@@ -730,7 +731,9 @@ __global__ __launch_bounds__(tree_waves(RG) * kWave, (RG == 1 ? 1 : 2)) void dra
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 p[i] = __builtin_amdgcn_exp2f(sc[kb][i]);
-                sum[i % 2] += p[i];  // unrounded; the second product takes them in the layer's type, which is what its operands are
+                // unrounded; the second product takes them in the layer's type, which is what its operands are (a decode step, whose second product is
+                // not the matrix cores', keeps fp32 there: errors against 64 bits 2.8e-4 here, 2.1e-4 with fp32 weights; bf16 2.3e-3 and 1.7e-3)
+                sum[i % 2] += p[i];
             }
             if constexpr (codes) {
 #pragma unroll
@@ -1047,7 +1050,14 @@ TreeSizes tree_sizes(const LayerParams& lp, int batch, int total_new, int max_ne
     const int drafts = ceil_div(max_new, kTile), dense = sel_stride > 0 ? std::min(max_pages, sel_stride + 1) : max_pages;
     const int stream = std::min(max_pages, lp.sink_pages + lp.local_pages);
     const long long shortest = tiles * ((lp.Hkv - z.streams) * (long long)(dense + drafts) + z.streams * (long long)(stream + drafts)) / kLeastPiece;
+    // So many lists that all stay whole: to find its piece a workgroup runs over the batch, 64 sequences at a time.  Whole and cut, trees of 4 on 8 KV heads: 600
+    // x 100 .. 2000 tokens 428 and 429 us, 600 x 2000 716 and 629, 1200 x 50 .. 700 400 and 647, 4000 x 50 .. 300 800 and 3800; below the border 300 x 2000 361 and
+    // 322, 150 x 2000 207 and 165.  What whole lists cost is a sequence far longer than the others, which a workgroup to a head walks alone: one of 100000
+    // among 600 of 100 .. 2000 1930 and 447.
     z.target = lists >= 8LL * resident || std::max(dense, stream) + drafts <= kLeastPiece ? 0 : (int)std::min<long long>(shortest, resident);
+    // Few lists are cut until the pieces all run at once, more are not searched for that (see make_plan).  Searched and not: 16 x 2000 .. 40000 tokens under 8
+    // heads 149 and 153 us, 32 x 2000 .. 40000 239 and 239, 16 x 4096 selected 47.6 and 46.2; past the border 64 x 2000 .. 20000, as many lists as
+    // pieces, 434 and 291, 9 x 1000 .. 20000 under 32 heads 128 and 122.  One KV head and 200 sequences, loaded anew in every round of the search, 231 and 225.
     z.exact = z.target > 0 && 2 * lists <= z.target;
     z.grid = z.target == 0 ? (long long)batch * lp.Hkv * z.row_tiles : z.target + lists;
     const long long cycle = 8LL * z.row_tiles;  // see the kernel
