@@ -241,7 +241,8 @@ class _CtypesCalls:
         kind, slab = _slab(d, kv.kv_bits)
         streams = sum(d.kv_head_is_streaming[:hkv]) if kv.k_pool_stream is not None else 0
         kv.c()
-        pool, bounded = kv._c.num_pages * (kv.pool_heads or hkv) * slab, kv._c.num_pages_stream * streams * slab
+        # (a layer whose heads are all in the bounded pool reads nothing of the main one)
+        pool, bounded = kv._c.num_pages * (kv.pool_heads or hkv) * slab if streams < hkv else 0, kv._c.num_pages_stream * streams * slab
         _checked("lserve_sparse_decode_tree", (q, dt, total * hq * dim), (k_new, dt, total * hkv * dim), (v_new, dt, total * hkv * dim),
                  (out, dt, total * hq * dim), (lse_out, torch.float32, total * hq), (cu_new, i32, batch + 1), (kv.seq_lens, i32, batch),
                  (kv.page_table, i32, 0), (kv.k_pool, kind, pool), (kv.v_pool, kind, pool), (kv.k_pool_stream, kind, bounded),

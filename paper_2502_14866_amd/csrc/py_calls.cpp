@@ -287,7 +287,8 @@ PyObject* py_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
         auto kind = [&](const Held& pool) { return rows16 ? t : codes || (pool.t && pool.t->scalar_type() == at::kByte) ? at::kByte : t; };
         int64_t streams = 0;
         for (int64_t h = 0; k_stream.t && h < hkv; ++h) streams += desc->kv_head_is_streaming[h] != 0;
-        const int64_t pool = kv.num_pages * (kv.pool_heads ? kv.pool_heads : hkv) * slab, bounded = kv.num_pages_stream * streams * slab;
+        // (a layer whose heads are all in the bounded pool reads nothing of the main one)
+        const int64_t pool = streams < hkv ? kv.num_pages * (kv.pool_heads ? kv.pool_heads : hkv) * slab : 0, bounded = kv.num_pages_stream * streams * slab;
         check(where, {{q, t, total * hq * dim}, {k, t, total * hkv * dim}, {v, t, total * hkv * dim}, {out, t, total * hq * dim}, {lse, kFloat, total * hq},
                       {cu, kInt, batch + 1}, {now.t, kInt, batch}, {table.t, kInt, 0}, {k_pool.t, kind(k_pool), pool}, {v_pool.t, kind(v_pool), pool},
                       {k_stream.t, kind(k_stream), bounded}, {v_stream.t, kind(v_stream), bounded},

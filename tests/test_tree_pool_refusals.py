@@ -71,3 +71,22 @@ def test_tensors_on_another_device(monkeypatch, route, name, refusing):
 
 def _rotary_of(call):
     return next(c.cell_contents for c in call.__closure__ if type(c.cell_contents).__name__ == "RotaryDesc")
+
+
+@pytest.mark.parametrize("route", ["native", "ctypes"])
+def test_a_main_pool_that_nobody_reads(monkeypatch, route):
+    """Where all heads are in the bounded pool the main one may be anything of the right type."""
+    import paper_2502_14866_amd as L
+
+    t = _tensors()
+    desc = L.AttnDesc(4, 2, [1, 1])
+    for streams, ok in ((half(5, 2, 64, 128), True), (half(5, 1, 64, 128), False)):
+        kv = L.PagedKV(half(1, 1, 1, 128), half(1, 1, 1, 128), None, t["table"], t["lens"], k_pool_stream=streams, v_pool_stream=streams.clone(), ring_table=t["ring"])
+        with _stand_in(monkeypatch, route) as seen:
+            call = lambda: L.lserve_sparse_decode_tree(desc, kv, t["q"], t["kn"], t["vn"], t["cu"], 5, t["out"], None, stream=1)  # noqa: E731
+            if ok:
+                call()
+            else:
+                with pytest.raises(ValueError):
+                    call()
+        assert len(seen) == int(ok)
