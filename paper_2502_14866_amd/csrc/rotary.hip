@@ -10,20 +10,13 @@
 // products of 32 bits and one rounding follow.
 #include <algorithm>
 
-#include "kernels.h"
+#include "rotary.h"
 
 namespace lserve {
 
 namespace {
 
 constexpr int kRotaryThreads = 256, kRotaryWaves = kRotaryThreads / kWave;
-
-__device__ __forceinline__ float2 turn_of(int position, double radians, float scale) {
-    const double turns = (double)position * (radians * 0.15915494309189533577);
-    float s, c;
-    sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-    return make_float2(c * scale, s * scale);
-}
 
 // Row of head h of token t: queries first, then keys.
 struct HeadRow {
