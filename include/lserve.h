@@ -13,8 +13,9 @@
  * caller-supplied block mask (Sec. 3.1, Sec. 3.4), lserve_sparse_prefill_paged: chunked prefill whose keys
  * and values all come from the paged cache (Sec. 2.1), and lserve_sparse_prefill_chunk: chunked prefill over
  * the history in the cache with the chunk's own K / V alongside, before their write-back (Sec. 3.2).
- * In front of them: lserve_extend_tables (page table, positions and slots of new tokens), lserve_rotary (rotary
- * positions), and for drafted tokens lserve_tree_masks (who descends from whom) and lserve_sparse_decode_tree (their attention).
+ * In front of them: lserve_extend_tables (page table, positions and slots of new tokens), lserve_rotary, lserve_rotary_axes and
+ * lserve_norm_rotary (rotary positions, of one axis or several, with or without the norm of heads), lserve_rotary_append_kv (the same on the way
+ * into the pages), and for drafted tokens lserve_tree_masks (who descends from whom) and lserve_sparse_decode_tree (their attention).
  *
  * Conventions common to every call
  *   - "device" pointers are HIP device memory owned by the caller; "host" pointers are ordinary
@@ -494,6 +495,83 @@ typedef struct lserve_rotary_scaling {
 
 /* Host only: the R / 2 frequencies (HOST, out) and the factor on the result (HOST, out) of a scaling. */
 int lserve_rotary_frequencies(const lserve_rotary_scaling *scaling, double *inv_freq, float *scale);
+
+/*
+ * Positions with several axes (time, height and width of a film's patches, for instance): pair i of a head turns by the position of its token on
+ * axis pair_axis[i], t_axis f_i in place of t f_i.  Sections of pairs to an axis, axes in turn and anything else are lists of these numbers;
+ * frequencies that start again with every axis are the caller's inv_freq.
+ */
+typedef struct lserve_position_axes {
+    int32_t num_axes;         /* A: 1 .. 4 */
+    const uint8_t *pair_axis; /* HOST [R / 2]: axis of every pair, below A */
+} lserve_position_axes;
+
+/*
+ * lserve_rotary with positions of several axes; arguments as there but for
+ *   positions         device, of token t on axis a at positions[a * positions_stride + t]; a token whose position on axis 0 is negative is
+ *                     left out: its rows are not written.  On other axes a negative position turns backwards
+ *   positions_stride  at least total
+ */
+int lserve_rotary_axes(const lserve_attn_desc *desc, const lserve_rotary_desc *rotary, const lserve_position_axes *axes, const void *q,
+                       const void *k, const int32_t *positions, int64_t positions_stride, int32_t total, int64_t q_stride,
+                       int64_t k_stride, void *q_out, void *k_out, void *stream);
+
+/*
+ * Norm of every query and key head over its D channels: (x - m) / sqrt(mean((x - m)^2) + eps) * weight, m = 0 or the mean of x.  In fp32
+ * throughout: the squares of a row have to add up to less than 2^128.
+ */
+#define LSERVE_NORM_RMS 0     /* m = 0 */
+#define LSERVE_NORM_CENTRED 1 /* m = mean(x) */
+typedef struct lserve_head_norm {
+    int32_t kind;           /* LSERVE_NORM_* */
+    int32_t per_head;       /* 0: weights [D], the same for all heads; 1: [H][D] and [Hkv][D] */
+    float eps;              /* > 0 */
+    const float *q_weight;  /* device, 16-byte aligned, or NULL: ones */
+    const float *k_weight;
+} lserve_head_norm;
+
+/*
+ * Norm and rotary position of queries and keys in one pass: normed, then turned, both in fp32, and rounded once.  (Weights of ones and whole heads that
+ * turn with a factor of 1: the norm may as well come after the turn, which it commutes with for m = 0.)
+ *   norm       required
+ *   rotary     NULL: nothing turns (a layer without positions); positions may then be NULL too
+ *   axes       NULL: one axis, positions [total] as in lserve_rotary, positions_stride is not looked at
+ * Other arguments as in lserve_rotary and lserve_rotary_axes; in place as there.  Channels that do not turn are normed like the others.
+ */
+int lserve_norm_rotary(const lserve_attn_desc *desc, const lserve_head_norm *norm, const lserve_rotary_desc *rotary,
+                       const lserve_position_axes *axes, const void *q, const void *k, const int32_t *positions,
+                       int64_t positions_stride, int32_t total, int64_t q_stride, int64_t k_stride, void *q_out, void *k_out,
+                       void *stream);
+
+/*
+ * New tokens from a fused projection into the paged cache: queries are normed and turned into q_out; keys are normed, turned and, with the values, written to
+ * the pages as lserve_append_kv writes them, the statistics of the turned keys included.  The cache afterwards holds what
+ * lserve_append_kv would have written of the turned keys, rounded to the layer's type, and of the values (quantised pages: the codes of these rounded rows).
+ * n_b = cu_new[b+1] - cu_new[b] >= 0 tokens of sequence b go to positions start_pos[b] + j of its pages.
+ *
+ *   norm       NULL: none
+ *   rotary     NULL: nothing turns
+ *   axes       NULL: one axis
+ *   q          device, row of token t at q + t * q_stride elements, H heads of D; or NULL with q_out, where queries are somebody else's
+ *   k, v       device, likewise with Hkv heads; strides are multiples of 8 and at least a row; rows cut out of those of one projection are fine
+ *   positions  device [A][positions_stride] (axes NULL: [total_new]), or NULL: a token's position is start_pos[b] + j on every axis.  Any
+ *              numbers: where a token is written does not depend on them, and a negative one turns backwards
+ *   cu_new     device [batch + 1] (batch = kv->batch), cu_new[0] = 0; rows from cu_new[batch] on are left alone, here and in all outputs
+ *   start_pos  device [batch]; kv->seq_lens may be given.  kv->seq_lens itself is not read
+ *   total_new  host: rows of q, k and v, and of the outputs
+ *   max_new_per_seq  host bound of n_b, > 0; 1 (a decode step) has a form of its own
+ *   q_out      device [total_new][H][D]; may be q itself where its rows are dense
+ *   k_out, v_out  device [total_new][Hkv][D] or NULL: the turned keys, and the values, as dense rows too, for a prefill that reads them from there
+ *              (also tokens that the streaming heads' ring does not keep).  k_out may be k itself where its rows are dense
+ * Outputs, the pools and statistics among them, overlap neither each other nor anything read otherwise.  A chunk that attends its history in a ring
+ * first and is written back afterwards (lserve_sparse_prefill_chunk) takes lserve_norm_rotary and lserve_append_kv instead: this call
+ * overwrites ring pages that the chunk's first tokens attend.  No workspace.
+ */
+int lserve_rotary_append_kv(const lserve_attn_desc *desc, const lserve_paged_kv *kv, const lserve_head_norm *norm,
+                            const lserve_rotary_desc *rotary, const lserve_position_axes *axes, const void *q, const void *k,
+                            const void *v, int64_t q_stride, int64_t k_stride, int64_t v_stride, const int32_t *positions,
+                            int64_t positions_stride, const int32_t *cu_new, const int32_t *start_pos, int32_t total_new,
+                            int32_t max_new_per_seq, void *q_out, void *k_out, void *v_out, void *stream);
 
 /*
  * Ancestors of drafted tokens.  Sequence b has n_b = cu_new[b+1] - cu_new[b] of them, and parents[cu_new[b] + j] is the index (inside the

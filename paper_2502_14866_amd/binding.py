@@ -50,6 +50,11 @@ EXPORTED_SYMBOLS = (
     "lserve_rotary",
     "lserve_rotary_frequencies",
     "RotaryDesc",
+    "lserve_rotary_axes",
+    "PositionAxes",
+    "lserve_norm_rotary",
+    "HeadNorm",
+    "lserve_rotary_append_kv",
     "lserve_tree_masks",
     "lserve_sparse_decode_tree",
     "lserve_tree_workspace_bytes",
@@ -93,6 +98,15 @@ class _CBlockMask(ctypes.Structure):
 
 class _CRotaryDesc(ctypes.Structure):
     _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("inv_freq", ctypes.c_void_p), ("scale", ctypes.c_float)]
+
+
+class _CPositionAxes(ctypes.Structure):
+    _fields_ = [("num_axes", ctypes.c_int32), ("pair_axis", ctypes.POINTER(ctypes.c_uint8))]
+
+
+class _CHeadNorm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("per_head", ctypes.c_int32), ("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p)]
 
 
 class _CRotaryScaling(ctypes.Structure):
@@ -162,6 +176,13 @@ def load_library():
         lib.lserve_rotary.restype = ctypes.c_int
         lib.lserve_rotary_frequencies.argtypes = [ctypes.POINTER(_CRotaryScaling), vp, vp]
         lib.lserve_rotary_frequencies.restype = ctypes.c_int
+        rp, ap, np_ = ctypes.POINTER(_CRotaryDesc), ctypes.POINTER(_CPositionAxes), ctypes.POINTER(_CHeadNorm)
+        lib.lserve_rotary_axes.argtypes = [dp, rp, ap, vp, vp, vp, i64, i32, i64, i64, vp, vp, vp]
+        lib.lserve_rotary_axes.restype = ctypes.c_int
+        lib.lserve_norm_rotary.argtypes = [dp, np_, rp, ap, vp, vp, vp, i64, i32, i64, i64, vp, vp, vp]
+        lib.lserve_norm_rotary.restype = ctypes.c_int
+        lib.lserve_rotary_append_kv.argtypes = [dp, kp, np_, rp, ap, vp, vp, vp, i64, i64, i64, vp, i64, vp, vp, i32, i32, vp, vp, vp, vp]
+        lib.lserve_rotary_append_kv.restype = ctypes.c_int
         lib.lserve_tree_masks.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
         lib.lserve_tree_masks.restype = ctypes.c_int
         lib.lserve_sparse_decode_tree.argtypes = [dp, kp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
@@ -226,10 +247,50 @@ class _CtypesCalls:
     def rotary(desc, rotary, inv_freq, q, k, positions, q_out, k_out, stream):
         d, r = _CAttnDesc.from_address(desc), _CRotaryDesc.from_address(rotary)
         total, dim, hq, hkv, dt = (0 if positions is None else positions.numel()), d.head_dim, d.num_q_heads, d.num_kv_heads, _dtype(d)
-        (q_at, q_stride), (k_at, k_stride) = _rows(q, hq, dim, "q"), _rows(k, hkv, dim, "k")
+        (q_at, q_stride), (k_at, k_stride) = _rows("lserve_rotary", q, hq, dim, "q"), _rows("lserve_rotary", k, hkv, dim, "k")
         _checked("lserve_rotary", (positions, torch.int32, 1), (inv_freq, torch.float64, r.rotary_dim // 2 if r.rotary_dim <= dim else 0), (q, dt, total * hq * dim),
                  (q_out, dt, total * hq * dim), (k, dt, total * hkv * dim), (k_out, dt, total * hkv * dim))
         return load_library().lserve_rotary(d, r, q_at, k_at, _ptr(positions), total, q_stride, k_stride, _ptr(q_out), _ptr(k_out), stream)
+
+    @staticmethod
+    def turned(desc, norm, rotary, axes, q_weight, k_weight, inv_freq, q, k, positions, q_out, k_out, stream):
+        where = "lserve_norm_rotary" if norm else "lserve_rotary_axes"
+        d, dt = _CAttnDesc.from_address(desc), _dtype(_CAttnDesc.from_address(desc))
+        dim, hq, hkv = d.head_dim, d.num_q_heads, d.num_kv_heads
+        total = positions.shape[-1] if positions is not None and positions.dim() else q.shape[0] if q is not None else 0 if k is None else k.shape[0]
+        (q_at, q_stride), (k_at, k_stride) = _rows(where, q, hq, dim, "q"), _rows(where, k, hkv, dim, "k")
+        at, apart = _places(where, positions, axes, total)
+        _checked(where, *_turn_tensors(d, norm, rotary, q_weight, k_weight, inv_freq), (positions, torch.int32, 1), (q, dt, total * hq * dim),
+                 (q_out, dt, total * hq * dim), (k, dt, total * hkv * dim), (k_out, dt, total * hkv * dim))
+        lib, n, r, a = load_library(), _struct(_CHeadNorm, norm), _struct(_CRotaryDesc, rotary), _struct(_CPositionAxes, axes)
+        if norm:
+            return lib.lserve_norm_rotary(d, n, r, a, q_at, k_at, at, apart, total, q_stride, k_stride, _ptr(q_out), _ptr(k_out), stream)
+        return lib.lserve_rotary_axes(d, r, a, q_at, k_at, at, apart, total, q_stride, k_stride, _ptr(q_out), _ptr(k_out), stream)
+
+    @staticmethod
+    def rotary_append(desc, kv, norm, rotary, axes, q_weight, k_weight, inv_freq, q, k, v, positions, cu_new, start_pos, max_new_per_seq, q_out, k_out,
+                      v_out, stream):
+        where, d, i32 = "lserve_rotary_append_kv", _CAttnDesc.from_address(desc), torch.int32
+        dt, dim, hq, hkv, batch = _dtype(d), d.head_dim, d.num_q_heads, d.num_kv_heads, kv.page_table.shape[0]
+        total = 0 if k is None or not k.dim() else k.shape[0]
+        rows = [_rows(where, t, heads, dim, name) for t, heads, name in ((q, hq, "q"), (k, hkv, "k"), (v, hkv, "v"))]
+        at, apart = _places(where, positions, axes, total)
+        kind, slab = _slab(d, kv.kv_bits)
+        streaming = sum(1 for f in d.kv_head_is_streaming[:hkv] if f)
+        streams = streaming if kv.k_pool_stream is not None else 0
+        kv.c()
+        heads = kv._c.num_pages * (kv.pool_heads or hkv) if streams < hkv else 0  # (all heads in the bounded pool: nothing of the main one)
+        spans = heads * (d.page_size // d.logical_page_size if d.logical_page_size > 0 else 0) * 2 * dim if streaming < hkv else 0
+        pool, bounded = heads * slab, kv._c.num_pages_stream * streams * slab
+        _checked(where, *_turn_tensors(d, norm, rotary, q_weight, k_weight, inv_freq), (q, dt, total * hq * dim), (k, dt, total * hkv * dim),
+                 (v, dt, total * hkv * dim), (positions, i32, 1), (cu_new, i32, batch + 1), (start_pos, i32, batch), (q_out, dt, total * hq * dim),
+                 (k_out, dt, total * hkv * dim), (v_out, dt, total * hkv * dim), (kv.page_table, i32, 0), (kv.k_pool, kind, pool),
+                 (kv.v_pool, kind, pool), (kv.k_pool_stream, kind, bounded), (kv.v_pool_stream, kind, bounded), (kv.stats, dt, spans),
+                 (kv.ring_table, i32, batch * _ring(d) if kv.k_pool_stream is not None else 0))
+        return load_library().lserve_rotary_append_kv(
+            d, kv.c(), _struct(_CHeadNorm, norm), _struct(_CRotaryDesc, rotary), _struct(_CPositionAxes, axes), rows[0][0], rows[1][0], rows[2][0],
+            rows[0][1], rows[1][1], rows[2][1], at, apart, _ptr(cu_new), _ptr(start_pos), total, max_new_per_seq, _ptr(q_out), _ptr(k_out), _ptr(v_out),
+            stream)
 
     @staticmethod
     def tree(desc, kv, q, k_new, v_new, cu_new, max_new_per_seq, out, lse_out, tree_mask, positions, sel_pages, sel_count, sel_seq_len,
@@ -290,12 +351,38 @@ def _checked(where: str, *args) -> None:
         raise ValueError(f"{where}: tensors on {device} while device {torch.cuda.current_device()} is current")
 
 
-def _rows(t: Optional[torch.Tensor], heads: int, dim: int, what: str) -> tuple:
+def _struct(kind, address: int):
+    return kind.from_address(address) if address else None
+
+
+def _turn_tensors(d: "_CAttnDesc", norm: int, rotary: int, q_weight, k_weight, inv_freq) -> tuple:
+    """What describes how heads are normed and turned, for _checked."""
+    dim, per_head = d.head_dim, bool(norm) and _CHeadNorm.from_address(norm).per_head
+    turning = _CRotaryDesc.from_address(rotary).rotary_dim if rotary else 0
+    return ((q_weight, torch.float32, dim * d.num_q_heads if per_head else dim), (k_weight, torch.float32, dim * d.num_kv_heads if per_head else dim),
+            (inv_freq, torch.float64, turning // 2 if turning <= dim else 0))
+
+
+def _places(where: str, positions: Optional[torch.Tensor], axes: int, total: int) -> tuple:
+    """(address, elements between two axes) of positions [total], or with axes [axes][total], whose axes may lie apart."""
+    if positions is None:
+        return None, 0
+    if not axes:
+        if positions.dim() != 1 or positions.shape[0] < total:
+            raise ValueError(f"{where}: positions are [total] without axes")
+        return _ptr(positions), 0
+    n = _CPositionAxes.from_address(axes).num_axes
+    if positions.dim() != 2 or positions.shape[0] != n or positions.shape[1] < total or (positions.shape[1] > 1 and positions.stride(1) != 1):
+        raise ValueError(f"{where}: positions are [{n}][total], those of an axis next to each other")
+    return positions.data_ptr(), positions.stride(0) if n > 1 else positions.shape[1]
+
+
+def _rows(where: str, t: Optional[torch.Tensor], heads: int, dim: int, what: str) -> tuple:
     """(address, elements between two rows) of [total][heads][dim] whose rows may lie apart."""
     if t is None:
         return None, 0
     if t.dim() != 3 or t.shape[1:] != (heads, dim) or t.stride(2) != 1 or t.stride(1) != dim:
-        raise ValueError(f"lserve_rotary: {what} is [total][{heads}][{dim}], heads next to each other")
+        raise ValueError(f"{where}: {what} is [total][{heads}][{dim}], heads next to each other")
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim
 
 
@@ -315,6 +402,9 @@ def _native():
             if hasattr(lib, "lserve_extend_tables"):  # what stands in for the library may have the decode step's calls alone
                 calls.bind_new(*(ctypes.cast(f, ctypes.c_void_p).value
                                  for f in (lib.lserve_extend_tables, lib.lserve_tree_masks, lib.lserve_rotary, lib.lserve_sparse_decode_tree)))
+            if hasattr(lib, "lserve_rotary_append_kv"):
+                calls.bind_turned(*(ctypes.cast(f, ctypes.c_void_p).value
+                                    for f in (lib.lserve_rotary_axes, lib.lserve_norm_rotary, lib.lserve_rotary_append_kv)))
         except ImportError as e:
             warnings.warn(f"the binding's native calls are missing ({e}): decode steps are marshalled by ctypes; build them with "
                           "`python -m paper_2502_14866_amd.build` (or __graft_entry__.build())", RuntimeWarning, stacklevel=3)
@@ -708,6 +798,83 @@ def lserve_rotary(desc: AttnDesc, rotary: RotaryDesc, q: Optional[torch.Tensor],
     """q and k may be cut out of the rows of a fused projection (any distance between rows that is a multiple of eight elements)."""
     _check((_calls or _native()).rotary(desc._address, rotary._address, rotary.inv_freq, q, k, positions, q_out, k_out, _stream(stream)),
            "lserve_rotary")
+
+
+@dataclass
+class PositionAxes:
+    """Mirror of lserve_position_axes: the axis of each of a head's rotary_dim / 2 pairs (num_axes: as many as are named)."""
+    pair_axis: Sequence[int]
+    num_axes: int = 0
+
+    def __post_init__(self):
+        self.pair_axis = [int(a) for a in self.pair_axis]
+        if not self.pair_axis or min(self.pair_axis) < 0 or max(self.pair_axis) > 255:
+            raise ValueError("PositionAxes: an axis for every pair")
+        self.num_axes = self.num_axes or max(self.pair_axis) + 1
+        # (the library reads rotary_dim / 2 of them, 64 at most; what is not named here is no axis)
+        self._axes = (ctypes.c_uint8 * max(64, len(self.pair_axis)))(*([255] * 64))
+        self._axes[:len(self.pair_axis)] = self.pair_axis
+        self._c = _CPositionAxes(self.num_axes, ctypes.cast(self._axes, ctypes.POINTER(ctypes.c_uint8)))
+        self._address = ctypes.addressof(self._c)
+
+    @classmethod
+    def sections(cls, *pairs: int) -> "PositionAxes":
+        """The first pairs[0] pairs turn by axis 0, the next pairs[1] by axis 1, ..."""
+        return cls([a for a, n in enumerate(pairs) for _ in range(n)], len(pairs))
+
+    @classmethod
+    def in_turn(cls, *pairs: int) -> "PositionAxes":
+        """Axis a > 0 has pairs a, a + A, a + 2 A, ..., pairs[a] of A axes' in all, axis 0 the others (of sum(pairs))."""
+        n, axes = sum(pairs), len(pairs)
+        if any(m and a + (m - 1) * axes >= n for a, m in enumerate(pairs) if a):
+            raise ValueError(f"PositionAxes: {pairs} pairs do not go in turn")
+        return cls([i % axes if i // axes < pairs[i % axes] else 0 for i in range(n)], axes)
+
+
+@dataclass
+class HeadNorm:
+    """Mirror of lserve_head_norm; weights: float32 [D] for all heads, or [heads][D] (both alike), or None for ones."""
+    q_weight: Optional[torch.Tensor] = None
+    k_weight: Optional[torch.Tensor] = None
+    eps: float = 1e-6
+    centred: bool = False
+
+    def __post_init__(self):
+        given = [w for w in (self.q_weight, self.k_weight) if w is not None]
+        if any(w.dtype != torch.float32 or w.dim() not in (1, 2) or w.dim() != given[0].dim() for w in given):
+            raise ValueError("HeadNorm: weights are [D] or [heads][D], of 32 bits")
+        self._c = _CHeadNorm(int(self.centred), int(bool(given) and given[0].dim() == 2), float(self.eps), _ptr(self.q_weight), _ptr(self.k_weight))
+        self._address = ctypes.addressof(self._c)
+
+
+def lserve_rotary_axes(desc: AttnDesc, rotary: RotaryDesc, axes: PositionAxes, q: Optional[torch.Tensor], k: Optional[torch.Tensor],
+                       positions: torch.Tensor, q_out: Optional[torch.Tensor], k_out: Optional[torch.Tensor], stream=None) -> None:
+    """positions: int32 [axes][total], axes any distance apart; q and k as in lserve_rotary."""
+    if positions is None:
+        raise ValueError("lserve_rotary_axes: positions [axes][total]")
+    _check((_calls or _native()).turned(desc._address, 0, rotary._address, axes._address, None, None, rotary.inv_freq, q, k, positions, q_out,
+                                        k_out, _stream(stream)), "lserve_rotary_axes")
+
+
+def lserve_norm_rotary(desc: AttnDesc, norm: HeadNorm, rotary: Optional[RotaryDesc], q: Optional[torch.Tensor], k: Optional[torch.Tensor],
+                       positions: Optional[torch.Tensor], q_out: Optional[torch.Tensor], k_out: Optional[torch.Tensor], stream=None,
+                       axes: Optional[PositionAxes] = None) -> None:
+    """positions: int32 [total], with axes [axes][total]; without rotary None will do."""
+    _check((_calls or _native()).turned(desc._address, norm._address, rotary._address if rotary else 0, axes._address if axes else 0, norm.q_weight,
+                                        norm.k_weight, rotary.inv_freq if rotary else None, q, k, positions, q_out, k_out, _stream(stream)),
+           "lserve_norm_rotary")
+
+
+def lserve_rotary_append_kv(desc: AttnDesc, kv: PagedKV, rotary: Optional[RotaryDesc], q: Optional[torch.Tensor], k: torch.Tensor,
+                            v: torch.Tensor, cu_new: torch.Tensor, start_pos: torch.Tensor, max_new_per_seq: int, q_out: Optional[torch.Tensor],
+                            k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None, norm: Optional[HeadNorm] = None,
+                            axes: Optional[PositionAxes] = None, positions: Optional[torch.Tensor] = None, stream=None) -> None:
+    """positions: int32 [total_new], with axes [axes][total_new], or None: start_pos[b] + j.  q, k and v may be cut out of the rows of a fused
+    projection."""
+    _check((_calls or _native()).rotary_append(
+        desc._address, kv, norm._address if norm else 0, rotary._address if rotary else 0, axes._address if axes else 0, norm.q_weight if norm else None,
+        norm.k_weight if norm else None, rotary.inv_freq if rotary else None, q, k, v, positions, cu_new, start_pos, max_new_per_seq, q_out, k_out, v_out,
+        _stream(stream)), "lserve_rotary_append_kv")
 
 
 def lserve_tree_masks(parents: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor, max_new_per_seq: int,

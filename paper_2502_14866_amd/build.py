@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(HERE, "liblserve.so")
 CALLS_PATH = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 SOURCES = ["lserve_api.hip", "page_stats.hip", "select_pages.hip", "sparse_decode.hip", "sparse_prefill.hip", "batch_tables.hip",
-           "rotary.hip", "tree_decode.hip"]
+           "rotary.hip", "norm_rotary.hip", "rotary_append.hip", "tree_decode.hip"]
 
 # Packed fp32 VALU forms are switched off for the device pass; the host pass does not know the
 # feature and says so, which is harmless.

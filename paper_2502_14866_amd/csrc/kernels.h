@@ -114,6 +114,44 @@ struct RotaryArgs {
 hipError_t preload_rotary_kernels();
 hipError_t launch_rotary(int dtype, const RotaryArgs& args, hipStream_t stream);
 
+// How heads are normed and turned on their way (lserve_rotary_axes, lserve_norm_rotary, lserve_rotary_append_kv).
+struct TurnArgs {
+    const int* positions;         // [axes][..], axis_stride apart; null where a token's place in its sequence is its position
+    long long axis_stride;
+    const double* inv_freq;
+    unsigned long long axis_of[2];  // axis of pair i: two bits, 2 (i % 32) up in word i / 32
+    int axes, rotary_dim, interleaved;  // rotary_dim 0: nothing turns
+    float scale;
+    int norm;                     // 0: none, 1: root mean square, 2: mean taken off first
+    int weight_step;              // elements between the weights of two heads: 0 or D
+    float eps;
+    const float *q_weight, *k_weight;  // null: ones
+};
+// q or k may be null; strides in elements.
+struct TurnedRowsArgs {
+    TurnArgs turn;
+    const void *q, *k;
+    void *q_out, *k_out;
+    long long q_stride, k_stride;
+    int heads_q, heads_k, total;
+};
+hipError_t preload_norm_rotary_kernels();
+hipError_t launch_turned_rows(int dtype, const TurnedRowsArgs& args, hipStream_t stream);
+
+// Rows into the paged cache (lserve_rotary_append_kv); q with q_out, k_out and v_out may be null.
+struct TurnedAppendArgs {
+    LayerParams lp;
+    PagedParams kv;
+    TurnArgs turn;
+    const void *q, *k, *v;
+    void *q_out, *k_out, *v_out;
+    long long q_stride, k_stride, v_stride;
+    const int *cu_new, *start_pos;
+    int total, max_new;
+};
+hipError_t preload_rotary_append_kernels();
+hipError_t launch_turned_append(int dtype, const TurnedAppendArgs& args, hipStream_t stream);
+
 // Attention of drafted tokens (lserve_sparse_decode_tree).
 struct TreeArgs {
     LayerParams lp;

@@ -166,6 +166,93 @@ HeadList selecting_heads(const LayerParams& lp) {
     return hl;
 }
 
+bool rotary_is_fine(const lserve_rotary_desc* r) {
+    return r->inv_freq && r->rotary_dim >= 2 && r->rotary_dim % 2 == 0 && r->scale >= 0.f && !std::isinf(r->scale) &&
+           (r->interleaved == 0 || r->interleaved == 1) && aligned16(r->inv_freq);
+}
+
+// How heads are normed and turned; positions as they are handed over (null is fine here where `own_places` says what stands in for them).
+int make_turn(const LayerParams& lp, const lserve_head_norm* norm, const lserve_rotary_desc* rotary, const lserve_position_axes* axes,
+              const int32_t* positions, int64_t positions_stride, int total, bool own_places, TurnArgs* t) {
+    if (norm) {
+        if ((norm->kind != LSERVE_NORM_RMS && norm->kind != LSERVE_NORM_CENTRED) || (norm->per_head != 0 && norm->per_head != 1)) return LSERVE_ERR_INVALID_ARG;
+        if (!(norm->eps > 0.f) || std::isinf(norm->eps) || !aligned16(norm->q_weight) || !aligned16(norm->k_weight)) return LSERVE_ERR_INVALID_ARG;
+        t->norm = norm->kind == LSERVE_NORM_RMS ? 1 : 2;
+        t->weight_step = norm->per_head ? kHeadDim : 0;
+        t->eps = norm->eps;
+        t->q_weight = norm->q_weight;
+        t->k_weight = norm->k_weight;
+    }
+    t->axes = 1;
+    t->scale = 1.f;
+    if (rotary) {
+        if (!rotary_is_fine(rotary) || (!positions && !own_places)) return LSERVE_ERR_INVALID_ARG;
+        if (rotary->rotary_dim > kHeadDim) return LSERVE_ERR_UNSUPPORTED;
+        t->inv_freq = rotary->inv_freq;
+        t->rotary_dim = rotary->rotary_dim;
+        t->interleaved = rotary->interleaved;
+        if (rotary->scale != 0.f) t->scale = rotary->scale;
+    }
+    if (axes) {
+        if (axes->num_axes < 1 || !rotary || !axes->pair_axis) return LSERVE_ERR_INVALID_ARG;
+        if (axes->num_axes > 4) return LSERVE_ERR_UNSUPPORTED;
+        if (positions && positions_stride < total) return LSERVE_ERR_INVALID_ARG;
+        for (int i = 0; i < rotary->rotary_dim / 2; ++i) {
+            if (axes->pair_axis[i] >= axes->num_axes) return LSERVE_ERR_INVALID_ARG;
+            t->axis_of[i / 32] |= (unsigned long long)axes->pair_axis[i] << (2 * (i % 32));
+        }
+        t->axes = axes->num_axes;
+        t->axis_stride = positions_stride;
+    }
+    if (!aligned16(positions)) return LSERVE_ERR_INVALID_ARG;
+    t->positions = positions;
+    return LSERVE_OK;
+}
+
+// What is read of all that.
+struct TurnRanges {
+    Range at[4];
+    TurnRanges(const LayerParams& lp, const TurnArgs& t, int total)
+        : at{{t.positions, ((t.axes - 1) * t.axis_stride + total) * 4}, {t.inv_freq, t.rotary_dim * 4LL},
+             {t.q_weight, (t.weight_step ? lp.H : 1) * kHeadDim * 4LL}, {t.k_weight, (t.weight_step ? lp.Hkv : 1) * kHeadDim * 4LL}} {}
+};
+
+// Rows of heads, dense where they may be written in place; `out` as handed over.
+bool rows_are_fine(const void* rows, int64_t stride, int64_t row, const void* out) {
+    return stride >= row && stride % 8 == 0 && !(out == rows && stride != row) && aligned16(rows) && aligned16(out);
+}
+
+// lserve_rotary_axes and lserve_norm_rotary behind their own checks.
+int turned_rows(const lserve_attn_desc* desc, const LayerParams& lp, const TurnArgs& turn, const void* q, const void* k, int32_t total, int64_t q_stride,
+                int64_t k_stride, void* q_out, void* k_out, void* stream) {
+    if (total <= 0 || (!q && !k) || !q != !q_out || !k != !k_out) return LSERVE_ERR_INVALID_ARG;
+    const int64_t q_row = (int64_t)lp.H * kHeadDim, k_row = (int64_t)lp.Hkv * kHeadDim;
+    if ((q && !rows_are_fine(q, q_stride, q_row, q_out)) || (k && !rows_are_fine(k, k_stride, k_row, k_out))) return LSERVE_ERR_INVALID_ARG;
+    // (outputs are whole, inputs rows that may lie apart; in place a row is read before it is written)
+    const Rows q_in = {q, q_row * 2, q_stride * 2, total}, k_in = {k, k_row * 2, k_stride * 2, total};
+    const Range q_to = {q_out, total * q_row * 2}, k_to = {k_out, total * k_row * 2};
+    const TurnRanges read(lp, turn, total);
+    for (const Range& o : {q_to, k_to}) {
+        for (const Range& i : read.at)
+            if (meet(o, i)) return LSERVE_ERR_INVALID_ARG;
+        if ((o.at != q && meet(o, q_in)) || (o.at != k && meet(o, k_in))) return LSERVE_ERR_INVALID_ARG;
+    }
+    if (meet(q_to, k_to) || (q_out && q_out == k) || (k_out && k_out == q)) return LSERVE_ERR_INVALID_ARG;
+    TurnedRowsArgs a = {};
+    a.turn = turn;
+    a.q = q;
+    a.k = k;
+    a.q_out = q_out;
+    a.k_out = k_out;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.heads_q = q ? lp.H : 0;
+    a.heads_k = k ? lp.Hkv : 0;
+    a.total = total;
+    const hipError_t e = launch_turned_rows(desc->dtype, a, (hipStream_t)stream);
+    return e == hipSuccess ? LSERVE_OK : fail_hip(e);
+}
+
 size_t select_workspace_bytes(const LayerParams& lp, int batch, int max_pages) {
     return (size_t)batch * lp.Hkv * max_pages * sizeof(float);
 }
@@ -600,6 +687,86 @@ int lserve_rotary_frequencies(const lserve_rotary_scaling* s, double* inv_freq, 
     return LSERVE_OK;
 }
 
+int lserve_rotary_axes(const lserve_attn_desc* desc, const lserve_rotary_desc* rotary, const lserve_position_axes* axes, const void* q, const void* k,
+                       const int32_t* positions, int64_t positions_stride, int32_t total, int64_t q_stride, int64_t k_stride, void* q_out,
+                       void* k_out, void* stream) {
+    LayerParams lp;
+    int rc = make_layer(desc, &lp);
+    if (rc) return rc;
+    if (!rotary || !axes) return LSERVE_ERR_INVALID_ARG;
+    TurnArgs turn = {};
+    rc = make_turn(lp, nullptr, rotary, axes, positions, positions_stride, total, false, &turn);
+    return rc ? rc : turned_rows(desc, lp, turn, q, k, total, q_stride, k_stride, q_out, k_out, stream);
+}
+
+int lserve_norm_rotary(const lserve_attn_desc* desc, const lserve_head_norm* norm, const lserve_rotary_desc* rotary, const lserve_position_axes* axes,
+                       const void* q, const void* k, const int32_t* positions, int64_t positions_stride, int32_t total, int64_t q_stride,
+                       int64_t k_stride, void* q_out, void* k_out, void* stream) {
+    LayerParams lp;
+    int rc = make_layer(desc, &lp);
+    if (rc) return rc;
+    if (!norm) return LSERVE_ERR_INVALID_ARG;
+    TurnArgs turn = {};
+    rc = make_turn(lp, norm, rotary, axes, positions, positions_stride, total, false, &turn);
+    return rc ? rc : turned_rows(desc, lp, turn, q, k, total, q_stride, k_stride, q_out, k_out, stream);
+}
+
+int lserve_rotary_append_kv(const lserve_attn_desc* desc, const lserve_paged_kv* kv, const lserve_head_norm* norm, const lserve_rotary_desc* rotary,
+                            const lserve_position_axes* axes, const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride,
+                            int64_t v_stride, const int32_t* positions, int64_t positions_stride, const int32_t* cu_new, const int32_t* start_pos,
+                            int32_t total_new, int32_t max_new_per_seq, void* q_out, void* k_out, void* v_out, void* stream) {
+    TurnedAppendArgs a = {};
+    int rc = make_layer(desc, &a.lp);
+    if (rc) return rc;
+    const int selecting = selecting_heads(a.lp).count;
+    rc = make_paged(kv, a.lp, true, true, selecting > 0, true, &a.kv);
+    if (rc) return rc;
+    if (!k || !v || !q != !q_out || !cu_new || !start_pos || total_new <= 0 || max_new_per_seq <= 0) return LSERVE_ERR_INVALID_ARG;
+    rc = make_turn(a.lp, norm, rotary, axes, positions, positions_stride, total_new, true, &a.turn);
+    if (rc) return rc;
+    const int64_t q_row = (int64_t)a.lp.H * kHeadDim, k_row = (int64_t)a.lp.Hkv * kHeadDim;
+    if ((q && !rows_are_fine(q, q_stride, q_row, q_out)) || !rows_are_fine(k, k_stride, k_row, k_out) || !rows_are_fine(v, v_stride, k_row, v_out))
+        return LSERVE_ERR_INVALID_ARG;
+    if (!aligned16(cu_new) || !aligned16(start_pos)) return LSERVE_ERR_INVALID_ARG;
+    // what one workgroup writes others still read rows, places and tables for
+    const long long batch = a.kv.batch, total = total_new, slab = 16LL * (long long)slab_chunks(a.lp.NP, a.kv.kv_bits);
+    const Rows rows[] = {{q, q_row * 2, q_stride * 2, total}, {k, k_row * 2, k_stride * 2, total}, {v, k_row * 2, v_stride * 2, total}};
+    const TurnRanges read(a.lp, a.turn, total_new);
+    const Range in[] = {read.at[0], read.at[1], read.at[2], read.at[3], {cu_new, (batch + 1) * 4}, {start_pos, batch * 4},
+                        {kv->page_table, batch * a.kv.max_pages * 4}, {a.kv.k_stream ? kv->ring_table : nullptr, batch * a.kv.ring * 4}};
+    // (a layer whose heads are all in the bounded pool writes nothing of the main one)
+    const bool main_used = !a.kv.k_stream || a.kv.stream_heads < a.lp.Hkv;
+    const long long main = main_used ? (long long)a.kv.num_pages * a.kv.pool_heads : 0, bounded = (long long)kv->num_pages_stream * a.kv.stream_heads;
+    const Range written[] = {{q_out, total * q_row * 2}, {k_out, total * k_row * 2}, {v_out, total * k_row * 2}, {kv->k_pool, main * slab},
+                             {kv->v_pool, main * slab}, {a.kv.k_stream, bounded * slab}, {a.kv.v_stream, bounded * slab},
+                             {selecting > 0 ? kv->stats : nullptr, main * a.lp.g * 4 * kHeadDim}};
+    for (const Range& o : written) {
+        for (const Range& i : in)
+            if (meet(o, i)) return LSERVE_ERR_INVALID_ARG;
+        for (const Rows& i : rows) {
+            const bool in_place = o.at && o.at == i.at && ((&i == &rows[0] && &o == &written[0]) || (&i == &rows[1] && &o == &written[1]));
+            if (!in_place && i.at && meet(o, i)) return LSERVE_ERR_INVALID_ARG;
+        }
+        for (const Range& other : written)
+            if (&other != &o && meet(o, other)) return LSERVE_ERR_INVALID_ARG;
+    }
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_out = q_out;
+    a.k_out = k_out;
+    a.v_out = v_out;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.cu_new = cu_new;
+    a.start_pos = start_pos;
+    a.total = total_new;
+    a.max_new = max_new_per_seq;
+    const hipError_t e = launch_turned_append(desc->dtype, a, (hipStream_t)stream);
+    return e == hipSuccess ? LSERVE_OK : fail_hip(e);
+}
+
 int lserve_tree_masks(const int32_t* parents, const int32_t* cu_new, const int32_t* seq_lens, int32_t batch, int32_t total_new,
                       int32_t max_new_per_seq, int32_t mask_words, uint64_t* tree_mask, int32_t* positions, void* stream) {
     if (!parents || !cu_new || !seq_lens || !tree_mask || !positions) return LSERVE_ERR_INVALID_ARG;
@@ -728,6 +895,8 @@ int lserve_init(void) {
     if (e == hipSuccess) e = preload_decode_kernels();
     if (e == hipSuccess) e = preload_table_kernels();
     if (e == hipSuccess) e = preload_rotary_kernels();
+    if (e == hipSuccess) e = preload_norm_rotary_kernels();
+    if (e == hipSuccess) e = preload_rotary_append_kernels();
     if (e == hipSuccess) e = preload_tree_kernels();
     return e == hipSuccess ? LSERVE_OK : fail_hip(e);
 }

@@ -21,6 +21,9 @@ decltype(&lserve_extend_tables) extend_tables;
 decltype(&lserve_tree_masks) tree_masks;
 decltype(&lserve_rotary) rotary;
 decltype(&lserve_sparse_decode_tree) sparse_decode_tree;
+decltype(&lserve_rotary_axes) rotary_axes;
+decltype(&lserve_norm_rotary) norm_rotary;
+decltype(&lserve_rotary_append_kv) rotary_append_kv;
 
 struct PythonError {};  // the interpreter's error is set
 
@@ -240,11 +243,11 @@ PyObject* py_masks(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // Address of [total][heads][dim] whose rows may lie apart, and how far.
-const void* rows(const at::Tensor* t, int64_t heads, int64_t dim, const char* what, int64_t* stride) {
+const void* rows(const char* where, const at::Tensor* t, int64_t heads, int64_t dim, const char* what, int64_t* stride) {
     *stride = 0;
     if (!t) return nullptr;
     if (t->dim() != 3 || t->size(1) != heads || t->size(2) != dim || t->stride(2) != 1 || t->stride(1) != dim)
-        refuse("lserve_rotary", std::string(what) + " is [total][" + std::to_string(heads) + "][" + std::to_string(dim) + "], heads next to each other");
+        refuse(where, std::string(what) + " is [total][" + std::to_string(heads) + "][" + std::to_string(dim) + "], heads next to each other");
     *stride = t->size(0) > 1 ? t->stride(0) : heads * dim;
     return t->data_ptr();
 }
@@ -257,7 +260,7 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
                          *qo = tensor_or_null(a[6]), *ko = tensor_or_null(a[7]);
         const int64_t dim = desc->head_dim, hq = desc->num_q_heads, hkv = desc->num_kv_heads, total = pos ? pos->numel() : 0;
         int64_t q_stride, k_stride;
-        const void *p_q = rows(q, hq, dim, "q", &q_stride), *p_k = rows(k, hkv, dim, "k", &k_stride);
+        const void *p_q = rows("lserve_rotary", q, hq, dim, "q", &q_stride), *p_k = rows("lserve_rotary", k, hkv, dim, "k", &k_stride);
         const at::ScalarType t = type_of(desc);
         check("lserve_rotary", {{pos, kInt, 1}, {freq, kDouble, rot->rotary_dim <= dim ? rot->rotary_dim / 2 : 0}, {q, t, total * hq * dim}, {qo, t, total * hq * dim},
                                 {k, t, total * hkv * dim}, {ko, t, total * hkv * dim}});
@@ -265,6 +268,110 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void *p_qo = address(qo), *p_ko = address(ko), *stream = stream_handle(a[8]);
         const WithoutLock w;
         return rotary(desc, rot, p_q, p_k, p_pos, (int32_t)total, q_stride, k_stride, p_qo, p_ko, stream);
+    });
+}
+
+template <class S> const S* described(PyObject* o) { return reinterpret_cast<const S*>((uintptr_t)number(o)); }
+
+// How heads are normed and turned: descriptions by address, and the tensors that they name.
+struct Turn {
+    const lserve_head_norm* norm;
+    const lserve_rotary_desc* rotary;
+    const lserve_position_axes* axes;
+    const at::Tensor *q_weight, *k_weight, *freq;
+    int64_t q_least, k_least, freq_least;
+    Turn(const lserve_attn_desc* d, PyObject* const* a)
+        : norm(described<lserve_head_norm>(a[0])), rotary(described<lserve_rotary_desc>(a[1])), axes(described<lserve_position_axes>(a[2])),
+          q_weight(tensor_or_null(a[3])), k_weight(tensor_or_null(a[4])), freq(tensor_or_null(a[5])) {
+        const int64_t dim = d->head_dim, turning = rotary ? rotary->rotary_dim : 0;
+        q_least = norm && norm->per_head ? dim * d->num_q_heads : dim;
+        k_least = norm && norm->per_head ? dim * d->num_kv_heads : dim;
+        freq_least = turning <= dim ? turning / 2 : 0;
+    }
+};
+
+// Address of positions [total], or with axes [axes][total], and how far the axes lie apart.
+const int32_t* places(const char* where, const at::Tensor* t, const lserve_position_axes* axes, int64_t total, int64_t* stride) {
+    *stride = 0;
+    if (!t) return nullptr;
+    if (!axes) {
+        if (t->dim() != 1 || t->size(0) < total) refuse(where, "positions are [total] without axes");
+        return address<const int32_t>(t);
+    }
+    if (t->dim() != 2 || t->size(0) != axes->num_axes || t->size(1) < total || (t->size(1) > 1 && t->stride(1) != 1))
+        refuse(where, "positions are [" + std::to_string(axes->num_axes) + "][total], those of an axis next to each other");
+    *stride = axes->num_axes > 1 ? t->stride(0) : t->size(1);
+    return static_cast<const int32_t*>(t->data_ptr());
+}
+
+PyObject* py_turned(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 13, [&] {
+        const lserve_attn_desc* desc = description(a[0]);
+        const Turn turn(desc, a + 1);
+        const char* where = turn.norm ? "lserve_norm_rotary" : "lserve_rotary_axes";
+        const at::Tensor *q = tensor_or_null(a[7]), *k = tensor_or_null(a[8]), *pos = tensor_or_null(a[9]), *qo = tensor_or_null(a[10]),
+                         *ko = tensor_or_null(a[11]);
+        const int64_t dim = desc->head_dim, hq = desc->num_q_heads, hkv = desc->num_kv_heads;
+        const int64_t total = pos && pos->dim() ? pos->size(-1) : q && q->dim() ? q->size(0) : k && k->dim() ? k->size(0) : 0;
+        int64_t q_stride, k_stride, apart;
+        const void *p_q = rows(where, q, hq, dim, "q", &q_stride), *p_k = rows(where, k, hkv, dim, "k", &k_stride);
+        const int32_t* p_pos = places(where, pos, turn.axes, total, &apart);
+        const at::ScalarType t = type_of(desc);
+        check(where, {{turn.q_weight, kFloat, turn.q_least}, {turn.k_weight, kFloat, turn.k_least}, {turn.freq, kDouble, turn.freq_least}, {pos, kInt, 1},
+                      {q, t, total * hq * dim}, {qo, t, total * hq * dim}, {k, t, total * hkv * dim}, {ko, t, total * hkv * dim}});
+        void *p_qo = address(qo), *p_ko = address(ko), *stream = stream_handle(a[12]);
+        const WithoutLock w;
+        return turn.norm ? norm_rotary(desc, turn.norm, turn.rotary, turn.axes, p_q, p_k, p_pos, apart, (int32_t)total, q_stride, k_stride, p_qo, p_ko, stream)
+                         : rotary_axes(desc, turn.rotary, turn.axes, p_q, p_k, p_pos, apart, (int32_t)total, q_stride, k_stride, p_qo, p_ko, stream);
+    });
+}
+
+PyObject* py_rotary_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 19, [&] {
+        const char* where = "lserve_rotary_append_kv";
+        const lserve_attn_desc* desc = description(a[0]);
+        const lserve_paged_kv kv = paged(a[1]);
+        const Held table(a[1], kPageTable), ring_table(a[1], kRingTable), k_pool(a[1], kKPool), v_pool(a[1], kVPool), k_stream(a[1], kKStream),
+            v_stream(a[1], kVStream), stats(a[1], kStats);
+        const Turn turn(desc, a + 2);
+        const at::Tensor *q = tensor_or_null(a[8]), *k = tensor_or_null(a[9]), *v = tensor_or_null(a[10]), *pos = tensor_or_null(a[11]),
+                         *cu = tensor_or_null(a[12]), *start = tensor_or_null(a[13]), *qo = tensor_or_null(a[15]), *ko = tensor_or_null(a[16]),
+                         *vo = tensor_or_null(a[17]);
+        const int64_t dim = desc->head_dim, hq = desc->num_q_heads, hkv = desc->num_kv_heads, batch = kv.batch, total = k && k->dim() ? k->size(0) : 0;
+        int64_t q_stride, k_stride, v_stride, apart;
+        const void *p_q = rows(where, q, hq, dim, "q", &q_stride), *p_k = rows(where, k, hkv, dim, "k", &k_stride),
+                   *p_v = rows(where, v, hkv, dim, "v", &v_stride);
+        const int32_t* p_pos = places(where, pos, turn.axes, total, &apart);
+        const at::ScalarType t = type_of(desc);
+        const bool rows16 = kv.kv_bits == 0 || kv.kv_bits == 16, codes = kv.kv_bits == 8 || kv.kv_bits == 4;
+        const int64_t slab = rows16 ? (int64_t)desc->page_size * dim : codes ? 8 * dim * kv.kv_bits + 256 : 0;
+        auto kind = [&](const Held& pool) { return rows16 ? t : codes || (pool.t && pool.t->scalar_type() == at::kByte) ? at::kByte : t; };
+        int64_t streaming = 0;
+        for (int64_t h = 0; h < hkv; ++h) streaming += desc->kv_head_is_streaming[h] != 0;
+        const int64_t streams = k_stream.t ? streaming : 0;
+        // (all heads in the bounded pool: nothing of the main one)
+        const int64_t heads = streams < hkv ? (int64_t)kv.num_pages * (kv.pool_heads ? kv.pool_heads : hkv) : 0;
+        const int64_t pool = heads * slab, bounded = kv.num_pages_stream * streams * slab;
+        const int64_t spans = streaming < hkv && desc->logical_page_size > 0 ? heads * (desc->page_size / desc->logical_page_size) * 2 * dim : 0;
+        check(where, {{turn.q_weight, kFloat, turn.q_least}, {turn.k_weight, kFloat, turn.k_least}, {turn.freq, kDouble, turn.freq_least},
+                      {q, t, total * hq * dim}, {k, t, total * hkv * dim}, {v, t, total * hkv * dim}, {pos, kInt, 1}, {cu, kInt, batch + 1},
+                      {start, kInt, batch}, {qo, t, total * hq * dim}, {ko, t, total * hkv * dim}, {vo, t, total * hkv * dim}, {table.t, kInt, 0},
+                      {k_pool.t, kind(k_pool), pool}, {v_pool.t, kind(v_pool), pool}, {k_stream.t, kind(k_stream), bounded},
+                      {v_stream.t, kind(v_stream), bounded}, {stats.t, t, spans}, {ring_table.t, kInt, k_stream.t ? batch * ring_of(desc) : 0}});
+        const int32_t *p_cu = address<int32_t>(cu), *p_start = address<int32_t>(start), longest = number32(a[14]);
+        void *p_qo = address(qo), *p_ko = address(ko), *p_vo = address(vo), *stream = stream_handle(a[18]);
+        const WithoutLock w;
+        return rotary_append_kv(desc, &kv, turn.norm, turn.rotary, turn.axes, p_q, p_k, p_v, q_stride, k_stride, v_stride, p_pos, apart, p_cu, p_start,
+                                (int32_t)total, longest, p_qo, p_ko, p_vo, stream);
+    });
+}
+
+PyObject* py_bind_turned(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 3, [&] {
+        rotary_axes = reinterpret_cast<decltype(rotary_axes)>((uintptr_t)number(a[0]));
+        norm_rotary = reinterpret_cast<decltype(norm_rotary)>((uintptr_t)number(a[1]));
+        rotary_append_kv = reinterpret_cast<decltype(rotary_append_kv)>((uintptr_t)number(a[2]));
+        return 0;
     });
 }
 
@@ -338,6 +445,12 @@ PyMethodDef methods[] = {
      "desc address, kv, new_lens, free_pages, cu_new, new_seq_lens, pages_taken, positions, slots, ring_slots, total_new, stream"},
     {"masks", LSERVE_FASTCALL(py_masks), "parents, cu_new, seq_lens, max_new_per_seq, tree_mask, positions, stream"},
     {"rotary", LSERVE_FASTCALL(py_rotary), "desc address, rotary address, inv_freq, q, k, positions, q_out, k_out, stream"},
+    {"bind_turned", LSERVE_FASTCALL(py_bind_turned), "addresses of lserve_rotary_axes, lserve_norm_rotary, lserve_rotary_append_kv"},
+    {"turned", LSERVE_FASTCALL(py_turned),
+     "desc address, norm address or 0, rotary address or 0, axes address or 0, q_weight, k_weight, inv_freq, q, k, positions, q_out, k_out, stream"},
+    {"rotary_append", LSERVE_FASTCALL(py_rotary_append),
+     "desc address, kv, norm address or 0, rotary address or 0, axes address or 0, q_weight, k_weight, inv_freq, q, k, v, positions, cu_new, start_pos, "
+     "max_new_per_seq, q_out, k_out, v_out, stream"},
     {"tree", LSERVE_FASTCALL(py_tree),
      "desc address, kv, q, k_new, v_new, cu_new, max_new_per_seq, out, lse_out, tree_mask, positions, sel_pages, sel_count, sel_seq_len, workspace, stream"},
     {nullptr, nullptr, 0, nullptr}};

@@ -1,4 +1,4 @@
-// Angles of rotary positions, for the kernels that turn rows.
+// Angles of rotary positions, and rows of heads normed and turned by them, for the kernels that turn rows.
 #pragma once
 
 #include "kernels.h"
@@ -11,6 +11,143 @@ __device__ __forceinline__ float2 turn_of(int position, double radians, float sc
     float s, c;
     sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
     return make_float2(c * scale, s * scale);
+}
+
+// Axis whose position turns a pair.
+__device__ __forceinline__ int axis_of(const TurnArgs& t, int pair) { return (int)(t.axis_of[pair / 32] >> (2 * (pair % 32))) & 3; }
+
+// Sum over groups of eight lanes; every lane of a group receives the total.
+__device__ __forceinline__ float row8_sum(float x) {
+    x += dpp_f<kDppXor1>(x);
+    x += dpp_f<kDppXor2>(x);
+    x += dpp_f<kDppHalfMirror>(x);
+    return x;
+}
+
+// A row (a head of a token) is held by eight lanes, two pieces of eight channels to a lane.  With halves (channel i turns with i + R / 2) a lane has
+// one piece of either half, or two neighbouring ones of what does not turn; interleaved (2 i with 2 i + 1) the two are eight apart.  Halves
+// whose R is no multiple of 16 have partners in other lanes: they pass through LDS.
+enum Layout { kHalves, kInterleaved, kOddHalves };
+struct Pieces {
+    int p0, p1;
+    bool turns;  // kHalves: these pieces turn
+};
+template <int LAYOUT> __device__ __forceinline__ Pieces pieces_of(int l, int rotary_dim) {
+    if (LAYOUT != kHalves) return {l, l + 8, true};
+    const int half = rotary_dim / 16;
+    return l < half ? Pieces{l, l + half, true} : Pieces{2 * l, 2 * l + 1, false};
+}
+// The lane's eight pairs: 0 .. 3 and 4 .. 7 are, interleaved, those of either piece.
+template <int LAYOUT> __device__ __forceinline__ int pair_of(const Pieces& p, int i) {
+    return LAYOUT == kInterleaved ? (i < 4 ? 4 * p.p0 + i : 4 * p.p1 + i - 4) : 8 * p.p0 + i;
+}
+
+// x - m over the root of mean((x - m)^2) + eps times the weight, in 32 bits throughout; m is 0 or the mean.
+__device__ __forceinline__ void norm_row(float (&x)[8], float (&y)[8], const TurnArgs& t, const float* weight, const Pieces& p) {
+    if (t.norm == 2) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += x[i] + y[i];
+        const float mean = row8_sum(sum) * (1.f / kHeadDim);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] -= mean;
+            y[i] -= mean;
+        }
+    }
+    float squares = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) squares = __builtin_fmaf(x[i], x[i], __builtin_fmaf(y[i], y[i], squares));
+    const float inverse = rsqrtf(row8_sum(squares) * (1.f / kHeadDim) + t.eps);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[i] *= inverse;
+        y[i] *= inverse;
+    }
+    if (weight) {
+        const float4* w = reinterpret_cast<const float4*>(weight);
+        const float4 a = w[2 * p.p0], b = w[2 * p.p0 + 1], c = w[2 * p.p1], d = w[2 * p.p1 + 1];
+        const float u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, v[8] = {c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] *= u[i];
+            y[i] *= v[i];
+        }
+    }
+}
+
+__device__ __forceinline__ float2 turned(float a, float b, float2 turn) {
+    return make_float2(__builtin_fmaf(a, turn.x, -(b * turn.y)), __builtin_fmaf(b, turn.x, a * turn.y));
+}
+
+// A lane's two pieces of a row, normed and turned; turn: of its eight pairs.  Channels that do not turn keep their bits without a norm.
+// kOddHalves: `room` is kHeadDim floats of LDS for the row, its own; turns: (cos, sin) of all pairs of the row's token.
+template <class T, int LAYOUT>
+__device__ __forceinline__ void turn_row(uint32_t (&x)[4], uint32_t (&y)[4], const float2 (&turn)[8], const TurnArgs& t, const float* weight,
+                                         const Pieces& p, float* room, const float2* turns) {
+    float a[8], b[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[2 * i] = Elem<T>::lo(x[i]);
+        a[2 * i + 1] = Elem<T>::hi(x[i]);
+        b[2 * i] = Elem<T>::lo(y[i]);
+        b[2 * i + 1] = Elem<T>::hi(y[i]);
+    }
+    if (t.norm) {
+        norm_row(a, b, t, weight, p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // what stands where nothing turns
+            x[i] = Elem<T>::pack(a[2 * i], a[2 * i + 1]);
+            y[i] = Elem<T>::pack(b[2 * i], b[2 * i + 1]);
+        }
+    }
+    if constexpr (LAYOUT == kHalves) {
+        uint32_t u[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 first = turned(a[2 * i], b[2 * i], turn[2 * i]), second = turned(a[2 * i + 1], b[2 * i + 1], turn[2 * i + 1]);
+            u[i] = Elem<T>::pack(first.x, second.x);
+            v[i] = Elem<T>::pack(first.y, second.y);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = p.turns ? u[i] : x[i];
+            y[i] = p.turns ? v[i] : y[i];
+        }
+    } else if constexpr (LAYOUT == kInterleaved) {
+        const int pairs = t.rotary_dim / 2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 first = turned(a[2 * i], a[2 * i + 1], turn[i]), second = turned(b[2 * i], b[2 * i + 1], turn[4 + i]);
+            if (4 * p.p0 + i < pairs) x[i] = Elem<T>::pack(first.x, first.y);
+            if (4 * p.p1 + i < pairs) y[i] = Elem<T>::pack(second.x, second.y);
+        }
+    } else {
+        const int pairs = t.rotary_dim / 2;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            room[8 * p.p0 + i] = a[i];
+            room[8 * p.p1 + i] = b[i];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (the row's lanes share a wavefront)
+        auto at = [&](int channel, float own) {  // a channel of the row as it comes out
+            if (channel >= 2 * pairs) return own;
+            const bool upper = channel >= pairs;
+            const int pair = upper ? channel - pairs : channel;
+            const float2 both = upper ? turned(room[pair], own, turns[pair]) : turned(own, room[pair + pairs], turns[pair]);
+            return upper ? both.y : both.x;
+        };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = 8 * p.p0 + 2 * i, d = 8 * p.p1 + 2 * i;
+            const float a0 = at(c, a[2 * i]), a1 = at(c + 1, a[2 * i + 1]), b0 = at(d, b[2 * i]), b1 = at(d + 1, b[2 * i + 1]);
+            const uint32_t u = Elem<T>::pack(a0, a1), v = Elem<T>::pack(b0, b1);
+            // (channel by channel: what does not turn keeps its bits)
+            x[i] = c + 1 < 2 * pairs ? u : c < 2 * pairs ? (u & 0xffffu) | (x[i] & 0xffff0000u) : x[i];
+            y[i] = d + 1 < 2 * pairs ? v : d < 2 * pairs ? (v & 0xffffu) | (y[i] & 0xffff0000u) : y[i];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next row takes the room over
+    }
 }
 
 }  // namespace lserve
