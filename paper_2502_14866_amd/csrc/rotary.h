@@ -42,8 +42,20 @@ template <int LAYOUT> __device__ __forceinline__ int pair_of(const Pieces& p, in
     return LAYOUT == kInterleaved ? (i < 4 ? 4 * p.p0 + i : 4 * p.p1 + i - 4) : 8 * p.p0 + i;
 }
 
+// A lane's weights of a row's norm: of its two pieces.
+struct Weights {
+    float x[8], y[8];
+};
+__device__ __forceinline__ void load_weights(const float* weight, const Pieces& p, Weights& to) {
+    if (weight) {
+        const float4* w = reinterpret_cast<const float4*>(weight);
+        const float4 a = w[2 * p.p0], b = w[2 * p.p0 + 1], c = w[2 * p.p1], d = w[2 * p.p1 + 1];
+        to = {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, {c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w}};
+    }
+}
+
 // x - m over the root of mean((x - m)^2) + eps times the weight, in 32 bits throughout; m is 0 or the mean.
-__device__ __forceinline__ void norm_row(float (&x)[8], float (&y)[8], const TurnArgs& t, const float* weight, const Pieces& p) {
+__device__ __forceinline__ void norm_row(float (&x)[8], float (&y)[8], const TurnArgs& t, bool weighted, const Weights& w) {
     if (t.norm == 2) {
         float sum = 0.f;
 #pragma unroll
@@ -64,14 +76,11 @@ __device__ __forceinline__ void norm_row(float (&x)[8], float (&y)[8], const Tur
         x[i] *= inverse;
         y[i] *= inverse;
     }
-    if (weight) {
-        const float4* w = reinterpret_cast<const float4*>(weight);
-        const float4 a = w[2 * p.p0], b = w[2 * p.p0 + 1], c = w[2 * p.p1], d = w[2 * p.p1 + 1];
-        const float u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, v[8] = {c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w};
+    if (weighted) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[i] *= u[i];
-            y[i] *= v[i];
+            x[i] *= w.x[i];
+            y[i] *= w.y[i];
         }
     }
 }
@@ -82,9 +91,9 @@ __device__ __forceinline__ float2 turned(float a, float b, float2 turn) {
 
 // A lane's two pieces of a row, normed and turned; turn: of its eight pairs.  Channels that do not turn keep their bits without a norm.
 // kOddHalves: `room` is kHeadDim floats of LDS for the row, its own; turns: (cos, sin) of all pairs of the row's token.
-template <class T, int LAYOUT>
-__device__ __forceinline__ void turn_row(uint32_t (&x)[4], uint32_t (&y)[4], const float2 (&turn)[8], const TurnArgs& t, const float* weight,
-                                         const Pieces& p, float* room, const float2* turns) {
+template <class T, int LAYOUT, bool NORM>
+__device__ __forceinline__ void turn_row(uint32_t (&x)[4], uint32_t (&y)[4], const float2 (&turn)[8], const TurnArgs& t, bool weighted,
+                                         const Weights& w, const Pieces& p, float* room, const float2* turns) {
     float a[8], b[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -93,8 +102,8 @@ __device__ __forceinline__ void turn_row(uint32_t (&x)[4], uint32_t (&y)[4], con
         b[2 * i] = Elem<T>::lo(y[i]);
         b[2 * i + 1] = Elem<T>::hi(y[i]);
     }
-    if (t.norm) {
-        norm_row(a, b, t, weight, p);
+    if constexpr (NORM) {
+        norm_row(a, b, t, weighted, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {  // what stands where nothing turns
             x[i] = Elem<T>::pack(a[2 * i], a[2 * i + 1]);
@@ -148,6 +157,41 @@ __device__ __forceinline__ void turn_row(uint32_t (&x)[4], uint32_t (&y)[4], con
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next row takes the room over
     }
+}
+
+// Angles of a token in LDS: what a lane reads of its eight pairs is four pieces of sixteen bytes, each next to those of the other lanes of the row;
+// the rows of neighbouring tokens start in other banks.  kOddHalves: pair by pair.
+constexpr int kTurnRow = 80;  // float2 to a token
+template <int LAYOUT> __device__ __forceinline__ int turn_place(int pair) {
+    if (LAYOUT == kOddHalves) return pair;
+    const int l = LAYOUT == kHalves ? pair / 8 : pair % 32 / 4, i = LAYOUT == kHalves ? pair % 8 : pair / 32 * 4 + pair % 4;
+    return i / 2 * 16 + l * 2 + i % 2;
+}
+__device__ __forceinline__ void read_turns(const float2* row, int l, float2 (&turn)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 two = *reinterpret_cast<const float4*>(row + i * 16 + l * 2);
+        turn[2 * i] = make_float2(two.x, two.y);
+        turn[2 * i + 1] = make_float2(two.z, two.w);
+    }
+}
+
+__device__ __forceinline__ void load_pieces(const void* base, size_t element, const Pieces& p, uint32_t (&x)[4], uint32_t (&y)[4]) {
+    const uint4* row = reinterpret_cast<const uint4*>((const uint16_t*)base + element);
+    const uint4 u = row[p.p0], v = row[p.p1];
+    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
+    y[0] = v.x, y[1] = v.y, y[2] = v.z, y[3] = v.w;
+}
+__device__ __forceinline__ void store_pieces(void* base, size_t element, const Pieces& p, const uint32_t (&x)[4], const uint32_t (&y)[4]) {
+    uint4* row = reinterpret_cast<uint4*>((uint16_t*)base + element);
+    row[p.p0] = make_uint4(x[0], x[1], x[2], x[3]);
+    row[p.p1] = make_uint4(y[0], y[1], y[2], y[3]);
+}
+
+// Waits for loads in flight into x and y: what follows, stores above all, is not asked for before they are there.  (A wait counts what was asked for
+// since, and where some of that is conditional the compiler counts none of it: behind a row's stores it would wait for these too.)
+__device__ __forceinline__ void arrived(uint32_t (&x)[4], uint32_t (&y)[4]) {
+    asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3])::"memory");
 }
 
 }  // namespace lserve

@@ -1,6 +1,8 @@
 // New tokens on their way from a projection into the paged cache: queries normed and turned, keys normed, turned and written to their pages
 // (16-bit rows or codes) with the key statistics brought up to date, values written next to them.  What it leaves in the cache is what
-// lserve_append_kv would be handed the turned keys for.  Bound: HBM, every row read once, queries and pages written once.
+// lserve_append_kv would be handed the turned keys for.  Bound: HBM, every row read once, queries and pages written once: 65536 tokens of 32 / 8 heads, 1.62 GB
+// with 16-bit pages, 300 us = 5.4 TB/s (a copy of 671 MiB runs at 5.3); eight of 512 to 8192 into 8-bit pages with dense keys and values kept, 618 MB, 120
+// us; 16 single tokens 4.2 us, which is a launch and the loads of a place, an angle, a row and a page one after the other.
 #include <algorithm>
 
 #include "quantize.h"
@@ -11,26 +13,7 @@ namespace lserve {
 namespace {
 
 constexpr int kAppendThreads = 256, kAppendWaves = kAppendThreads / kWave;
-
-constexpr int kDppRor8 = 0x128;  // lane i <-> i ^ 8 inside each row
-
-// Combines lanes l, l ^ 8, l ^ 16, l ^ 32, as far as `rows` (a power of two) rows of eight lanes go.
-template <class Op> __device__ __forceinline__ float over_rows(float x, int rows, Op op) {
-    if (rows >= 2) x = op(x, dpp_f<kDppRor8>(x));
-    if (rows >= 4) {
-        const unsigned u = __builtin_bit_cast(unsigned, x);
-        const swap_pair_t s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-        const unsigned s0 = s[0], s1 = s[1];
-        x = op(__builtin_bit_cast(float, s0), __builtin_bit_cast(float, s1));
-    }
-    if (rows >= 8) {
-        const unsigned u = __builtin_bit_cast(unsigned, x);
-        const swap_pair_t s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-        const unsigned s0 = s[0], s1 = s[1];
-        x = op(__builtin_bit_cast(float, s0), __builtin_bit_cast(float, s1));
-    }
-    return x;
-}
+constexpr int kStepThreads = 256, kStepWaves = kStepThreads / kWave;
 
 // Writes the ranges of eight channels into the statistics rows of a logical page, with what they hold taken in if it held tokens before.
 template <class T>
@@ -61,103 +44,136 @@ struct Slab {
     uint4 *k, *v;
     size_t page_head;  // (page, head) index inside the pool
 };
-__device__ __forceinline__ Slab slab_of(const LayerParams& lp, const PagedParams& kv, int b, int hk, int p, int bits) {
+// Physical pages of page p of sequence b, in the main pool and in the ring.
+struct Pages {
+    int main, ring;
+};
+__device__ __forceinline__ Pages pages_of(const LayerParams& lp, const PagedParams& kv, int b, int p) {
+    return {kv.page_table[(size_t)b * kv.max_pages + p], kv.k_stream ? kv.ring_table[(size_t)b * kv.ring + ring_slot(lp, p)] : 0};
+}
+__device__ __forceinline__ Slab slab_of(const LayerParams& lp, const PagedParams& kv, const Pages& pages, int hk, int bits) {
     const bool ring = in_stream_pool(lp, kv, hk);
-    const int phys = ring ? kv.ring_table[(size_t)b * kv.ring + ring_slot(lp, p)] : kv.page_table[(size_t)b * kv.max_pages + p];
+    const int phys = ring ? pages.ring : pages.main;
     const size_t ph = (size_t)phys * (ring ? kv.stream_heads : kv.pool_heads) + pool_rank(lp, kv, hk, ring);
     uint4 *k = reinterpret_cast<uint4*>(const_cast<void*>(ring ? kv.k_stream : kv.k_pool)),
           *v = reinterpret_cast<uint4*>(const_cast<void*>(ring ? kv.v_stream : kv.v_pool));
     return {k + ph * slab_chunks(lp.NP, bits), v + ph * slab_chunks(lp.NP, bits), ph};
 }
 
-// A lane's two pieces of a row to its slot of a slab.
-template <class T, int BITS>
-__device__ __forceinline__ void write_row(uint4* slab, int page_size, int slot, const Pieces& p, int l, const uint32_t (&x)[4], const uint32_t (&y)[4]) {
+// A lane's two pieces of a row as a page of BITS keeps them, and on their way to a slot.
+template <int BITS> struct Stored {
+    uint2 x, y;
+    uint32_t pair;
+};
+template <> struct Stored<16> {
+    uint4 x, y;
+};
+template <class T, int BITS> __device__ __forceinline__ Stored<BITS> stored(const uint32_t (&x)[4], const uint32_t (&y)[4]) {
+    Stored<BITS> s;
+    if constexpr (BITS == 16)
+        s = {make_uint4(x[0], x[1], x[2], x[3]), make_uint4(y[0], y[1], y[2], y[3])};
+    else
+        quantize_pieces<T, BITS>(x, y, s.x, s.y, s.pair);
+    return s;
+}
+template <int BITS> __device__ __forceinline__ void write_row(uint4* slab, int page_size, int slot, const Pieces& p, int l, const Stored<BITS>& s) {
     const size_t row = (size_t)slot * (kHeadDim / 8);
     if constexpr (BITS == 16) {
-        slab[row + p.p0] = make_uint4(x[0], x[1], x[2], x[3]);
-        slab[row + p.p1] = make_uint4(y[0], y[1], y[2], y[3]);
+        slab[row + p.p0] = s.x;
+        slab[row + p.p1] = s.y;
     } else {
-        uint2 u, v;
-        uint32_t pair;
-        quantize_pieces<T, BITS>(x, y, u, v, pair);
         if constexpr (BITS == 8) {
-            reinterpret_cast<uint2*>(slab)[row + p.p0] = u;
-            reinterpret_cast<uint2*>(slab)[row + p.p1] = v;
+            reinterpret_cast<uint2*>(slab)[row + p.p0] = s.x;
+            reinterpret_cast<uint2*>(slab)[row + p.p1] = s.y;
         } else {
-            reinterpret_cast<uint32_t*>(slab)[row + p.p0] = u.x;
-            reinterpret_cast<uint32_t*>(slab)[row + p.p1] = v.x;
+            reinterpret_cast<uint32_t*>(slab)[row + p.p0] = s.x.x;
+            reinterpret_cast<uint32_t*>(slab)[row + p.p1] = s.y.x;
         }
-        if (l == 0) reinterpret_cast<uint32_t*>(slab + page_size * (kHeadDim * BITS / 128))[slot] = pair;
+        if (l == 0) reinterpret_cast<uint32_t*>(slab + page_size * (kHeadDim * BITS / 128))[slot] = s.pair;
     }
 }
 
-// Angles of a token in LDS: what a lane reads of its eight pairs is four pieces of sixteen bytes, each next to those of the other lanes of the row;
-// the rows of neighbouring tokens start in other banks.  kOddHalves: pair by pair.
-constexpr int kTurnRow = 80;  // float2 to a token
-template <int LAYOUT> __device__ __forceinline__ int turn_place(int pair) {
-    if (LAYOUT == kOddHalves) return pair;
-    const int l = LAYOUT == kHalves ? pair / 8 : pair % 32 / 4, i = LAYOUT == kHalves ? pair % 8 : pair / 32 * 4 + pair % 4;
-    return i / 2 * 16 + l * 2 + i % 2;
-}
-__device__ __forceinline__ void read_turns(const float2* row, int l, float2 (&turn)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float4 two = *reinterpret_cast<const float4*>(row + i * 16 + l * 2);
-        turn[2 * i] = make_float2(two.x, two.y);
-        turn[2 * i + 1] = make_float2(two.z, two.w);
-    }
-}
-
-template <class T> __device__ __forceinline__ void load_pieces(const void* base, size_t element, const Pieces& p, uint32_t (&x)[4], uint32_t (&y)[4]) {
-    const uint4* row = reinterpret_cast<const uint4*>((const uint16_t*)base + element);
-    const uint4 u = row[p.p0], v = row[p.p1];
-    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
-    y[0] = v.x, y[1] = v.y, y[2] = v.z, y[3] = v.w;
-}
-__device__ __forceinline__ void store_pieces(void* base, size_t element, const Pieces& p, const uint32_t (&x)[4], const uint32_t (&y)[4]) {
-    uint4* row = reinterpret_cast<uint4*>((uint16_t*)base + element);
-    row[p.p0] = make_uint4(x[0], x[1], x[2], x[3]);
-    row[p.p1] = make_uint4(y[0], y[1], y[2], y[3]);
-}
+// Sixteen-byte pieces of LDS for a wavefront: sixteen 16-bit rows, or (kOddHalves, at another time) eight 32-bit ones.
+constexpr int kTile = 16 * kHeadDim / 8;
 
 __device__ __forceinline__ int position_of(const TurnArgs& t, int token, int place, int pair) {
     return t.positions ? t.positions[axis_of(t, pair) * t.axis_stride + token] : place;
 }
 
-// First block of sequence b: sequences get a block for every `block` tokens or part of it, and one more for a start inside of one.
-__device__ __forceinline__ int first_block(const int* cu_new, int b, int block) { return cu_new[b] / block + 2 * b; }
-// The sequence of a block, by 64 candidates at a time.
-__device__ __forceinline__ int sequence_of(const int* cu_new, int batch, int block, int at, int lane) {
+// First block of a sequence: each gets a block for every `block` tokens or part of it, and one more for a start inside of one.
+__device__ __forceinline__ int first_block(int cu, int b, int block) { return cu / block + 2 * b; }
+// The sequence of a block, by 64 candidates at a time, with its first row, the first row behind it and its first position.
+struct Found {
+    int b, cu, cu_next, start;
+};
+__device__ __forceinline__ Found sequence_of(const int* cu_new, const int* start_pos, int batch, int block, int at, int lane) {
     int lo = 0, left = batch;
-    while (left > 1) {
-        const int step = (left + kWave - 1) / kWave, i = lane * step;
-        const unsigned long long in = __ballot(i < left && first_block(cu_new, lo + min(i, left - 1), block) <= at);
-        const int n = max(__popcll(in) - 1, 0) * step;
-        left = min(step, left - n);
-        lo += n;
+    while (true) {
+        const int step = (left + kWave - 1) / kWave, i = lo + min(lane * step, left - 1);
+        const int cu = cu_new[i], cu_next = cu_new[i + 1], start = start_pos[i];
+        const unsigned long long in = __ballot(lane * step < left && first_block(cu, i, block) <= at);
+        const int n = max(__popcll(in) - 1, 0);
+        if (step == 1)
+            return {lo + n, __builtin_amdgcn_readlane(cu, n), __builtin_amdgcn_readlane(cu_next, n), __builtin_amdgcn_readlane(start, n)};
+        lo += n * step;
+        left = min(step, left - n * step);
     }
-    return __builtin_amdgcn_readfirstlane(lo);
 }
 
 }  // namespace
 
 // A workgroup has a block of `block` neighbouring tokens of a sequence, aligned in the sequence and at least a logical page, and works out its
-// angles once, into LDS.  Its wavefronts, and those of the `share` workgroups of the block, take heads in turn: keys, values, queries; eight lanes to
-// a row and eight tokens of a head at a time, so that the rows of a page are written next to each other and a logical page's
-// range stays in the registers of one wavefront.
-template <class T, int LAYOUT, int BITS>
+// angles once, into LDS.  Its wavefronts, and those of the `share` workgroups of the block, take units in turn, eight lanes to a row and twice eight rows at
+// a time: a KV head of keys or values, sixteen tokens at a time, so that the rows of a page are written next to each other; or eight heads of the queries,
+// two tokens at a time.  The next sixteen rows are in flight while sixteen are worked on.
+template <class T, int LAYOUT, int BITS, bool NORM>
 __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedAppendArgs a, int block, int share) {
-    extern __shared__ float2 lds[];  // [block][kTurnRow], then for kOddHalves a row of channels for every row in hand
+    extern __shared__ float2 lds[];  // [block][kTurnRow], then a tile for every wavefront
     const LayerParams& lp = a.lp;
     const PagedParams& kv = a.kv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    const int part = blockIdx.x % share, at = blockIdx.x / share;
-    const int b = sequence_of(a.cu_new, kv.batch, block, at, lane);
-    const int src0 = a.cu_new[b], s = a.start_pos[b], e = s + min(a.cu_new[b + 1], a.total) - src0;
-    const int lo = (s / block + at - first_block(a.cu_new, b, block)) * block;
+    // (workgroups go to the XCDs in turn: the parts, some of them dearer, move on by one with every block)
+    const int at = blockIdx.x / share, part = (blockIdx.x + at) % share;
+    const Found found = sequence_of(a.cu_new, a.start_pos, kv.batch, block, at, lane);
+    const int b = found.b, src0 = found.cu, s = found.start, e = s + min(found.cu_next, a.total) - src0;
+    const int lo = (s / block + at - first_block(src0, b, block)) * block;
     const int t0 = max(lo, s), t1 = min(lo + block, e);
     if (t0 >= t1) return;
+
+    const int page = lo / lp.NP, in_page = lo - page * lp.NP;
+    const Pages pages = pages_of(lp, kv, b, page);
+    const int l = lane % 8, r = lane / 8;
+    const Pieces p = pieces_of<LAYOUT>(l, a.turn.rotary_dim);
+    const int chunks = block / 16, groups = a.q ? ceil_div(lp.H, 8) : 0, units = 2 * lp.Hkv + 8 * groups, stride = kAppendWaves * share;
+    // a row: its token (held back inside the block's tokens), its head, whether it is there at all
+    struct Row {
+        int t, head, there;
+    };
+    auto row_of = [&](int u, int c, int half) {
+        int t, h;
+        if (u < 2 * lp.Hkv) {
+            t = lo + 16 * c + 8 * half + r;
+            h = u < lp.Hkv ? u : u - lp.Hkv;
+        } else {
+            const int i = u - 2 * lp.Hkv;
+            t = lo + (i / groups * chunks + c) * 2 + half;
+            h = i % groups * 8 + r;
+        }
+        const int held = min(max(t, t0), t1 - 1), head = u < 2 * lp.Hkv ? h : min(h, lp.H - 1);
+        return Row{held, head, t == held && h == head};
+    };
+    auto ask = [&](int u, int c, uint32_t (&x)[2][4], uint32_t (&y)[2][4]) {
+        const void* from = u >= 2 * lp.Hkv ? a.q : u >= lp.Hkv ? a.v : a.k;
+        const long long apart = u >= 2 * lp.Hkv ? a.q_stride : u >= lp.Hkv ? a.v_stride : a.k_stride;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const Row row = row_of(u, c, half);
+            load_pieces(from, (size_t)(src0 + row.t - s) * apart + row.head * kHeadDim, p, x[half], y[half]);
+        }
+    };
+    int u = wave + kAppendWaves * part, c = 0;
+    uint32_t x[2][4], y[2][4], next_x[2][4], next_y[2][4];
+    ask(min(u, units - 1), 0, x, y);
 
     const int pairs = a.turn.rotary_dim / 2;
     if (lane < pairs) {
@@ -167,93 +183,117 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
     }
     __syncthreads();
 
-    const int l = lane % 8, r = lane / 8;
-    const Pieces p = pieces_of<LAYOUT>(l, a.turn.rotary_dim);
-    float* room = reinterpret_cast<float*>(lds + block * kTurnRow) + (wave * 8 + r) * kHeadDim;
-    const int page = lo / lp.NP, heads_q = a.q ? lp.H : 0;
-    const int rows = min(lp.NL, 8);  // of a logical page among the eight rows in hand
-    auto turn_it = [&](uint32_t (&x)[4], uint32_t (&y)[4], int t, const float* weight) {
-        float2 turn[8];
-        const float2* row = lds + (t - lo) * kTurnRow;
-        if constexpr (LAYOUT != kOddHalves) read_turns(row, l, turn);
-        turn_row<T, LAYOUT>(x, y, turn, a.turn, weight, p, room, row);
-    };
-
-    for (int u = wave + kAppendWaves * part; u < 2 * lp.Hkv + heads_q; u += kAppendWaves * share) {
-        if (u >= 2 * lp.Hkv) {  // queries
-            const int h = u - 2 * lp.Hkv;
-            const float* weight = a.turn.q_weight ? a.turn.q_weight + (size_t)h * a.turn.weight_step : nullptr;
-            for (int j = 0; j < block; j += 8) {
-                const int t = lo + j + r, held = min(max(t, t0), t1 - 1);
-                const size_t src = (size_t)(src0 + held - s);
-                uint32_t x[4], y[4];
-                load_pieces<T>(a.q, src * a.q_stride + h * kHeadDim, p, x, y);
-                turn_it(x, y, held, weight);
-                if (t == held) store_pieces(a.q_out, (src * lp.H + h) * kHeadDim, p, x, y);
-            }
-            continue;
-        }
-        const bool is_v = u >= lp.Hkv;
-        const int hk = is_v ? u - lp.Hkv : u;
-        const bool streaming = (lp.streaming_mask >> hk) & 1ull;
-        // bounded pool: only sink pages and those that are local once all new tokens are in
-        const bool kept = !in_stream_pool(lp, kv, hk) || page < lp.sink_pages || page >= ceil_div(e, lp.NP) - lp.local_pages;
-        void* dense = is_v ? a.v_out : a.k_out;
-        if (!kept && !dense) continue;
-        Slab slab = {};
-        if (kept) slab = slab_of(lp, kv, b, hk, page, BITS);
-        const float* weight = a.turn.k_weight ? a.turn.k_weight + (size_t)hk * a.turn.weight_step : nullptr;
-        RowRange<T> range_x, range_y;
-        for (int j = 0; j < block; j += 8) {
-            const int t = lo + j + r, held = min(max(t, t0), t1 - 1);
-            const bool there = t == held;
-            const size_t src = (size_t)(src0 + held - s);
-            uint32_t x[4], y[4];
-            load_pieces<T>(is_v ? a.v : a.k, src * (is_v ? a.v_stride : a.k_stride) + hk * kHeadDim, p, x, y);
-            if (!is_v) turn_it(x, y, held, weight);
-            if (there) {
-                if (kept) write_row<T, BITS>(is_v ? slab.v : slab.k, lp.NP, held - page * lp.NP, p, l, x, y);
-                if (dense) store_pieces(dense, (src * lp.Hkv + hk) * kHeadDim, p, x, y);
-            }
-            if (is_v || streaming) continue;
-            if (there) {
-                range_x.add(make_uint4(x[0], x[1], x[2], x[3]));
-                range_y.add(make_uint4(y[0], y[1], y[2], y[3]));
-            }
-            if ((j + 8) % lp.NL != 0 && lp.NL > 8) continue;
-            // a logical page ends here, or several do
-            float xh[8], xl[8], yh[8], yl[8];
-            auto larger_of = [](float u, float v) { return fmaxf(u, v); };
-            auto smaller_of = [](float u, float v) { return fminf(u, v); };
+    uint4* tile = reinterpret_cast<uint4*>(lds + block * kTurnRow) + wave * kTile;
+    float* room = reinterpret_cast<float*>(tile) + r * kHeadDim;
+    float high[2] = {-INFINITY, -INFINITY}, low[2] = {INFINITY, INFINITY};  // of the lane's two channels in a logical page
+    while (u < units) {
+        const bool is_q = u >= 2 * lp.Hkv, is_v = !is_q && u >= lp.Hkv;
+        const Row rows[2] = {row_of(u, c, 0), row_of(u, c, 1)};
+        const float* weight = !NORM || is_v ? nullptr : is_q ? a.turn.q_weight : a.turn.k_weight;
+        Weights w;  // (asked for ahead of the next rows: loads come back in order)
+        if (weight) weight += (size_t)rows[0].head * a.turn.weight_step;
+        if (NORM) load_weights(weight, p, w);
+        const int next_c = c + 1 < chunks ? c + 1 : 0, next_u = next_c ? u : u + stride;
+        ask(min(next_u, units - 1), next_c, next_x, next_y);
+        if (!is_v) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                xh[i] = over_rows(range_x.largest(i), rows, larger_of);
-                xl[i] = over_rows(range_x.smallest(i), rows, smaller_of);
-                yh[i] = over_rows(range_y.largest(i), rows, larger_of);
-                yl[i] = over_rows(range_y.smallest(i), rows, smaller_of);
+            for (int half = 0; half < 2; ++half) {
+                float2 turn[8];
+                const float2* turns = lds + (rows[half].t - lo) * kTurnRow;
+                if constexpr (LAYOUT != kOddHalves) read_turns(turns, l, turn);
+                turn_row<T, LAYOUT, NORM>(x[half], y[half], turn, a.turn, weight != nullptr, w, p, room, turns);
             }
-            const int first = t / lp.NL * lp.NL;  // of the row's logical page
-            if (r % rows == 0 && first < t1 && first + lp.NL > t0) {
-                uint4* stats = reinterpret_cast<uint4*>(kv.stats) + ((slab.page_head * lp.g + (first - page * lp.NP) / lp.NL) * 2) * (kHeadDim / 8);
-                write_range<T>(stats, p.p0, xh, xl, first < s);
-                write_range<T>(stats, p.p1, yh, yl, first < s);
+        }
+        if (is_q) {
+            arrived(next_x[0], next_y[0]);
+            arrived(next_x[1], next_y[1]);
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+                if (rows[half].there) store_pieces(a.q_out, ((size_t)(src0 + rows[half].t - s) * lp.H + rows[half].head) * kHeadDim, p, x[half], y[half]);
+        } else {
+            const int hk = is_v ? u - lp.Hkv : u;
+            // bounded pool: only sink pages and those that are local once all new tokens are in
+            const bool kept = !in_stream_pool(lp, kv, hk) || page < lp.sink_pages || page >= ceil_div(e, lp.NP) - lp.local_pages;
+            const bool scored = !is_v && !((lp.streaming_mask >> hk) & 1ull);
+            if (scored) {
+                // The rows change hands in LDS: two channels to a lane, so that a range is four registers and needs no other lane
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint4* to = tile + (8 * half + r) * (kHeadDim / 8);
+                    to[p.p0] = make_uint4(x[half][0], x[half][1], x[half][2], x[half][3]);
+                    to[p.p1] = make_uint4(y[half][0], y[half][1], y[half][2], y[half][3]);
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
-            range_x = RowRange<T>();
-            range_y = RowRange<T>();
+            const Stored<BITS> first_row = stored<T, BITS>(x[0], y[0]), second_row = stored<T, BITS>(x[1], y[1]);
+            arrived(next_x[0], next_y[0]);
+            arrived(next_x[1], next_y[1]);
+            void* dense = is_v ? a.v_out : a.k_out;
+            if (dense) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    if (rows[half].there) store_pieces(dense, ((size_t)(src0 + rows[half].t - s) * lp.Hkv + hk) * kHeadDim, p, x[half], y[half]);
+            }
+            const Slab slab = slab_of(lp, kv, pages, hk, BITS);
+            if (kept) {
+                uint4* to = is_v ? slab.v : slab.k;
+                if (rows[0].there) write_row<BITS>(to, lp.NP, in_page + rows[0].t - lo, p, l, first_row);
+                if (rows[1].there) write_row<BITS>(to, lp.NP, in_page + rows[1].t - lo, p, l, second_row);
+            }
+            if (scored) {
+                const int from = lo + 16 * c;
+                uint32_t keys[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) keys[i] = reinterpret_cast<const uint32_t*>(tile)[i * (kHeadDim / 2) + lane];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int t = from + i;
+                    if (t < t0 || t >= t1) continue;
+                    high[0] = fmaxf(high[0], Elem<T>::lo(keys[i]));
+                    high[1] = fmaxf(high[1], Elem<T>::hi(keys[i]));
+                    low[0] = fminf(low[0], Elem<T>::lo(keys[i]));
+                    low[1] = fminf(low[1], Elem<T>::hi(keys[i]));
+                    if ((t + 1) % lp.NL != 0 && t + 1 != t1) continue;
+                    // the logical page ends here, or the new tokens do
+                    const int first = t / lp.NL * lp.NL;
+                    uint32_t* stats = reinterpret_cast<uint32_t*>(kv.stats) + ((slab.page_head * lp.g + (first - page * lp.NP) / lp.NL) * 2) * (kHeadDim / 2) + lane;
+                    if (first < s) {  // it held tokens before
+                        high[0] = fmaxf(high[0], Elem<T>::lo(stats[0]));
+                        high[1] = fmaxf(high[1], Elem<T>::hi(stats[0]));
+                        low[0] = fminf(low[0], Elem<T>::lo(stats[kHeadDim / 2]));
+                        low[1] = fminf(low[1], Elem<T>::hi(stats[kHeadDim / 2]));
+                    }
+                    stats[0] = Elem<T>::pack(high[0], high[1]);
+                    stats[kHeadDim / 2] = Elem<T>::pack(low[0], low[1]);
+                    high[0] = high[1] = -INFINITY;
+                    low[0] = low[1] = INFINITY;
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (the next rows take the tile over)
+            }
+        }
+        u = next_u;
+        c = next_c;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[half][i] = next_x[half][i];
+                y[half][i] = next_y[half][i];
+            }
         }
     }
 }
 
 // At most one new token per sequence (a decode step): nothing but latency.  A wavefront has eight heads of one token, works out the token's angles, one
 // to a lane, and passes them round through LDS; all loads that depend on nothing but the position go out together.
-template <class T, int LAYOUT, int BITS>
-__global__ __launch_bounds__(kAppendThreads) void turned_step_kernel(TurnedAppendArgs a, int groups_q, int groups_kv) {
-    __shared__ float2 all_turns[kAppendWaves][kTurnRow];
-    __shared__ float rooms[LAYOUT == kOddHalves ? kAppendWaves * 8 : 1][kHeadDim];
+template <class T, int LAYOUT, int BITS, bool NORM>
+__global__ __launch_bounds__(kStepThreads) void turned_step_kernel(TurnedAppendArgs a, int groups_q, int groups_kv) {
+    __shared__ float2 all_turns[kStepWaves][kTurnRow];
+    __shared__ float rooms[LAYOUT == kOddHalves ? kStepWaves * 8 : 1][kHeadDim];
     const LayerParams& lp = a.lp;
     const PagedParams& kv = a.kv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, l = lane % 8, r = lane / 8;
-    const int groups = groups_q + 2 * groups_kv, unit = blockIdx.x * kAppendWaves + wave;
+    const int groups = groups_q + 2 * groups_kv, unit = blockIdx.x * kStepWaves + wave;
     const int b = unit / groups, group = unit % groups;
     if (b >= kv.batch) return;
     const int src = a.cu_new[b], s = a.start_pos[b];
@@ -266,7 +306,7 @@ __global__ __launch_bounds__(kAppendThreads) void turned_step_kernel(TurnedAppen
     const void* from = kind == 0 ? a.k : kind == 1 ? a.v : a.q;
     const long long stride = kind == 0 ? a.k_stride : kind == 1 ? a.v_stride : a.q_stride;
     uint32_t x[4], y[4];
-    load_pieces<T>(from, (size_t)src * stride + head * kHeadDim, p, x, y);
+    load_pieces(from, (size_t)src * stride + head * kHeadDim, p, x, y);
     if (kind != 1) {
         const int pairs = a.turn.rotary_dim / 2;
         float2* turns = all_turns[wave];
@@ -274,9 +314,11 @@ __global__ __launch_bounds__(kAppendThreads) void turned_step_kernel(TurnedAppen
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         float2 turn[8];
         if constexpr (LAYOUT != kOddHalves) read_turns(turns, l, turn);
-        const float* weight = kind == 2 ? a.turn.q_weight : a.turn.k_weight;
+        const float* weight = !NORM ? nullptr : kind == 2 ? a.turn.q_weight : a.turn.k_weight;
         if (weight) weight += (size_t)head * a.turn.weight_step;
-        turn_row<T, LAYOUT>(x, y, turn, a.turn, weight, p, rooms[LAYOUT == kOddHalves ? wave * 8 + r : 0], turns);
+        Weights w;
+        if (NORM) load_weights(weight, p, w);
+        turn_row<T, LAYOUT, NORM>(x, y, turn, a.turn, weight != nullptr, w, p, rooms[LAYOUT == kOddHalves ? wave * 8 + r : 0], turns);
     }
     if (!there) return;
     void* dense = kind == 0 ? a.k_out : kind == 1 ? a.v_out : a.q_out;
@@ -284,8 +326,8 @@ __global__ __launch_bounds__(kAppendThreads) void turned_step_kernel(TurnedAppen
     if (kind == 2) return;
     // the one new token is the last of its sequence, so its page is a local one: a bounded pool always keeps it
     const int page = s / lp.NP, slot = s - page * lp.NP;
-    const Slab slab = slab_of(lp, kv, b, head, page, BITS);
-    write_row<T, BITS>(kind == 0 ? slab.k : slab.v, lp.NP, slot, p, l, x, y);
+    const Slab slab = slab_of(lp, kv, pages_of(lp, kv, b, page), head, BITS);
+    write_row<BITS>(kind == 0 ? slab.k : slab.v, lp.NP, slot, p, l, stored<T, BITS>(x, y));
     if (kind == 1 || ((lp.streaming_mask >> head) & 1ull)) return;
     RowRange<T> range_x, range_y;
     range_x.add(make_uint4(x[0], x[1], x[2], x[3]));
@@ -307,26 +349,37 @@ __global__ __launch_bounds__(kAppendThreads) void turned_step_kernel(TurnedAppen
 
 namespace {
 
-template <class T, int LAYOUT, int BITS> hipError_t launch(const TurnedAppendArgs& a, hipStream_t stream) {
-    const dim3 threads(kAppendThreads);
+template <class T, int LAYOUT, int BITS, bool NORM> hipError_t launch(const TurnedAppendArgs& a, hipStream_t stream) {
     if (a.max_new == 1) {
         const int groups_q = a.q ? ceil_div(a.lp.H, 8) : 0, groups_kv = ceil_div(a.lp.Hkv, 8);
         const long long waves = (long long)a.kv.batch * (groups_q + 2 * groups_kv);
-        hipLaunchKernelGGL((turned_step_kernel<T, LAYOUT, BITS>), dim3((unsigned)((waves + kAppendWaves - 1) / kAppendWaves)), threads, 0, stream, a, groups_q,
+        hipLaunchKernelGGL((turned_step_kernel<T, LAYOUT, BITS, NORM>), dim3((unsigned)((waves + kStepWaves - 1) / kStepWaves)), dim3(kStepThreads), 0, stream, a, groups_q,
                            groups_kv);
         return hipGetLastError();
     }
     const int block = std::max(16, a.lp.NL);
     const long long blocks = a.total / block + 2LL * a.kv.batch;
-    const int units = 2 * a.lp.Hkv + (a.q ? a.lp.H : 0);
-    const int share = (int)std::max(1LL, std::min<long long>(ceil_div(units, kAppendWaves), 8LL * num_compute_units() / blocks));
-    const size_t lds = (size_t)block * kTurnRow * sizeof(float2) + (LAYOUT == kOddHalves ? kAppendWaves * 8 * kHeadDim * sizeof(float) : 0);
-    hipLaunchKernelGGL((turned_append_kernel<T, LAYOUT, BITS>), dim3((unsigned)(blocks * share)), threads, lds, stream, a, block, share);
+    const int units = 2 * a.lp.Hkv + (a.q ? 8 * ceil_div(a.lp.H, 8) : 0);
+    // Parts of a block: enough for three workgroups to a compute unit, as long as every wavefront has a unit; with plenty of blocks few, as each part works out
+    // the block's angles: with a norm, or where blocks are few all the same, four units to a wavefront, else two.  Two, three, four, six and twelve parts, us:
+    // 65536 tokens of 32 / 8 heads 315, 311, 309, 303, 302, with a norm 311, 301, 315, 311, 404; 8 x 512 25.9, 24.0, 24.8, 25.6, 25.6; one
+    // of 512 11.9, 10.5, 9.5, 8.8, 8.4, of 2000 13.8, 14.1, 12.9, 12.7, 15.0; 20000 of 64 / 8 165, 163, 160, 159, 152; 30000 into 4-bit pages 156, 148, 154,
+    // 149, 191.  (A number that leaves some wavefronts a unit more than others costs: eight parts of 48 units 321 where six took 305.)
+    const long long wanted = std::max<long long>(units / ((NORM || blocks < 4 * num_compute_units() ? 4 : 2) * kAppendWaves), 3LL * num_compute_units() / blocks);
+    const int most = (int)std::max(1LL, std::min<long long>(ceil_div(units, kAppendWaves), wanted));
+    const int each = ceil_div(units, kAppendWaves * most), share = ceil_div(units, kAppendWaves * each);  // as many to every wavefront
+    const size_t lds = (size_t)block * kTurnRow * sizeof(float2) + kAppendWaves * kTile * sizeof(uint4);
+    hipLaunchKernelGGL((turned_append_kernel<T, LAYOUT, BITS, NORM>), dim3((unsigned)(blocks * share)), dim3(kAppendThreads), lds, stream, a, block, share);
     return hipGetLastError();
 }
 
+template <class T, int LAYOUT, int BITS> hipError_t launch_norm(const TurnedAppendArgs& a, hipStream_t stream) {
+    return a.turn.norm ? launch<T, LAYOUT, BITS, true>(a, stream) : launch<T, LAYOUT, BITS, false>(a, stream);
+}
 template <class T, int LAYOUT> hipError_t launch_bits(const TurnedAppendArgs& a, hipStream_t stream) {
-    return a.kv.kv_bits == 8 ? launch<T, LAYOUT, 8>(a, stream) : a.kv.kv_bits == 4 ? launch<T, LAYOUT, 4>(a, stream) : launch<T, LAYOUT, 16>(a, stream);
+    return a.kv.kv_bits == 8   ? launch_norm<T, LAYOUT, 8>(a, stream)
+           : a.kv.kv_bits == 4 ? launch_norm<T, LAYOUT, 4>(a, stream)
+                               : launch_norm<T, LAYOUT, 16>(a, stream);
 }
 template <class T> hipError_t launch_layout(const TurnedAppendArgs& a, hipStream_t stream) {
     if (a.turn.interleaved) return launch_bits<T, kInterleaved>(a, stream);
@@ -337,7 +390,7 @@ template <class T> hipError_t launch_layout(const TurnedAppendArgs& a, hipStream
 
 hipError_t preload_rotary_append_kernels() {
     hipFuncAttributes attr;
-    return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&turned_step_kernel<F16, kHalves, 16>));
+    return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&turned_step_kernel<F16, kHalves, 16, false>));
 }
 
 hipError_t launch_turned_append(int dtype, const TurnedAppendArgs& a, hipStream_t stream) {
