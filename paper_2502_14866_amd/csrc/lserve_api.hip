@@ -4,6 +4,7 @@
 #include "../../include/lserve.h"
 
 #include <cmath>
+#include <iterator>
 #include <mutex>
 
 #include "kernels.h"
@@ -741,14 +742,15 @@ int lserve_rotary_append_kv(const lserve_attn_desc* desc, const lserve_paged_kv*
                              {kv->v_pool, main * slab}, {a.kv.k_stream, bounded * slab}, {a.kv.v_stream, bounded * slab},
                              {selecting > 0 ? kv->stats : nullptr, main * a.lp.g * 4 * kHeadDim}};
     for (const Range& o : written) {
+        if (!o.at) continue;
         for (const Range& i : in)
             if (meet(o, i)) return LSERVE_ERR_INVALID_ARG;
         for (const Rows& i : rows) {
             const bool in_place = o.at && o.at == i.at && ((&i == &rows[0] && &o == &written[0]) || (&i == &rows[1] && &o == &written[1]));
             if (!in_place && i.at && meet(o, i)) return LSERVE_ERR_INVALID_ARG;
         }
-        for (const Range& other : written)
-            if (&other != &o && meet(o, other)) return LSERVE_ERR_INVALID_ARG;
+        for (const Range* other = &o + 1; other != std::end(written); ++other)
+            if (meet(o, *other)) return LSERVE_ERR_INVALID_ARG;
     }
     a.q = q;
     a.k = k;

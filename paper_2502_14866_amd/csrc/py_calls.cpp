@@ -95,12 +95,17 @@ struct Attribute {
 enum { kKPool, kVPool, kStats, kPageTable, kSeqLens, kPoolHeads, kKStream, kVStream, kRingTable, kBits, kNames };
 PyObject* names[kNames];
 
-// binding.PagedKV as lserve_paged_kv.  (The tensors stay alive: the caller holds the object.)
-lserve_paged_kv paged(PyObject* kv) {
+// The tensors of a PagedKV, for what is checked of them.  (They stay alive: the caller holds the object.)
+struct PagedTensors {
+    const at::Tensor *k, *v, *stats, *table, *lens, *k_stream, *v_stream, *ring;
+};
+// binding.PagedKV as lserve_paged_kv.
+lserve_paged_kv paged(PyObject* kv, PagedTensors* tensors = nullptr) {
     const Attribute k(kv, names[kKPool]), v(kv, names[kVPool]), st(kv, names[kStats]), table(kv, names[kPageTable]), lens(kv, names[kSeqLens]),
         heads(kv, names[kPoolHeads]), ks(kv, names[kKStream]), vs(kv, names[kVStream]), ring(kv, names[kRingTable]), bits(kv, names[kBits]);
     const at::Tensor *kt = tensor_or_null(k.o), *vt = tensor_or_null(v.o), *stt = tensor_or_null(st.o), *tt = tensor_or_null(table.o),
-                     *kst = tensor_or_null(ks.o);
+                     *kst = tensor_or_null(ks.o), *lt = tensor_or_null(lens.o), *vst = tensor_or_null(vs.o), *rt = tensor_or_null(ring.o);
+    if (tensors) *tensors = {kt, vt, stt, tt, lt, kst, vst, rt};
     const at::Tensor* sized = stt ? stt : vt ? vt : kt;
     if (!tt) {
         PyErr_SetString(PyExc_TypeError, "PagedKV.page_table is None");
@@ -111,14 +116,14 @@ lserve_paged_kv paged(PyObject* kv) {
     p.v_pool = address(vt);
     p.stats = address(stt);
     p.page_table = address<int32_t>(tt);
-    p.seq_lens = address<int32_t>(lens.o);
+    p.seq_lens = address<int32_t>(lt);
     p.batch = (int32_t)tt->size(0);
     p.max_pages_per_seq = (int32_t)tt->size(1);
     p.num_pages = sized ? (int32_t)sized->size(0) : 0;
     p.pool_heads = number32(heads.o);
     p.k_pool_stream = address(kst);
-    p.v_pool_stream = address(vs.o);
-    p.ring_table = address<int32_t>(ring.o);
+    p.v_pool_stream = address(vst);
+    p.ring_table = address<int32_t>(rt);
     p.num_pages_stream = kst ? (int32_t)kst->size(0) : 0;
     p.kv_bits = number32(bits.o);
     return p;
@@ -330,9 +335,8 @@ PyObject* py_rotary_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 19, [&] {
         const char* where = "lserve_rotary_append_kv";
         const lserve_attn_desc* desc = description(a[0]);
-        const lserve_paged_kv kv = paged(a[1]);
-        const Held table(a[1], kPageTable), ring_table(a[1], kRingTable), k_pool(a[1], kKPool), v_pool(a[1], kVPool), k_stream(a[1], kKStream),
-            v_stream(a[1], kVStream), stats(a[1], kStats);
+        PagedTensors held;
+        const lserve_paged_kv kv = paged(a[1], &held);
         const Turn turn(desc, a + 2);
         const at::Tensor *q = tensor_or_null(a[8]), *k = tensor_or_null(a[9]), *v = tensor_or_null(a[10]), *pos = tensor_or_null(a[11]),
                          *cu = tensor_or_null(a[12]), *start = tensor_or_null(a[13]), *qo = tensor_or_null(a[15]), *ko = tensor_or_null(a[16]),
@@ -345,19 +349,19 @@ PyObject* py_rotary_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::ScalarType t = type_of(desc);
         const bool rows16 = kv.kv_bits == 0 || kv.kv_bits == 16, codes = kv.kv_bits == 8 || kv.kv_bits == 4;
         const int64_t slab = rows16 ? (int64_t)desc->page_size * dim : codes ? 8 * dim * kv.kv_bits + 256 : 0;
-        auto kind = [&](const Held& pool) { return rows16 ? t : codes || (pool.t && pool.t->scalar_type() == at::kByte) ? at::kByte : t; };
+        auto kind = [&](const at::Tensor* pool) { return rows16 ? t : codes || (pool && pool->scalar_type() == at::kByte) ? at::kByte : t; };
         int64_t streaming = 0;
         for (int64_t h = 0; h < hkv; ++h) streaming += desc->kv_head_is_streaming[h] != 0;
-        const int64_t streams = k_stream.t ? streaming : 0;
+        const int64_t streams = held.k_stream ? streaming : 0;
         // (all heads in the bounded pool: nothing of the main one)
         const int64_t heads = streams < hkv ? (int64_t)kv.num_pages * (kv.pool_heads ? kv.pool_heads : hkv) : 0;
         const int64_t pool = heads * slab, bounded = kv.num_pages_stream * streams * slab;
         const int64_t spans = streaming < hkv && desc->logical_page_size > 0 ? heads * (desc->page_size / desc->logical_page_size) * 2 * dim : 0;
         check(where, {{turn.q_weight, kFloat, turn.q_least}, {turn.k_weight, kFloat, turn.k_least}, {turn.freq, kDouble, turn.freq_least},
                       {q, t, total * hq * dim}, {k, t, total * hkv * dim}, {v, t, total * hkv * dim}, {pos, kInt, 1}, {cu, kInt, batch + 1},
-                      {start, kInt, batch}, {qo, t, total * hq * dim}, {ko, t, total * hkv * dim}, {vo, t, total * hkv * dim}, {table.t, kInt, 0},
-                      {k_pool.t, kind(k_pool), pool}, {v_pool.t, kind(v_pool), pool}, {k_stream.t, kind(k_stream), bounded},
-                      {v_stream.t, kind(v_stream), bounded}, {stats.t, t, spans}, {ring_table.t, kInt, k_stream.t ? batch * ring_of(desc) : 0}});
+                      {start, kInt, batch}, {qo, t, total * hq * dim}, {ko, t, total * hkv * dim}, {vo, t, total * hkv * dim}, {held.table, kInt, 0},
+                      {held.k, kind(held.k), pool}, {held.v, kind(held.v), pool}, {held.k_stream, kind(held.k_stream), bounded},
+                      {held.v_stream, kind(held.v_stream), bounded}, {held.stats, t, spans}, {held.ring, kInt, held.k_stream ? batch * ring_of(desc) : 0}});
         const int32_t *p_cu = address<int32_t>(cu), *p_start = address<int32_t>(start), longest = number32(a[14]);
         void *p_qo = address(qo), *p_ko = address(ko), *p_vo = address(vo), *stream = stream_handle(a[18]);
         const WithoutLock w;

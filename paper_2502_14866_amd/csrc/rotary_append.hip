@@ -15,28 +15,14 @@ namespace {
 constexpr int kAppendThreads = 256, kAppendWaves = kAppendThreads / kWave;
 constexpr int kStepThreads = 256, kStepWaves = kStepThreads / kWave;
 
-// Writes the ranges of eight channels into the statistics rows of a logical page, with what they hold taken in if it held tokens before.
-template <class T>
-__device__ __forceinline__ void write_range(uint4* stats, int piece, const float (&high)[8], const float (&low)[8], bool held) {
-    float h[8], l[8];
+// Larger (or smaller) of eight pairs of channels, as numbers, in the type that they are in.  (What is not a number gives way: to the other, or to nothing.)
+template <class T, bool LARGER> __device__ __forceinline__ uint4 further(const uint32_t (&x)[4], const uint4& y4) {
+    const uint32_t y[4] = {y4.x, y4.y, y4.z, y4.w};
+    uint32_t out[4];
+    auto of = [](float a, float b) { return LARGER ? fmaxf(fmaxf(-INFINITY, a), b) : fminf(fminf(INFINITY, a), b); };
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        h[i] = high[i];
-        l[i] = low[i];
-    }
-    if (held) {
-        const uint4 om = stats[piece], on = stats[kHeadDim / 8 + piece];
-        const uint32_t wm[4] = {om.x, om.y, om.z, om.w}, wn[4] = {on.x, on.y, on.z, on.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h[2 * i] = fmaxf(h[2 * i], Elem<T>::lo(wm[i]));
-            h[2 * i + 1] = fmaxf(h[2 * i + 1], Elem<T>::hi(wm[i]));
-            l[2 * i] = fminf(l[2 * i], Elem<T>::lo(wn[i]));
-            l[2 * i + 1] = fminf(l[2 * i + 1], Elem<T>::hi(wn[i]));
-        }
-    }
-    stats[piece] = make_uint4(Elem<T>::pack(h[0], h[1]), Elem<T>::pack(h[2], h[3]), Elem<T>::pack(h[4], h[5]), Elem<T>::pack(h[6], h[7]));
-    stats[kHeadDim / 8 + piece] = make_uint4(Elem<T>::pack(l[0], l[1]), Elem<T>::pack(l[2], l[3]), Elem<T>::pack(l[4], l[5]), Elem<T>::pack(l[6], l[7]));
+    for (int i = 0; i < 4; ++i) out[i] = Elem<T>::pack(of(Elem<T>::lo(x[i]), Elem<T>::lo(y[i])), of(Elem<T>::hi(x[i]), Elem<T>::hi(y[i])));
+    return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
 // Where the rows of a KV head of a page go.
@@ -307,6 +293,22 @@ __global__ __launch_bounds__(kStepThreads) void turned_step_kernel(TurnedAppendA
     const long long stride = kind == 0 ? a.k_stride : kind == 1 ? a.v_stride : a.q_stride;
     uint32_t x[4], y[4];
     load_pieces(from, (size_t)src * stride + head * kHeadDim, p, x, y);
+    // the one new token is the last of its sequence, so its page is a local one: a bounded pool always keeps it
+    const int page = s / lp.NP, slot = s - page * lp.NP, j = slot / lp.NL;
+    Slab slab = {};
+    uint4* stats = nullptr;
+    uint4 old[4] = {};  // what the logical page's rows hold: largest of either piece, smallest
+    const bool held = slot - j * lp.NL != 0;
+    if (kind != 2) {
+        slab = slab_of(lp, kv, pages_of(lp, kv, b, page), head, BITS);
+        if (kind == 0 && there && !((lp.streaming_mask >> head) & 1ull)) {
+            stats = reinterpret_cast<uint4*>(kv.stats) + ((slab.page_head * lp.g + j) * 2) * (kHeadDim / 8);
+            if (held) {
+                old[0] = stats[p.p0], old[1] = stats[p.p1];
+                old[2] = stats[kHeadDim / 8 + p.p0], old[3] = stats[kHeadDim / 8 + p.p1];
+            }
+        }
+    }
     if (kind != 1) {
         const int pairs = a.turn.rotary_dim / 2;
         float2* turns = all_turns[wave];
@@ -324,27 +326,13 @@ __global__ __launch_bounds__(kStepThreads) void turned_step_kernel(TurnedAppendA
     void* dense = kind == 0 ? a.k_out : kind == 1 ? a.v_out : a.q_out;
     if (dense) store_pieces(dense, ((size_t)src * heads + head) * kHeadDim, p, x, y);
     if (kind == 2) return;
-    // the one new token is the last of its sequence, so its page is a local one: a bounded pool always keeps it
-    const int page = s / lp.NP, slot = s - page * lp.NP;
-    const Slab slab = slab_of(lp, kv, pages_of(lp, kv, b, page), head, BITS);
     write_row<BITS>(kind == 0 ? slab.k : slab.v, lp.NP, slot, p, l, stored<T, BITS>(x, y));
-    if (kind == 1 || ((lp.streaming_mask >> head) & 1ull)) return;
-    RowRange<T> range_x, range_y;
-    range_x.add(make_uint4(x[0], x[1], x[2], x[3]));
-    range_y.add(make_uint4(y[0], y[1], y[2], y[3]));
-    float xh[8], xl[8], yh[8], yl[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        xh[i] = range_x.largest(i);
-        xl[i] = range_x.smallest(i);
-        yh[i] = range_y.largest(i);
-        yl[i] = range_y.smallest(i);
-    }
-    const int j = slot / lp.NL;
-    const bool held = slot - j * lp.NL != 0;
-    uint4* stats = reinterpret_cast<uint4*>(kv.stats) + ((slab.page_head * lp.g + j) * 2) * (kHeadDim / 8);
-    write_range<T>(stats, p.p0, xh, xl, held);
-    write_range<T>(stats, p.p1, yh, yl, held);
+    if (!stats) return;
+    const uint4 x4 = make_uint4(x[0], x[1], x[2], x[3]), y4 = make_uint4(y[0], y[1], y[2], y[3]);
+    stats[p.p0] = further<T, true>(x, held ? old[0] : x4);
+    stats[p.p1] = further<T, true>(y, held ? old[1] : y4);
+    stats[kHeadDim / 8 + p.p0] = further<T, false>(x, held ? old[2] : x4);
+    stats[kHeadDim / 8 + p.p1] = further<T, false>(y, held ? old[3] : y4);
 }
 
 namespace {
