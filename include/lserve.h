@@ -525,7 +525,7 @@ int lserve_rotary_axes(const lserve_attn_desc *desc, const lserve_rotary_desc *r
 typedef struct lserve_head_norm {
     int32_t kind;           /* LSERVE_NORM_* */
     int32_t per_head;       /* 0: weights [D], the same for all heads; 1: [H][D] and [Hkv][D] */
-    float eps;              /* > 0 */
+    float eps;              /* > 0, no subnormal number */
     const float *q_weight;  /* device, 16-byte aligned, or NULL: ones */
     const float *k_weight;
 } lserve_head_norm;

@@ -5,6 +5,7 @@
 
 #include <cmath>
 #include <iterator>
+#include <limits>
 #include <mutex>
 
 #include "kernels.h"
@@ -177,7 +178,7 @@ int make_turn(const LayerParams& lp, const lserve_head_norm* norm, const lserve_
               const int32_t* positions, int64_t positions_stride, int total, bool own_places, TurnArgs* t) {
     if (norm) {
         if ((norm->kind != LSERVE_NORM_RMS && norm->kind != LSERVE_NORM_CENTRED) || (norm->per_head != 0 && norm->per_head != 1)) return LSERVE_ERR_INVALID_ARG;
-        if (!(norm->eps > 0.f) || std::isinf(norm->eps) || !aligned16(norm->q_weight) || !aligned16(norm->k_weight)) return LSERVE_ERR_INVALID_ARG;
+        if (!(norm->eps >= std::numeric_limits<float>::min()) || std::isinf(norm->eps) || !aligned16(norm->q_weight) || !aligned16(norm->k_weight)) return LSERVE_ERR_INVALID_ARG;
         t->norm = norm->kind == LSERVE_NORM_RMS ? 1 : 2;
         t->weight_step = norm->per_head ? kHeadDim : 0;
         t->eps = norm->eps;

@@ -130,7 +130,8 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
     const Pages pages = pages_of(lp, kv, b, page);
     const int l = lane % 8, r = lane / 8;
     const Pieces p = pieces_of<LAYOUT>(l, a.turn.rotary_dim);
-    const int chunks = block / 16, groups = a.q ? ceil_div(lp.H, 8) : 0, units = 2 * lp.Hkv + 8 * groups, stride = kAppendWaves * share;
+    const int chunks = block / 16, groups = a.q ? ceil_div(lp.H, 8) : 0, stride = kAppendWaves * share;
+    const int units = 2 * lp.Hkv + groups * ceil_div(t1 - t0, 2 * chunks);  // (queries: of the tokens that there are)
     // a row: its token (held back inside the block's tokens), its head, whether it is there at all
     struct Row {
         int t, head, there;
@@ -142,10 +143,10 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
             h = u < lp.Hkv ? u : u - lp.Hkv;
         } else {
             const int i = u - 2 * lp.Hkv;
-            t = lo + (i / groups * chunks + c) * 2 + half;
+            t = t0 + (i / groups * chunks + c) * 2 + half;
             h = i % groups * 8 + r;
         }
-        const int held = min(max(t, t0), t1 - 1), head = u < 2 * lp.Hkv ? h : min(h, lp.H - 1);
+        const int held = min(max(t, t0), t1 - 1), head = min(h, lp.H - 1);
         return Row{held, head, t == held && h == head};
     };
     auto ask = [&](int u, int c, uint32_t (&x)[2][4], uint32_t (&y)[2][4]) {
@@ -347,7 +348,8 @@ template <class T, int LAYOUT, int BITS, bool NORM> hipError_t launch(const Turn
     }
     const int block = std::max(16, a.lp.NL);
     const long long blocks = a.total / block + 2LL * a.kv.batch;
-    const int units = 2 * a.lp.Hkv + (a.q ? 8 * ceil_div(a.lp.H, 8) : 0);
+    const int each_seq = std::min(block, ceil_div(a.total, a.kv.batch));  // tokens of a block, where sequences are alike
+    const int units = 2 * a.lp.Hkv + (a.q ? ceil_div(a.lp.H, 8) * ceil_div(8 * each_seq, block) : 0);
     // Parts of a block: enough for three workgroups to a compute unit, as long as every wavefront has a unit; with plenty of blocks few, as each part works out
     // the block's angles: with a norm, or where blocks are few all the same, four units to a wavefront, else two.  Two, three, four, six and twelve parts, us:
     // 65536 tokens of 32 / 8 heads 315, 311, 309, 303, 302, with a norm 311, 301, 315, 311, 404; 8 x 512 25.9, 24.0, 24.8, 25.6, 25.6; one

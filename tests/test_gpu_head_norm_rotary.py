@@ -178,6 +178,7 @@ def test_rows_of_all_sizes(norm):
             _run(torch.float16, tokens, 128, False, norm=norm, rows=rows, eps=eps)
         _run(torch.bfloat16, tokens, 128, True, norm=norm, rows=rows * 1e12)
         _run(torch.bfloat16, tokens, 64, False, norm=norm, rows=rows * 1e-12, eps=1e-30)
+        _run(torch.float16, tokens, 128, False, norm=norm, rows=rows, eps=2e-38)
 
 
 def test_infinite_and_missing_numbers_stay_in_their_row():

@@ -100,7 +100,7 @@ def _norm(**kw):
 @pytest.mark.parametrize("bad,code", [(dict(rotary=r), c) for r, c in ROTARY] + [
     (dict(norm=_c_norm(kind=2)), -1), (dict(norm=_c_norm(kind=-1)), -1), (dict(norm=_c_norm(per_head=2)), -1), (dict(norm=L.HeadNorm(eps=0.0)), -1),
     (dict(norm=L.HeadNorm(eps=-1e-6)), -1), (dict(norm=L.HeadNorm(eps=math.nan)), -1), (dict(norm=L.HeadNorm(eps=math.inf)), -1),
-    (dict(norm=L.HeadNorm(eps=1e-50)), -1),  # zero in 32 bits
+    (dict(norm=L.HeadNorm(eps=1e-50)), -1), (dict(norm=L.HeadNorm(eps=1e-39)), -1),  # zero in 32 bits, a subnormal number
     (dict(norm=L.HeadNorm(_off_by(128, (128,)), None)), -1), (dict(norm=L.HeadNorm(None, _off_by(128, (128,)))), -1),
     (dict(positions=None), -1), (dict(rotary=None, axes=AXES, positions=i32(3, 3)), -1), (dict(q=None), -1), (dict(k_out=None), -1),
 ])
