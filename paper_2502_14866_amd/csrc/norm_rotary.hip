@@ -35,15 +35,15 @@ __device__ __forceinline__ int place_of(const TurnArgs& t, int token, int pair) 
 
 // Eight lanes to a head, eight heads at a time (rotary.h).  A wavefront has `tokens` neighbouring tokens, or one of `share` parts of the heads of one; their
 // angles are worked out one to a lane and passed round through LDS, and the next eight heads are in flight while it works on eight.
-template <class T, bool INTERLEAVED, bool NORM>
+template <class T, int LAYOUT, bool NORM>
 __global__ __launch_bounds__(kRowThreads) void turned_rows_kernel(TurnedRowsArgs a, int tokens, int share, int heads_inverse) {
-    constexpr int kLayout = INTERLEAVED ? kInterleaved : kHalves;
-    extern __shared__ float2 all_turns[];  // [wavefronts][tokens][kTurnRow]; behind the angles of a token, whether it is there
+    extern __shared__ float2 all_turns[];  // [wavefronts][tokens][kTurnRow]; behind the angles of a token, whether it is there; for kOddHalves rows in 32 bits
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int unit = blockIdx.x * kRowWaves + wave, t0 = unit / share * tokens, part = unit % share;
     if (t0 >= a.total) return;
     float2* turns = all_turns + wave * tokens * kTurnRow;
-    const Pieces p = pieces_of<kLayout>(lane % 8, a.turn.rotary_dim);
+    float* room = reinterpret_cast<float*>(all_turns + kRowWaves * tokens * kTurnRow) + (wave * 8 + lane / 8) * kHeadDim;
+    const Pieces p = pieces_of<LAYOUT>(lane % 8, a.turn.rotary_dim);
     const int heads = a.heads_q + a.heads_k, here = min(tokens, a.total - t0), rows = here * heads, first = part * 8 + lane / 8;
     auto token_of = [&](int j) { return tokens == 1 ? 0 : j * heads_inverse >> 16; };  // j / heads
     auto row_of = [&](int j) {
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kRowThreads) void turned_rows_kernel(TurnedRowsArgs
     if (a.turn.positions) {
         for (int i = 0; i < here; ++i) {
             float2* to = turns + i * kTurnRow;
-            if (lane < a.turn.rotary_dim / 2) to[turn_place<kLayout>(lane)] = turn_of(place_of(a.turn, t0 + i, lane), a.turn.inv_freq[lane], a.turn.scale);
+            if (lane < a.turn.rotary_dim / 2) to[turn_place<LAYOUT>(lane)] = turn_of(place_of(a.turn, t0 + i, lane), a.turn.inv_freq[lane], a.turn.scale);
             if (lane == 0) to[kHeadDim / 2].x = a.turn.positions[t0 + i] < 0 ? 0.f : 1.f;  // (a row that is only there to fill up the batch)
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -69,8 +69,8 @@ __global__ __launch_bounds__(kRowThreads) void turned_rows_kernel(TurnedRowsArgs
         const NormedRow next = row_of(j + share * 8);
         load_pieces(next.from, 0, p, next_x, next_y);
         float2 turn[8];
-        read_turns(turns_of_row, lane % 8, turn);
-        turn_row<T, kLayout, NORM>(x, y, turn, a.turn, row.weight != nullptr, w, p, nullptr, nullptr);
+        if constexpr (LAYOUT != kOddHalves) read_turns(turns_of_row, lane % 8, turn);
+        turn_row<T, LAYOUT, NORM>(x, y, turn, a.turn, row.weight != nullptr, w, p, room, turns_of_row);
         arrived(next_x, next_y);
         if (there) store_pieces(row.to, 0, p, x, y);
         row = next;
@@ -138,9 +138,10 @@ namespace {
 
 template <class T> hipError_t launch(const TurnedRowsArgs& a, hipStream_t stream) {
     // Few rows: a launch takes as long as one wavefront does, and turned_pairs_kernel has no trip through LDS: 16 tokens of 40 heads 3.2 us against 3.6
-    // by rows, 64 3.4 to 3.6 either way, 128 4.3 against 3.6 and 256 5.2 against 4.0 (with a norm 3.2, 3.6, 3.6, 4.7, 3.8, 5.8 and 4.1).
+    // by rows, 64 3.4 to 3.6 either way, 128 4.3 against 3.6 and 256 5.2 against 4.0 (with a norm 3.2, 3.6, 3.6, 4.7, 3.8, 5.8 and 4.1).  Halves of 20 channels,
+    // whose rows pass through LDS: 500 tokens 7.7 us by pairs and 6.5 by rows, 5000 57.7 and 27.4, 60000 492 and 231.
     const int heads = a.heads_q + a.heads_k;
-    const bool rows = (a.turn.interleaved || a.turn.rotary_dim % 16 == 0) && (long long)a.total * heads > 12LL * num_compute_units();
+    const bool rows = (long long)a.total * heads > 12LL * num_compute_units();
     // Parts of a token: as many as it has groups of heads while there are few tokens.  With plenty, short wavefronts suit the memory better, long ones work
     // out fewer angles, which tells where a norm makes a group dearer.  One to five parts, us: 65536 tokens of five groups 246, 231, 235, 224, 232, with a
     // norm 243, 236, 246, 264, 272; 36000 of nine 255, 246, 241, 238, 237 (seven 227), with a norm 251, 237, 231, 234, 238; 40000 of eight 247, 238, 240,
@@ -154,16 +155,16 @@ template <class T> hipError_t launch(const TurnedRowsArgs& a, hipStream_t stream
     }
     const long long blocks = (((long long)a.total + tokens - 1) / tokens * share + kRowWaves - 1) / kRowWaves;
     const dim3 grid((unsigned)blocks), threads(kRowThreads);
-    const size_t lds = sizeof(float2) * kRowWaves * tokens * kTurnRow;
+    const int layout = a.turn.interleaved ? kInterleaved : a.turn.rotary_dim % 16 == 0 ? kHalves : kOddHalves;
+    const size_t lds = sizeof(float2) * kRowWaves * tokens * kTurnRow + (layout == kOddHalves ? sizeof(float) * kRowWaves * 8 * kHeadDim : 0);
     const int heads_inverse = 65536 / heads + 1;
-    if (rows && a.turn.interleaved && a.turn.norm)
-        hipLaunchKernelGGL((turned_rows_kernel<T, true, true>), grid, threads, lds, stream, a, tokens, share, heads_inverse);
-    else if (rows && a.turn.interleaved)
-        hipLaunchKernelGGL((turned_rows_kernel<T, true, false>), grid, threads, lds, stream, a, tokens, share, heads_inverse);
-    else if (rows && a.turn.norm)
-        hipLaunchKernelGGL((turned_rows_kernel<T, false, true>), grid, threads, lds, stream, a, tokens, share, heads_inverse);
+    auto by_rows = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, lds, stream, a, tokens, share, heads_inverse); };
+    if (rows && layout == kInterleaved)
+        a.turn.norm ? by_rows(turned_rows_kernel<T, kInterleaved, true>) : by_rows(turned_rows_kernel<T, kInterleaved, false>);
+    else if (rows && layout == kHalves)
+        a.turn.norm ? by_rows(turned_rows_kernel<T, kHalves, true>) : by_rows(turned_rows_kernel<T, kHalves, false>);
     else if (rows)
-        hipLaunchKernelGGL((turned_rows_kernel<T, false, false>), grid, threads, lds, stream, a, tokens, share, heads_inverse);
+        a.turn.norm ? by_rows(turned_rows_kernel<T, kOddHalves, true>) : by_rows(turned_rows_kernel<T, kOddHalves, false>);
     else if (a.turn.interleaved)
         hipLaunchKernelGGL((turned_pairs_kernel<T, true>), grid, threads, 0, stream, a, share);
     else
@@ -175,7 +176,7 @@ template <class T> hipError_t launch(const TurnedRowsArgs& a, hipStream_t stream
 
 hipError_t preload_norm_rotary_kernels() {
     hipFuncAttributes attr;
-    return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&turned_rows_kernel<F16, false, false>));
+    return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&turned_rows_kernel<F16, kHalves, false>));
 }
 
 hipError_t launch_turned_rows(int dtype, const TurnedRowsArgs& a, hipStream_t stream) {

@@ -10,7 +10,7 @@ def _found(kernels, pattern):  # noqa: F811
 
 def test_no_scratch(kernels):  # noqa: F811
     found = _found(kernels, r"turned_(rows|pairs|append|step)_kernel")
-    assert len(found) == 2 * (2 * 2 + 2 + 2 * 3 * 3 * 2)  # types; layouts and norms of rows, layouts of pairs; layouts, bits and norms of the other two
+    assert len(found) == 2 * (3 * 2 + 2 + 2 * 3 * 3 * 2)  # types; layouts and norms of rows, layouts of pairs; layouts, bits and norms of the other two
     assert all(k[".private_segment_fixed_size"] == 0 for k in found.values())
 
 
