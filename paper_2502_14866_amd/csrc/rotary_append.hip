@@ -159,8 +159,8 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
         }
     };
     int u = wave + kAppendWaves * part, c = 0;
-    uint32_t x[2][4], y[2][4], next_x[2][4], next_y[2][4];
-    ask(min(u, units - 1), 0, x, y);
+    uint32_t x[2][4] = {}, y[2][4] = {}, next_x[2][4], next_y[2][4];
+    if (u < units) ask(u, 0, x, y);
 
     const int pairs = a.turn.rotary_dim / 2;
     if (lane < pairs) {
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
         if (weight) weight += (size_t)rows[0].head * a.turn.weight_step;
         if (NORM) load_weights(weight, p, w);
         const int next_c = c + 1 < chunks ? c + 1 : 0, next_u = next_c ? u : u + stride;
-        ask(min(next_u, units - 1), next_c, next_x, next_y);
+        ask(next_u < units ? next_u : u, next_u < units ? next_c : c, next_x, next_y);  // (its own once more behind its last unit: no branch)
         if (!is_v) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
