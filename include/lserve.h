@@ -531,8 +531,8 @@ typedef struct lserve_head_norm {
 } lserve_head_norm;
 
 /*
- * Norm and rotary position of queries and keys in one pass: normed, then turned, both in fp32, and rounded once.  (Weights of ones and whole heads that
- * turn with a factor of 1: the norm may as well come after the turn, which it commutes with for m = 0.)
+ * Norm and rotary position of queries and keys in one pass: normed, then turned, both in fp32, and rounded once.  (With weights of ones, m = 0 and a
+ * factor of 1 on what turns this is also the norm after the turn.)
  *   norm       required
  *   rotary     NULL: nothing turns (a layer without positions); positions may then be NULL too
  *   axes       NULL: one axis, positions [total] as in lserve_rotary, positions_stride is not looked at

@@ -1,6 +1,6 @@
 // New tokens on their way from a projection into the paged cache: queries normed and turned, keys normed, turned and written to their pages
-// (16-bit rows or codes) with the key statistics brought up to date, values written next to them.  What it leaves in the cache is what
-// lserve_append_kv would be handed the turned keys for.  Bound: HBM, every row read once, queries and pages written once: 65536 tokens of 32 / 8 heads, 1.62 GB
+// (16-bit rows or codes) with the key statistics brought up to date, values written next to them.  The cache is left as lserve_append_kv would
+// leave it, handed the turned keys.  Bound: HBM, every row read once, queries and pages written once: 65536 tokens of 32 / 8 heads, 1.62 GB
 // with 16-bit pages, 300 us = 5.4 TB/s (a copy of 671 MiB runs at 5.3); eight of 512 to 8192 into 8-bit pages with dense keys and values kept, 618 MB, 120
 // us; 16 single tokens 4.2 us, which is a launch and the loads of a place, an angle, a row and a page one after the other.
 #include <algorithm>
@@ -35,7 +35,9 @@ struct Pages {
     int main, ring;
 };
 __device__ __forceinline__ Pages pages_of(const LayerParams& lp, const PagedParams& kv, int b, int p) {
-    return {kv.page_table[(size_t)b * kv.max_pages + p], kv.k_stream ? kv.ring_table[(size_t)b * kv.ring + ring_slot(lp, p)] : 0};
+    // (with every head in the ring the page table may be narrower than the sequence)
+    return {kv.k_stream && kv.stream_heads == lp.Hkv ? 0 : kv.page_table[(size_t)b * kv.max_pages + p],
+            kv.k_stream ? kv.ring_table[(size_t)b * kv.ring + ring_slot(lp, p)] : 0};
 }
 __device__ __forceinline__ Slab slab_of(const LayerParams& lp, const PagedParams& kv, const Pages& pages, int hk, int bits) {
     const bool ring = in_stream_pool(lp, kv, hk);

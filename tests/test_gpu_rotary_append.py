@@ -220,6 +220,28 @@ def test_a_step_written_as_more_than_one_token_at_most():
     _assert_same_cache(a, b)
 
 
+@pytest.mark.parametrize("counts", [[1, 1], [40, 150]])
+def test_a_page_table_narrower_than_the_ring_s_sequences(counts):
+    """A layer whose heads all stream through the ring keeps no pages elsewhere."""
+    L = _lib()
+    g = torch.Generator().manual_seed(6)
+    desc = L.AttnDesc(4, 2, [1, 1], sink_tokens=64, local_tokens=128)
+    pool = lambda: torch.zeros((6, 2, 64, 128), dtype=torch.float16, device=DEV)  # noqa: E731
+    start = torch.tensor([1000, 64 * 100000 + 5, 0, 0], dtype=torch.int32, device=DEV)[:2]
+    ring = torch.randperm(6, generator=g).to(torch.int32).view(2, 3).to(DEV)
+    none = torch.zeros((1, 2, 64, 128), dtype=torch.float16, device=DEV)
+    kv, twin = (L.PagedKV(none, none.clone(), None, torch.zeros((2, 1), dtype=torch.int32, device=DEV), start, k_pool_stream=pool(), v_pool_stream=pool(), ring_table=ring)
+                for _ in range(2))
+    _, (q, k, v) = _rows(g, torch.float16, sum(counts), 4, 2, True)
+    cu = torch.tensor([0, counts[0], sum(counts)], dtype=torch.int32, device=DEV)
+    qo, ko = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
+    L.lserve_rotary_append_kv(desc, kv, L.RotaryDesc(), q, k, v, cu, start, max(counts), qo, k_out=ko)
+    L.lserve_append_kv(desc, twin, ko, v.contiguous(), cu, start, max(counts))
+    torch.cuda.synchronize()
+    assert kv.k_pool_stream.any()
+    _assert_same_cache(kv, twin)
+
+
 @pytest.mark.parametrize("step", [False, True])
 def test_on_a_stream_of_its_own_and_captured(step):
     L = _lib()
