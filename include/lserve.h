@@ -547,6 +547,7 @@ int lserve_norm_rotary(const lserve_attn_desc *desc, const lserve_head_norm *nor
  * New tokens from a fused projection into the paged cache: queries are normed and turned into q_out; keys are normed, turned and, with the values, written to
  * the pages as lserve_append_kv writes them, the statistics of the turned keys included.  The cache afterwards holds what
  * lserve_append_kv would have written of the turned keys, rounded to the layer's type, and of the values (quantised pages: the codes of these rounded rows).
+ * What is not a number takes no part in a row's range or in statistics.
  * n_b = cu_new[b+1] - cu_new[b] >= 0 tokens of sequence b go to positions start_pos[b] + j of its pages.
  *
  *   norm       NULL: none

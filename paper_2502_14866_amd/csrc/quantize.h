@@ -185,12 +185,26 @@ __device__ __forceinline__ void quantize_row(const uint4& x, uint2& packed, uint
     scale_zero = row.pair;
 }
 
+// A value with a signalling not-a-number quieted, which the forms of three operands (v_min3, v_max3) would take for the range so far.  (Conversions
+// from fp16 have done so.  Written out: the compiler drops its own form as one that a minimum or maximum makes needless.)
+template <class T> __device__ __forceinline__ float quieted(float x) { return x; }
+template <> __device__ __forceinline__ float quieted<BF16>(float x) {
+    float r;
+    asm("v_max_f32 %0, %1, %1" : "=v"(r) : "v"(x));
+    return r;
+}
+
 // A row held by eight lanes, two pieces of eight features to a lane.
 template <class T, int BITS>
 __device__ __forceinline__ void quantize_pieces(const uint32_t (&x)[4], const uint32_t (&y)[4], uint2& x_codes, uint2& y_codes, uint32_t& scale_zero) {
     float f[8], g[8];
     unpack8<T>(x, f);
     unpack8<T>(y, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        f[i] = quieted<T>(f[i]);
+        g[i] = quieted<T>(g[i]);
+    }
     float lo, hi, lo_y, hi_y;
     range8<T>(x, f, lo, hi);
     range8<T>(y, g, lo_y, hi_y);

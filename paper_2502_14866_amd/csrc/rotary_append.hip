@@ -19,7 +19,7 @@ constexpr int kStepThreads = 256, kStepWaves = kStepThreads / kWave;
 template <class T, bool LARGER> __device__ __forceinline__ uint4 further(const uint32_t (&x)[4], const uint4& y4) {
     const uint32_t y[4] = {y4.x, y4.y, y4.z, y4.w};
     uint32_t out[4];
-    auto of = [](float a, float b) { return LARGER ? fmaxf(fmaxf(-INFINITY, a), b) : fminf(fminf(INFINITY, a), b); };
+    auto of = [](float a, float b) { return LARGER ? fmaxf(fmaxf(-INFINITY, quieted<T>(a)), b) : fminf(fminf(INFINITY, quieted<T>(a)), b); };
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = Elem<T>::pack(of(Elem<T>::lo(x[i]), Elem<T>::lo(y[i])), of(Elem<T>::hi(x[i]), Elem<T>::hi(y[i])));
     return make_uint4(out[0], out[1], out[2], out[3]);
@@ -238,19 +238,21 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
                 for (int i = 0; i < 16; ++i) {
                     const int t = from + i;
                     if (t < t0 || t >= t1) continue;
-                    high[0] = fmaxf(high[0], Elem<T>::lo(keys[i]));
-                    high[1] = fmaxf(high[1], Elem<T>::hi(keys[i]));
-                    low[0] = fminf(low[0], Elem<T>::lo(keys[i]));
-                    low[1] = fminf(low[1], Elem<T>::hi(keys[i]));
+                    const float first_channel = quieted<T>(Elem<T>::lo(keys[i])), second_channel = quieted<T>(Elem<T>::hi(keys[i]));
+                    high[0] = fmaxf(high[0], first_channel);
+                    high[1] = fmaxf(high[1], second_channel);
+                    low[0] = fminf(low[0], first_channel);
+                    low[1] = fminf(low[1], second_channel);
                     if ((t + 1) % lp.NL != 0 && t + 1 != t1) continue;
                     // the logical page ends here, or the new tokens do
                     const int first = t / lp.NL * lp.NL;
                     uint32_t* stats = reinterpret_cast<uint32_t*>(kv.stats) + ((slab.page_head * lp.g + (first - page * lp.NP) / lp.NL) * 2) * (kHeadDim / 2) + lane;
                     if (first < s) {  // it held tokens before
-                        high[0] = fmaxf(high[0], Elem<T>::lo(stats[0]));
-                        high[1] = fmaxf(high[1], Elem<T>::hi(stats[0]));
-                        low[0] = fminf(low[0], Elem<T>::lo(stats[kHeadDim / 2]));
-                        low[1] = fminf(low[1], Elem<T>::hi(stats[kHeadDim / 2]));
+                        const uint32_t most = stats[0], least = stats[kHeadDim / 2];
+                        high[0] = fmaxf(high[0], Elem<T>::lo(most));
+                        high[1] = fmaxf(high[1], Elem<T>::hi(most));
+                        low[0] = fminf(low[0], Elem<T>::lo(least));
+                        low[1] = fminf(low[1], Elem<T>::hi(least));
                     }
                     stats[0] = Elem<T>::pack(high[0], high[1]);
                     stats[kHeadDim / 2] = Elem<T>::pack(low[0], low[1]);
@@ -331,11 +333,15 @@ __global__ __launch_bounds__(kStepThreads) void turned_step_kernel(TurnedAppendA
     if (kind == 2) return;
     write_row<BITS>(kind == 0 ? slab.k : slab.v, lp.NP, slot, p, l, stored<T, BITS>(x, y));
     if (!stats) return;
-    const uint4 x4 = make_uint4(x[0], x[1], x[2], x[3]), y4 = make_uint4(y[0], y[1], y[2], y[3]);
-    stats[p.p0] = further<T, true>(x, held ? old[0] : x4);
-    stats[p.p1] = further<T, true>(y, held ? old[1] : y4);
-    stats[kHeadDim / 8 + p.p0] = further<T, false>(x, held ? old[2] : x4);
-    stats[kHeadDim / 8 + p.p1] = further<T, false>(y, held ? old[3] : y4);
+    if (!held) {  // nothing yet: infinities of either sign
+        const uint32_t inf = Elem<T>::pack(INFINITY, INFINITY), none = inf | 0x80008000u;
+        old[0] = old[1] = make_uint4(none, none, none, none);
+        old[2] = old[3] = make_uint4(inf, inf, inf, inf);
+    }
+    stats[p.p0] = further<T, true>(x, old[0]);
+    stats[p.p1] = further<T, true>(y, old[1]);
+    stats[kHeadDim / 8 + p.p0] = further<T, false>(x, old[2]);
+    stats[kHeadDim / 8 + p.p1] = further<T, false>(y, old[3]);
 }
 
 namespace {

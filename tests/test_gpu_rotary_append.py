@@ -1,8 +1,11 @@
 """Rows of a projection into the paged cache: queries and dense keys against the formulas in 64 bits, the cache against the write-back of these keys,
 byte for byte."""
+import numpy as np
 import pytest
 import torch
 
+from test_gpu_append_special import _expected
+from test_gpu_quant import _unpack_rows
 from turn_reference import assert_close, reference
 
 pytestmark = pytest.mark.gpu
@@ -218,6 +221,62 @@ def test_a_step_written_as_more_than_one_token_at_most():
     a = _run(torch.float16, [5, 64, 200], [1, 1, 1], norm=None)
     b = _run(torch.float16, [5, 64, 200], [1, 1, 1], norm=None, most=3)
     _assert_same_cache(a, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("counts", [[1, 1, 1], [40, 19, 64]])
+def test_rows_of_any_bits(dtype, bits, counts):
+    """Infinities, what is not a number, signalling or not, zeros of both signs: where nothing turns, the bytes that the formulas in numpy make of the same
+    rows.  A not-a-number takes no part in ranges and gets code 0."""
+    L = _lib()
+    g = torch.Generator().manual_seed(sum(counts))
+    desc = L.AttnDesc(4, 2, [0, 0], dtype=dtype)
+    lens = [7, 100, 64]
+    kv = _cache(L, g, dtype, desc, lens, counts, bits, False, 64)
+    before = kv.stats.float().cpu().numpy()
+    n = sum(counts)
+    k, v = (torch.randn((n, 2, 128), generator=g).to(dtype) for _ in range(2))
+    odd = torch.tensor([0x7c00, 0xfc00, 0x7e00, 0x7c01, 0xfe00, 0x8000, 0x0000, 0x0001, 0x7f80, 0xff80, 0x7fc0, 0x7f81, 0xffc0], dtype=torch.int32).to(torch.int16)
+    for t in (k, v):
+        bits_of = t.view(torch.int16).view(-1)
+        at = torch.randint(0, bits_of.numel(), (bits_of.numel() // 50,), generator=g)
+        bits_of[at] = odd[torch.randint(0, len(odd), at.shape, generator=g)]
+        t[0, 0] = 0.0
+        t[0, 0, ::2] = -0.0
+    cu = torch.tensor([0] + torch.tensor(counts).cumsum(0).tolist(), dtype=torch.int32)
+    ko, vo = torch.empty_like(k, device=DEV), torch.empty_like(v, device=DEV)
+    L.lserve_rotary_append_kv(desc, kv, None, None, k.to(DEV), v.to(DEV), cu.to(DEV), kv.seq_lens, max(counts), None, k_out=ko, v_out=vo)
+    torch.cuda.synchronize()
+    assert torch.equal(ko.view(torch.int16).cpu(), k.view(torch.int16)) and torch.equal(vo.view(torch.int16).cpu(), v.view(torch.int16))
+    table, stats = kv.page_table.cpu(), kv.stats.float().cpu().numpy()
+
+    def numbers(x):  # (a signalling not-a-number would take the place of what numpy's reductions held before it)
+        f = x.float().numpy()
+        return np.where(np.isnan(f), np.float32(np.nan), f)
+
+    for rows, pool in ((k, kv.k_pool.cpu()), (v, kv.v_pool.cpu())):
+        where = [(b, lens[b] + j, int(cu[b]) + j) for b in range(3) for j in range(counts[b])]
+        for h in range(2):
+            x = rows[[t for _, _, t in where], h]
+            slabs = [(pool[table[b, p // 64], h], p % 64) for b, p, _ in where]
+            if bits == 16:
+                assert torch.equal(torch.stack([s[i] for s, i in slabs]).view(torch.int16), x.view(torch.int16))
+                continue
+            codes, scale, zero = _expected(numbers(x), bits)
+            size = 128 * bits // 8
+            got = np.stack([_unpack_rows(s[:64 * size].numpy().reshape(64, size)[i:i + 1], bits)[0] for s, i in slabs])
+            pair = np.stack([s[64 * size:].numpy().view(np.float16).reshape(64, 2)[i] for s, i in slabs])
+            # (as numbers: the smallest of zeros of both signs is either)
+            assert np.array_equal(pair[:, 0], scale, equal_nan=True) and np.array_equal(pair[:, 1], zero, equal_nan=True)
+            assert np.array_equal(got, codes)
+    for b in range(3):  # statistics, logical page by logical page
+        for first in range(lens[b] // 16 * 16, lens[b] + counts[b], 16):
+            part = numbers(k[int(cu[b]) + max(first - lens[b], 0):int(cu[b]) + min(first + 16, lens[b] + counts[b]) - lens[b]])
+            at = table[b, first // 64], slice(None), first % 64 // 16
+            old = before[at] if first < lens[b] else np.stack([np.full((2, 128), -np.inf), np.full((2, 128), np.inf)], 1)
+            high, low = np.fmax(np.fmax.reduce(part, axis=0), old[:, 0]), np.fmin(np.fmin.reduce(part, axis=0), old[:, 1])
+            assert np.array_equal(stats[at][:, 0], high.astype(np.float32)) and np.array_equal(stats[at][:, 1], low.astype(np.float32)), (b, first)
 
 
 @pytest.mark.parametrize("counts", [[1, 1], [40, 150]])
