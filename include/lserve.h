@@ -560,7 +560,7 @@ int lserve_norm_rotary(const lserve_attn_desc *desc, const lserve_head_norm *nor
  *   cu_new     device [batch + 1] (batch = kv->batch), cu_new[0] = 0; rows from cu_new[batch] on are left alone, here and in all outputs
  *   start_pos  device [batch]; kv->seq_lens may be given.  kv->seq_lens itself is not read
  *   total_new  host: rows of q, k and v, and of the outputs
- *   max_new_per_seq  host bound of n_b, > 0; 1 (a decode step) has a form of its own
+ *   max_new_per_seq  host bound of n_b, > 0; 1 (a decode step) and a few (2, more in larger batches) have a form of their own
  *   q_out      device [total_new][H][D]; may be q itself where its rows are dense
  *   k_out, v_out  device [total_new][Hkv][D] or NULL: the turned keys, and the values, as dense rows too, for a prefill that reads them from there
  *              (also tokens that the streaming heads' ring does not keep).  k_out may be k itself where its rows are dense

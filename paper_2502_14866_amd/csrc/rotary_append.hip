@@ -275,8 +275,9 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
     }
 }
 
-// At most one new token per sequence (a decode step): nothing but latency.  A wavefront has eight heads of one token, works out the token's angles, one
-// to a lane, and passes them round through LDS; all loads that depend on nothing but the position go out together.
+// One new token per sequence (a decode step), or a few (drafted ones that were accepted): nothing but latency.  A wavefront has eight heads of a sequence and
+// takes its tokens one after the other; their angles are worked out one to a lane and passed round through LDS, and all loads that depend on nothing
+// but the position go out together.  The range of a logical page stays in the lanes from token to token.
 template <class T, int LAYOUT, int BITS, bool NORM>
 __global__ __launch_bounds__(kStepThreads) void turned_step_kernel(TurnedAppendArgs a, int groups_q, int groups_kv) {
     __shared__ float2 all_turns[kStepWaves][kTurnRow];
@@ -287,67 +288,85 @@ __global__ __launch_bounds__(kStepThreads) void turned_step_kernel(TurnedAppendA
     const int groups = groups_q + 2 * groups_kv, unit = blockIdx.x * kStepWaves + wave;
     const int b = unit / groups, group = unit % groups;
     if (b >= kv.batch) return;
-    const int src = a.cu_new[b], s = a.start_pos[b];
-    if (a.cu_new[b + 1] <= src || src >= a.total) return;  // no new token
+    const int src0 = a.cu_new[b], start = a.start_pos[b], n = min(a.cu_new[b + 1], a.total) - src0;
+    if (n <= 0) return;  // no new token
     const int kind = group < groups_kv ? 0 : group < 2 * groups_kv ? 1 : 2;  // keys, values, queries
     const int heads = kind == 2 ? lp.H : lp.Hkv, h = (group - kind * groups_kv) * 8 + r;
     const bool there = h < heads;
     const int head = there ? h : 0;
+    const bool scored = kind == 0 && there && !((lp.streaming_mask >> head) & 1ull);
     const Pieces p = pieces_of<LAYOUT>(l, a.turn.rotary_dim);
-    const void* from = kind == 0 ? a.k : kind == 1 ? a.v : a.q;
     const long long stride = kind == 0 ? a.k_stride : kind == 1 ? a.v_stride : a.q_stride;
-    uint32_t x[4], y[4];
-    load_pieces(from, (size_t)src * stride + head * kHeadDim, p, x, y);
-    // the one new token is the last of its sequence, so its page is a local one: a bounded pool always keeps it
-    const int page = s / lp.NP, slot = s - page * lp.NP, j = slot / lp.NL;
-    Slab slab = {};
-    uint4* stats = nullptr;
-    uint4 old[4] = {};  // what the logical page's rows hold: largest of either piece, smallest
-    const bool held = slot - j * lp.NL != 0;
-    if (kind != 2) {
-        slab = slab_of(lp, kv, pages_of(lp, kv, b, page), head, BITS);
-        if (kind == 0 && there && !((lp.streaming_mask >> head) & 1ull)) {
-            stats = reinterpret_cast<uint4*>(kv.stats) + ((slab.page_head * lp.g + j) * 2) * (kHeadDim / 8);
-            if (held) {
-                old[0] = stats[p.p0], old[1] = stats[p.p1];
-                old[2] = stats[kHeadDim / 8 + p.p0], old[3] = stats[kHeadDim / 8 + p.p1];
+    const uint16_t* from = (const uint16_t*)(kind == 0 ? a.k : kind == 1 ? a.v : a.q) + (size_t)src0 * stride + head * kHeadDim;
+    void* dense = kind == 0 ? a.k_out : kind == 1 ? a.v_out : a.q_out;
+    float2* turns = all_turns[wave];
+    const uint32_t inf = Elem<T>::pack(INFINITY, INFINITY), none = inf | 0x80008000u;
+    uint4 range[4];  // of the logical page: largest of either piece, smallest
+    uint32_t x[4], y[4], next_x[4], next_y[4];
+    load_pieces(from, 0, p, x, y);
+    for (int i = 0; i < n; ++i) {
+        const int s = start + i, page = s / lp.NP, slot = s - page * lp.NP, j = slot / lp.NL;
+        Slab slab = {};
+        uint4* stats = nullptr;
+        bool kept = true;
+        if (kind != 2) {
+            slab = slab_of(lp, kv, pages_of(lp, kv, b, page), head, BITS);
+            // bounded pool: only sink pages and those that are local once all new tokens are in
+            kept = !in_stream_pool(lp, kv, head) || page < lp.sink_pages || page >= ceil_div(start + n, lp.NP) - lp.local_pages;
+            if (scored) {
+                stats = reinterpret_cast<uint4*>(kv.stats) + ((slab.page_head * lp.g + j) * 2) * (kHeadDim / 8);
+                if (slot == j * lp.NL) {  // nothing yet: infinities of either sign
+                    range[0] = range[1] = make_uint4(none, none, none, none);
+                    range[2] = range[3] = make_uint4(inf, inf, inf, inf);
+                } else if (i == 0) {
+                    range[0] = stats[p.p0], range[1] = stats[p.p1];
+                    range[2] = stats[kHeadDim / 8 + p.p0], range[3] = stats[kHeadDim / 8 + p.p1];
+                }
             }
         }
-    }
-    if (kind != 1) {
-        const int pairs = a.turn.rotary_dim / 2;
-        float2* turns = all_turns[wave];
-        if (lane < pairs) turns[turn_place<LAYOUT>(lane)] = turn_of(position_of(a.turn, src, s, lane), a.turn.inv_freq[lane], a.turn.scale);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        float2 turn[8];
-        if constexpr (LAYOUT != kOddHalves) read_turns(turns, l, turn);
-        const float* weight = !NORM ? nullptr : kind == 2 ? a.turn.q_weight : a.turn.k_weight;
+        Weights w;  // (asked for ahead of the next rows: loads come back in order)
+        const float* weight = !NORM || kind == 1 ? nullptr : kind == 2 ? a.turn.q_weight : a.turn.k_weight;
         if (weight) weight += (size_t)head * a.turn.weight_step;
-        Weights w;
         if (NORM) load_weights(weight, p, w);
-        turn_row<T, LAYOUT, NORM>(x, y, turn, a.turn, weight != nullptr, w, p, rooms[LAYOUT == kOddHalves ? wave * 8 + r : 0], turns);
+        if (i + 1 < n) load_pieces(from, (size_t)(i + 1) * stride, p, next_x, next_y);
+        if (kind != 1) {
+            if (lane < a.turn.rotary_dim / 2)
+                turns[turn_place<LAYOUT>(lane)] = turn_of(position_of(a.turn, src0 + i, s, lane), a.turn.inv_freq[lane], a.turn.scale);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            float2 turn[8];
+            if constexpr (LAYOUT != kOddHalves) read_turns(turns, l, turn);
+            turn_row<T, LAYOUT, NORM>(x, y, turn, a.turn, weight != nullptr, w, p, rooms[LAYOUT == kOddHalves ? wave * 8 + r : 0], turns);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (the next token's angles take their place)
+        }
+        if (there && dense) store_pieces(dense, ((size_t)(src0 + i) * heads + head) * kHeadDim, p, x, y);
+        if (there && kind != 2 && kept) write_row<BITS>(kind == 0 ? slab.k : slab.v, lp.NP, slot, p, l, stored<T, BITS>(x, y));
+        if (scored) {
+            range[0] = further<T, true>(x, range[0]);
+            range[1] = further<T, true>(y, range[1]);
+            range[2] = further<T, false>(x, range[2]);
+            range[3] = further<T, false>(y, range[3]);
+            if (i + 1 == n || (slot + 1) % lp.NL == 0) {
+                stats[p.p0] = range[0];
+                stats[p.p1] = range[1];
+                stats[kHeadDim / 8 + p.p0] = range[2];
+                stats[kHeadDim / 8 + p.p1] = range[3];
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            x[q] = next_x[q];
+            y[q] = next_y[q];
+        }
     }
-    if (!there) return;
-    void* dense = kind == 0 ? a.k_out : kind == 1 ? a.v_out : a.q_out;
-    if (dense) store_pieces(dense, ((size_t)src * heads + head) * kHeadDim, p, x, y);
-    if (kind == 2) return;
-    write_row<BITS>(kind == 0 ? slab.k : slab.v, lp.NP, slot, p, l, stored<T, BITS>(x, y));
-    if (!stats) return;
-    if (!held) {  // nothing yet: infinities of either sign
-        const uint32_t inf = Elem<T>::pack(INFINITY, INFINITY), none = inf | 0x80008000u;
-        old[0] = old[1] = make_uint4(none, none, none, none);
-        old[2] = old[3] = make_uint4(inf, inf, inf, inf);
-    }
-    stats[p.p0] = further<T, true>(x, old[0]);
-    stats[p.p1] = further<T, true>(y, old[1]);
-    stats[kHeadDim / 8 + p.p0] = further<T, false>(x, old[2]);
-    stats[kHeadDim / 8 + p.p1] = further<T, false>(y, old[3]);
 }
 
 namespace {
 
 template <class T, int LAYOUT, int BITS, bool NORM> hipError_t launch(const TurnedAppendArgs& a, hipStream_t stream) {
-    if (a.max_new == 1) {
+    // A sequence's few tokens one after the other, a microsecond each, or blocks of sixteen places with as few rows in them, of which more sequences are more: one
+    // sequence of two tokens 4.9 and 5.1 us, of three 5.6 and 5.2; 64 of two 5.1 and 6.6, of three 6.2 and 7.5, of four 7.4 and 7.5, of six 9.6 and 9.4; 256 of
+    // four 10.1 and 13.1, of six 13.0 and 15.1, of eight 16.0 and 13.3; 500 of two 8.7 and 14.6, of eight 26.5 and 31.5, of twelve 40 and 38.
+    if (a.max_new <= 2 || (a.max_new <= 8 && (a.max_new - 2) * 64 <= a.kv.batch)) {
         const int groups_q = a.q ? ceil_div(a.lp.H, 8) : 0, groups_kv = ceil_div(a.lp.Hkv, 8);
         const long long waves = (long long)a.kv.batch * (groups_q + 2 * groups_kv);
         hipLaunchKernelGGL((turned_step_kernel<T, LAYOUT, BITS, NORM>), dim3((unsigned)((waves + kStepWaves - 1) / kStepWaves)), dim3(kStepThreads), 0, stream, a, groups_q,

@@ -152,6 +152,31 @@ def test_decode_steps(dtype, bits, two_way, R, interleaved):
     _run(dtype, lens, [1, 1, 1, 1, 1, 1, 1, 0, 1, 1, 0, 1], R=R, interleaved=interleaved, bits=bits, two_way=two_way, norm="centred" if R == 64 else None)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("two_way", [False, True])
+@pytest.mark.parametrize("R,interleaved,norm", [(128, False, None), (64, True, "rms"), (20, False, "centred"), (0, False, None)])
+def test_a_few_tokens_each(dtype, bits, two_way, R, interleaved, norm):
+    """Up to two, three, four and eight of as many sequences as take them one after the other, across the ends of logical and physical pages."""
+    g = torch.Generator().manual_seed(R + bits)
+    for batch, most in ((5, 2), (64, 3), (130, 4), (390, 8)):
+        counts = torch.randint(0, most + 1, (batch,), generator=g).tolist()
+        counts[0], counts[-1] = most, 1
+        lens = torch.randint(0, 200, (batch,), generator=g).tolist()
+        lens[:4] = [63, 15, 0, 64]
+        _run(dtype, lens, counts, R=R, interleaved=interleaved, norm=norm, bits=bits, two_way=two_way, sink=64, local=64, hq=2, hkv=2, dense=batch != 64, spare=batch % 3,
+             weights="heads" if norm else False)
+
+
+@pytest.mark.parametrize("two_way", [False, True])
+@pytest.mark.parametrize("page,logical", [(16, 2), (16, 4), (32, 32), (128, 128)])
+def test_a_few_tokens_each_in_pages_of_other_sizes(two_way, page, logical):
+    """One local page of sixteen tokens: some of the call's own are gone by its end."""
+    g = torch.Generator().manual_seed(page + logical)
+    counts, lens = torch.randint(0, 9, (400,), generator=g).tolist(), torch.randint(0, 300, (400,), generator=g).tolist()
+    _run(torch.bfloat16, lens, counts, page=page, logical=logical, two_way=two_way, sink=16, local=1, hq=4, hkv=2, in_place=page == 32)
+
+
 @pytest.mark.parametrize("page,logical", [(16, 16), (16, 2), (32, 16), (32, 4), (64, 64), (64, 32), (64, 8), (128, 16), (128, 128), (128, 64)])
 @pytest.mark.parametrize("two_way", [False, True])
 def test_pages(page, logical, two_way):
