@@ -363,9 +363,10 @@ __global__ __launch_bounds__(kStepThreads) void turned_step_kernel(TurnedAppendA
 namespace {
 
 template <class T, int LAYOUT, int BITS, bool NORM> hipError_t launch(const TurnedAppendArgs& a, hipStream_t stream) {
-    // A sequence's few tokens one after the other, a microsecond each, or blocks of sixteen places with as few rows in them, of which more sequences are more: one
-    // sequence of two tokens 4.9 and 5.1 us, of three 5.6 and 5.2; 64 of two 5.1 and 6.6, of three 6.2 and 7.5, of four 7.4 and 7.5, of six 9.6 and 9.4; 256 of
-    // four 10.1 and 13.1, of six 13.0 and 15.1, of eight 16.0 and 13.3; 500 of two 8.7 and 14.6, of eight 26.5 and 31.5, of twelve 40 and 38.
+    // A sequence's few tokens one after the other, a microsecond each, or blocks of sixteen places with as few rows in them,
+    // of which more sequences are more: one sequence of two tokens 4.9 and 5.1 us, of three 5.6 and 5.2; 64 of two 5.1 and 6.6, of
+    // three 6.2 and 7.5, of four 7.4 and 7.5, of six 9.6 and 9.4; 256 of four 10.1 and 13.1, of six 13.0 and 15.1, of eight 16.0 and
+    // 13.3; 500 of two 8.7 and 14.6, of eight 26.5 and 31.5, of twelve 40 and 38.
     if (a.max_new <= 2 || (a.max_new <= 8 && (a.max_new - 2) * 64 <= a.kv.batch)) {
         const int groups_q = a.q ? ceil_div(a.lp.H, 8) : 0, groups_kv = ceil_div(a.lp.Hkv, 8);
         const long long waves = (long long)a.kv.batch * (groups_q + 2 * groups_kv);
