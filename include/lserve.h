@@ -173,7 +173,8 @@ int lserve_build_page_stats(const lserve_attn_desc *desc, const lserve_paged_kv 
  * neither read nor written (the caller bumps the lengths).  kv->stats may be NULL when every KV head is
  * streaming.  With kv->kv_bits == 8 or 4 the rows are quantised on the way in (see lserve_paged_kv: one
  * scale and zero point per token, KV head and pool, written behind the page's rows); the statistics are
- * those of the 16-bit keys handed in, exactly as for a 16-bit cache.
+ * those of the 16-bit keys handed in, exactly as for a 16-bit cache.  What is not a number, signalling or not, takes no part in a
+ * row's range or in statistics and has code 0.
  *
  *   k_new, v_new   device [total_new][Hkv][D], tokens of all sequences concatenated
  *   cu_new         device [batch + 1], cu_new[0] = 0

@@ -126,6 +126,7 @@ __global__ __launch_bounds__(kWave* kMaxLogical) void append_kv_kernel(LayerPara
             if constexpr (BITS == 16) {
                 kdst[dst] = x[u];
                 vdst[dst] = y[u];
+                range.add(x[u]);
             } else {
                 uint32_t ksz, vsz;
                 uint2 kc, vc;
@@ -143,7 +144,10 @@ __global__ __launch_bounds__(kWave* kMaxLogical) void append_kv_kernel(LayerPara
                     reinterpret_cast<uint32_t*>(vdst + lp.NP * (kHeadDim * BITS / 128))[slot] = vsz;
                 }
             }
-            range.add(x[u]);
+        }
+        if constexpr (BITS != 16) {  // (four at a time; a row that is not there is the last one once more)
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) range.add(x[u]);
         }
     }
     if (streaming) return;  // streaming heads are never scored

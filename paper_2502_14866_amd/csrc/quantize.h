@@ -24,13 +24,23 @@ __device__ __forceinline__ half2_t quiet(uint32_t w) {
     return pk_max(x, x);
 }
 
-// Smallest and largest of eight values (f: the same as numbers).
+// A value with a signalling not-a-number quieted, which the forms of three operands (v_min3, v_max3) would take for the range so far.  (Conversions
+// from fp16 have done so.  Written out: the compiler drops its own form as one that a minimum or maximum makes needless.)
+template <class T> __device__ __forceinline__ float quieted(float x) { return x; }
+template <> __device__ __forceinline__ float quieted<BF16>(float x) {
+    float r;
+    asm("v_max_f32 %0, %1, %1" : "=v"(r) : "v"(x));
+    return r;
+}
+
+// Smallest and largest of eight values (f: the same as numbers); what is not a number gives way.
 template <class T> __device__ __forceinline__ void range8(const uint32_t (&)[4], const float (&f)[8], float& lo, float& hi) {
-    lo = hi = f[0];
+    lo = hi = quieted<T>(f[0]);
 #pragma unroll
     for (int i = 1; i < 8; ++i) {
-        lo = fminf(lo, f[i]);
-        hi = fmaxf(hi, f[i]);
+        const float x = quieted<T>(f[i]);
+        lo = fminf(lo, x);
+        hi = fmaxf(hi, x);
     }
 }
 template <> __device__ __forceinline__ void range8<F16>(const uint32_t (&w)[4], const float (&)[8], float& lo, float& hi) {
@@ -59,10 +69,11 @@ template <class T> struct RowRange {
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            hi[2 * i] = fmaxf(hi[2 * i], Elem<T>::lo(w[i]));
-            lo[2 * i] = fminf(lo[2 * i], Elem<T>::lo(w[i]));
-            hi[2 * i + 1] = fmaxf(hi[2 * i + 1], Elem<T>::hi(w[i]));
-            lo[2 * i + 1] = fminf(lo[2 * i + 1], Elem<T>::hi(w[i]));
+            const float a = quieted<T>(Elem<T>::lo(w[i])), b = quieted<T>(Elem<T>::hi(w[i]));
+            hi[2 * i] = fmaxf(hi[2 * i], a);
+            lo[2 * i] = fminf(lo[2 * i], a);
+            hi[2 * i + 1] = fmaxf(hi[2 * i + 1], b);
+            lo[2 * i + 1] = fminf(lo[2 * i + 1], b);
         }
     }
     __device__ __forceinline__ float largest(int i) const { return hi[i]; }
@@ -185,26 +196,12 @@ __device__ __forceinline__ void quantize_row(const uint4& x, uint2& packed, uint
     scale_zero = row.pair;
 }
 
-// A value with a signalling not-a-number quieted, which the forms of three operands (v_min3, v_max3) would take for the range so far.  (Conversions
-// from fp16 have done so.  Written out: the compiler drops its own form as one that a minimum or maximum makes needless.)
-template <class T> __device__ __forceinline__ float quieted(float x) { return x; }
-template <> __device__ __forceinline__ float quieted<BF16>(float x) {
-    float r;
-    asm("v_max_f32 %0, %1, %1" : "=v"(r) : "v"(x));
-    return r;
-}
-
 // A row held by eight lanes, two pieces of eight features to a lane.
 template <class T, int BITS>
 __device__ __forceinline__ void quantize_pieces(const uint32_t (&x)[4], const uint32_t (&y)[4], uint2& x_codes, uint2& y_codes, uint32_t& scale_zero) {
     float f[8], g[8];
     unpack8<T>(x, f);
     unpack8<T>(y, g);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        f[i] = quieted<T>(f[i]);
-        g[i] = quieted<T>(g[i]);
-    }
     float lo, hi, lo_y, hi_y;
     range8<T>(x, f, lo, hi);
     range8<T>(y, g, lo_y, hi_y);
