@@ -200,7 +200,8 @@ __global__ __launch_bounds__(256) void append_token_kernel(LayerParams lp, Paged
     const size_t ph = (size_t)phys * (ring ? kv.stream_heads : kv.pool_heads) + pool_rank(lp, kv, hk, ring);
     const bool with_stats = !streaming && !is_v, first = slot - j * lp.NL == 0;
     uint4* st = reinterpret_cast<uint4*>(kv.stats) + ((ph * lp.g + j) * 2) * (kHeadDim / 8) + c;
-    uint4 om = x, on = x;
+    const uint32_t inf = Elem<T>::pack(INFINITY, INFINITY), none = inf | 0x80008000u;
+    uint4 om = make_uint4(none, none, none, none), on = make_uint4(inf, inf, inf, inf);
     if (with_stats && !first) {  // the logical page already holds tokens
         om = st[0];
         on = st[kHeadDim / 8];
@@ -224,10 +225,9 @@ __global__ __launch_bounds__(256) void append_token_kernel(LayerParams lp, Paged
     uint32_t mx[4], mn[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        mx[i] = Elem<T>::pack(fmaxf(fmaxf(-INFINITY, Elem<T>::lo(w[i])), Elem<T>::lo(wm[i])),
-                              fmaxf(fmaxf(-INFINITY, Elem<T>::hi(w[i])), Elem<T>::hi(wm[i])));
-        mn[i] = Elem<T>::pack(fminf(fminf(INFINITY, Elem<T>::lo(w[i])), Elem<T>::lo(wn[i])),
-                              fminf(fminf(INFINITY, Elem<T>::hi(w[i])), Elem<T>::hi(wn[i])));
+        const float a = quieted<T>(Elem<T>::lo(w[i])), b = quieted<T>(Elem<T>::hi(w[i]));
+        mx[i] = Elem<T>::pack(fmaxf(fmaxf(-INFINITY, a), Elem<T>::lo(wm[i])), fmaxf(fmaxf(-INFINITY, b), Elem<T>::hi(wm[i])));
+        mn[i] = Elem<T>::pack(fminf(fminf(INFINITY, a), Elem<T>::lo(wn[i])), fminf(fminf(INFINITY, b), Elem<T>::hi(wn[i])));
     }
     st[0] = make_uint4(mx[0], mx[1], mx[2], mx[3]);
     st[kHeadDim / 8] = make_uint4(mn[0], mn[1], mn[2], mn[3]);

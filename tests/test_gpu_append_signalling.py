@@ -1,12 +1,16 @@
-"""Signalling not-a-numbers of rows on their way into pages take no part in a row's range or in statistics, like any other."""
+"""Signalling not-a-numbers of rows on their way into pages: like any other they take no part in a row's range or in statistics, through lserve_append_kv as through
+lserve_rotary_append_kv, which leave the same bytes."""
 import numpy as np
 import pytest
 import torch
 
 from test_gpu_append_special import SIGNALLING, _append, _expected
 from test_gpu_quant import _unpack_rows
+from test_gpu_rotary_append import _assert_same_cache, _cache, _twin
 
 pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
 
 
 def _numbers(x):
@@ -45,3 +49,56 @@ def test_extremes_next_to_signalling_not_a_numbers(dtype, bits, one_by_one, seed
         part = _numbers(x)[16 * page:16 * page + 16]
         high, low = np.fmax(np.fmax.reduce(part, axis=0), -np.inf), np.fmin(np.fmin.reduce(part, axis=0), np.inf)
         assert np.array_equal(stats[0, 0, page, 0].float().numpy(), high) and np.array_equal(stats[0, 0, page, 1].float().numpy(), low)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("two_way", [False, True])
+@pytest.mark.parametrize("counts", [[1, 1, 1], [2, 1, 2], [40, 19, 64]])
+def test_both_calls_leave_the_same_bytes(dtype, bits, two_way, counts):
+    import paper_2502_14866_amd as L
+
+    L.load_library()
+    g = torch.Generator().manual_seed(sum(counts) + bits)
+    desc = L.AttnDesc(4, 4, [1, 0, 1, 0], dtype=dtype)
+    kv = _cache(L, g, dtype, desc, [7, 100, 64], counts, bits, two_way, 64)
+    twin = _twin(L, kv)
+    k, v = (torch.randn((sum(counts), 4, 128), generator=g).to(dtype) for _ in range(2))
+    odd = torch.tensor([0x7c00, 0xfc00, 0x7e00, 0x7c01, 0x7d01, 0x7f80, 0xff80, 0x7fc0, 0x7f81, 0x7fa1, 0xffa1], dtype=torch.int32).to(torch.int16)
+    for t in (k, v):
+        row = t.view(torch.int16).view(-1)
+        at = torch.randint(0, row.numel(), (row.numel() // 12,), generator=g)
+        row[at] = odd[torch.randint(0, len(odd), at.shape, generator=g)]
+    k, v = k.to(DEV), v.to(DEV)
+    cu = torch.tensor([0] + torch.tensor(counts).cumsum(0).tolist(), dtype=torch.int32, device=DEV)
+    L.lserve_rotary_append_kv(desc, kv, None, None, k, v, cu, kv.seq_lens, max(counts), None)
+    L.lserve_append_kv(desc, twin, k, v, cu, kv.seq_lens, max(counts))
+    torch.cuda.synchronize()
+    _assert_same_cache(kv, twin)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("at", [0, 16, 47])
+def test_a_token_of_nothing_but_not_a_numbers(dtype, at):
+    """Statistics of a logical page whose first token, or last of three, has no number: infinities, or what the others left."""
+    import paper_2502_14866_amd as L
+
+    L.load_library()
+    desc = L.AttnDesc(1, 1, [0], dtype=dtype)
+    i32 = lambda *a: torch.tensor(a + (0,) * 4, dtype=torch.int32, device=DEV)[:len(a)]  # noqa: E731
+    pool = torch.zeros((1, 1, 64, 128), dtype=dtype, device=DEV)
+    stats = torch.full((1, 1, 4, 2, 128), 3.0, dtype=dtype, device=DEV)
+    kv = L.PagedKV(pool, pool.clone(), stats, i32(0).reshape(1, 1), i32(at + 1))
+    row = torch.full((1, 1, 128), float("nan"), dtype=dtype, device=DEV)
+    for kind in ("bf16" if dtype == torch.bfloat16 else "fp16", None):
+        if kind:
+            row.view(torch.int16)[:] = SIGNALLING[kind]
+        else:
+            row.fill_(float("nan"))
+        L.lserve_append_kv(desc, kv, row, row, i32(0, 1), i32(at), 1)
+        torch.cuda.synchronize()
+        got = stats[0, 0, at // 16].float().cpu()
+        if at % 16 == 0:
+            assert (got[0] == -float("inf")).all() and (got[1] == float("inf")).all()
+        else:
+            assert (got == 3.0).all()
