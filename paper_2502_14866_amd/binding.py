@@ -262,7 +262,7 @@ class _CtypesCalls:
         at, apart = _places(where, positions, axes, total)
         _checked(where, *_turn_tensors(d, norm, rotary, q_weight, k_weight, inv_freq), (positions, torch.int32, 1), (q, dt, total * hq * dim),
                  (q_out, dt, total * hq * dim), (k, dt, total * hkv * dim), (k_out, dt, total * hkv * dim))
-        lib, n, r, a = load_library(), _struct(_CHeadNorm, norm), _struct(_CRotaryDesc, rotary), _struct(_CPositionAxes, axes)
+        lib, n, r, a = load_library(), _norm_struct(norm, q_weight, k_weight), _struct(_CRotaryDesc, rotary), _struct(_CPositionAxes, axes)
         if norm:
             return lib.lserve_norm_rotary(d, n, r, a, q_at, k_at, at, apart, total, q_stride, k_stride, _ptr(q_out), _ptr(k_out), stream)
         return lib.lserve_rotary_axes(d, r, a, q_at, k_at, at, apart, total, q_stride, k_stride, _ptr(q_out), _ptr(k_out), stream)
@@ -288,7 +288,7 @@ class _CtypesCalls:
                  (kv.v_pool, kind, pool), (kv.k_pool_stream, kind, bounded), (kv.v_pool_stream, kind, bounded), (kv.stats, dt, spans),
                  (kv.ring_table, i32, batch * _ring(d) if kv.k_pool_stream is not None else 0))
         return load_library().lserve_rotary_append_kv(
-            d, kv.c(), _struct(_CHeadNorm, norm), _struct(_CRotaryDesc, rotary), _struct(_CPositionAxes, axes), rows[0][0], rows[1][0], rows[2][0],
+            d, kv.c(), _norm_struct(norm, q_weight, k_weight), _struct(_CRotaryDesc, rotary), _struct(_CPositionAxes, axes), rows[0][0], rows[1][0], rows[2][0],
             rows[0][1], rows[1][1], rows[2][1], at, apart, _ptr(cu_new), _ptr(start_pos), total, max_new_per_seq, _ptr(q_out), _ptr(k_out), _ptr(v_out),
             stream)
 
@@ -353,6 +353,15 @@ def _checked(where: str, *args) -> None:
 
 def _struct(kind, address: int):
     return kind.from_address(address) if address else None
+
+
+def _norm_struct(address: int, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor]) -> Optional["_CHeadNorm"]:
+    """A norm's description with its weights where they are now."""
+    if not address:
+        return None
+    n = _CHeadNorm.from_buffer_copy(_CHeadNorm.from_address(address))
+    n.q_weight, n.k_weight = _ptr(q_weight) if n.q_weight else None, _ptr(k_weight) if n.k_weight else None
+    return n
 
 
 def _turn_tensors(d: "_CAttnDesc", norm: int, rotary: int, q_weight, k_weight, inv_freq) -> tuple:
@@ -833,11 +842,23 @@ class PositionAxes:
 
 @dataclass
 class HeadNorm:
-    """Mirror of lserve_head_norm; weights: float32 [D] for all heads, or [heads][D] (both alike), or None for ones."""
+    """Mirror of lserve_head_norm; weights: float32 [D] for all heads, or [heads][D] (both alike), or None for ones.  A call works with what
+    the attributes are by then, and with the memory that the weights' tensors have by then."""
     q_weight: Optional[torch.Tensor] = None
     k_weight: Optional[torch.Tensor] = None
     eps: float = 1e-6
     centred: bool = False
+
+    def __setattr__(self, name, value):
+        described = "_c" in self.__dict__ and name in self.__dataclass_fields__
+        before = getattr(self, name, None)
+        super().__setattr__(name, value)
+        if described:
+            try:
+                self.__post_init__()
+            except ValueError:
+                super().__setattr__(name, before)
+                raise
 
     def __post_init__(self):
         given = [w for w in (self.q_weight, self.k_weight) if w is not None]

@@ -278,8 +278,9 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 template <class S> const S* described(PyObject* o) { return reinterpret_cast<const S*>((uintptr_t)number(o)); }
 
-// How heads are normed and turned: descriptions by address, and the tensors that they name.
+// How heads are normed and turned: descriptions by address, and the tensors that they name, at their addresses of now.
 struct Turn {
+    lserve_head_norm norm_now = {};
     const lserve_head_norm* norm;
     const lserve_rotary_desc* rotary;
     const lserve_position_axes* axes;
@@ -292,7 +293,14 @@ struct Turn {
         q_least = norm && norm->per_head ? dim * d->num_q_heads : dim;
         k_least = norm && norm->per_head ? dim * d->num_kv_heads : dim;
         freq_least = turning <= dim ? turning / 2 : 0;
+        if (norm) {
+            norm_now = *norm;
+            if (norm->q_weight) norm_now.q_weight = address<const float>(q_weight);
+            if (norm->k_weight) norm_now.k_weight = address<const float>(k_weight);
+            norm = &norm_now;
+        }
     }
+    Turn(const Turn&) = delete;
 };
 
 // Address of positions [total], or with axes [axes][total], and how far the axes lie apart.

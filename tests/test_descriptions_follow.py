@@ -1,0 +1,69 @@
+"""A description of how heads are normed changed after it was made: the next call works with what it says now, or the change is refused."""
+import pytest
+import torch
+
+import paper_2502_14866_amd as L
+from test_turned_calls_native import _stand_in, _tensors
+
+ROUTES = pytest.mark.parametrize("route", ["native", "ctypes"])
+
+
+def _called(monkeypatch, route, t, norm):
+    """What both calls that take a norm hand over of it."""
+    kv = L.PagedKV(t["k"], t["v"], t["stats"], t["table"], t["lens"], pool_heads=1, k_pool_stream=t["ks"], v_pool_stream=t["vs"], ring_table=t["ring"])
+    desc, rot = L.AttnDesc(4, 2, [1, 0]), L.RotaryDesc(rotary_dim=64, inv_freq=t["freq"], device="cpu")
+    with _stand_in(monkeypatch, route) as seen:
+        L.lserve_norm_rotary(desc, norm, rot, t["qn"], t["kn"], t["pos"], t["qo"], t["ko"], 0x10)
+        L.lserve_rotary_append_kv(desc, kv, rot, None, t["kn"], t["vn"], t["cu"], t["lens"], 1, None, norm=norm, stream=0x20)
+    return [s[2] for s in seen[:1]] + [s[3] for s in seen[1:]]
+
+
+def _says(norm, t_q, t_k, per_head, eps, kind):
+    where = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    return (norm.q_weight, norm.k_weight, norm.per_head, round(norm.eps, 9), norm.kind) == (where(t_q), where(t_k), per_head, eps, kind)
+
+
+@ROUTES
+def test_weights_assigned_anew(monkeypatch, route):
+    t = _tensors()
+    norm = L.HeadNorm(t["wq"], t["wk"], eps=1e-5)
+    q, k = torch.ones(4, 128), torch.ones(2, 128)
+    norm.q_weight, norm.k_weight = q, k
+    assert all(_says(n, q, k, 1, 1e-5, 0) for n in _called(monkeypatch, route, t, norm))
+    norm.k_weight = None
+    assert all(_says(n, q, None, 1, 1e-5, 0) for n in _called(monkeypatch, route, t, norm))
+    norm.q_weight = None
+    norm.k_weight = torch.ones(128)  # from weights a head to shared ones
+    assert all(_says(n, None, norm.k_weight, 0, 1e-5, 0) for n in _called(monkeypatch, route, t, norm))
+
+
+@ROUTES
+def test_weights_whose_memory_is_another(monkeypatch, route):
+    """What a module that is moved, or loaded by its tensors' data, does."""
+    t = _tensors()
+    norm = L.HeadNorm(torch.nn.Parameter(torch.ones(4, 128)), torch.nn.Parameter(torch.ones(2, 128)))
+    moved = torch.ones(4, 128), torch.ones(2, 128)
+    norm.q_weight.data, norm.k_weight.data = moved
+    assert all(_says(n, *moved, 1, 1e-6, 0) for n in _called(monkeypatch, route, t, norm))
+    # (the type and the size are those of the new memory)
+    norm.q_weight.data = torch.ones(3, 128)
+    with pytest.raises(ValueError):
+        _called(monkeypatch, route, t, norm)
+
+
+@ROUTES
+def test_eps_and_kind(monkeypatch, route):
+    t = _tensors()
+    norm = L.HeadNorm(t["wq"], t["wk"])
+    norm.eps, norm.centred = 1e-3, True
+    assert all(_says(n, t["wq"], t["wk"], 1, 1e-3, 1) for n in _called(monkeypatch, route, t, norm))
+
+
+def test_a_change_that_is_refused_leaves_it_as_it_was(monkeypatch):
+    t = _tensors()
+    norm = L.HeadNorm(t["wq"], t["wk"])
+    for bad in (torch.ones(128), torch.ones(4, 128, dtype=torch.float16), torch.ones(1, 4, 128), torch.ones(4, 256)[:, ::2]):
+        with pytest.raises(ValueError):
+            norm.q_weight = bad
+        assert norm.q_weight is t["wq"]
+    assert all(_says(n, t["wq"], t["wk"], 1, 1e-6, 0) for n in _called(monkeypatch, "ctypes", t, norm))
