@@ -809,22 +809,35 @@ def lserve_rotary(desc: AttnDesc, rotary: RotaryDesc, q: Optional[torch.Tensor],
            "lserve_rotary")
 
 
-@dataclass
 class PositionAxes:
-    """Mirror of lserve_position_axes: the axis of each of a head's rotary_dim / 2 pairs (num_axes: as many as are named)."""
-    pair_axis: Sequence[int]
-    num_axes: int = 0
+    """Mirror of lserve_position_axes: the axis of each of a head's rotary_dim / 2 pairs (num_axes: as many as are named).  Stays as it was made."""
 
-    def __post_init__(self):
-        self.pair_axis = [int(a) for a in self.pair_axis]
-        if not self.pair_axis or min(self.pair_axis) < 0 or max(self.pair_axis) > 255:
+    def __init__(self, pair_axis: Sequence[int], num_axes: int = 0):
+        pairs = [int(a) for a in pair_axis]
+        if not pairs or min(pairs) < 0 or max(pairs) > 255:
             raise ValueError("PositionAxes: an axis for every pair")
-        self.num_axes = self.num_axes or max(self.pair_axis) + 1
         # (the library reads rotary_dim / 2 of them, 64 at most; what is not named here is no axis)
-        self._axes = (ctypes.c_uint8 * max(64, len(self.pair_axis)))(*([255] * 64))
-        self._axes[:len(self.pair_axis)] = self.pair_axis
-        self._c = _CPositionAxes(self.num_axes, ctypes.cast(self._axes, ctypes.POINTER(ctypes.c_uint8)))
+        self._pairs = len(pairs)
+        self._axes = (ctypes.c_uint8 * max(64, len(pairs)))(*([255] * 64))
+        self._axes[:len(pairs)] = pairs
+        self._c = _CPositionAxes(num_axes or max(pairs) + 1, ctypes.cast(self._axes, ctypes.POINTER(ctypes.c_uint8)))
         self._address = ctypes.addressof(self._c)
+
+    @property
+    def pair_axis(self) -> list:
+        return list(self._axes[:self._pairs])
+
+    @property
+    def num_axes(self) -> int:
+        return self._c.num_axes
+
+    def __eq__(self, other):
+        return isinstance(other, PositionAxes) and (self.pair_axis, self.num_axes) == (other.pair_axis, other.num_axes)
+
+    __hash__ = None
+
+    def __repr__(self):
+        return f"PositionAxes(pair_axis={self.pair_axis}, num_axes={self.num_axes})"
 
     @classmethod
     def sections(cls, *pairs: int) -> "PositionAxes":

@@ -67,3 +67,18 @@ def test_a_change_that_is_refused_leaves_it_as_it_was(monkeypatch):
             norm.q_weight = bad
         assert norm.q_weight is t["wq"]
     assert all(_says(n, t["wq"], t["wk"], 1, 1e-6, 0) for n in _called(monkeypatch, "ctypes", t, norm))
+
+
+def test_axes_stay_as_they_were_made():
+    """The library's copy of the list is the only one: nothing that looks like a change goes unseen."""
+    given = [0, 1, 2, 0] * 16
+    axes = L.PositionAxes(given)
+    given[0] = 2
+    axes.pair_axis[1] = 2
+    assert axes.pair_axis == [0, 1, 2, 0] * 16 and list(axes._c.pair_axis[:64]) == axes.pair_axis and axes.num_axes == axes._c.num_axes == 3
+    for name, value in (("pair_axis", [0] * 64), ("num_axes", 4)):
+        with pytest.raises(AttributeError):
+            setattr(axes, name, value)
+    assert axes == L.PositionAxes([0, 1, 2, 0] * 16) and axes != L.PositionAxes([0] * 64, 3) and axes != L.PositionAxes([0, 1, 2, 0] * 16, 4)
+    assert repr(L.PositionAxes([0, 1], 3)) == "PositionAxes(pair_axis=[0, 1], num_axes=3)"
+    assert L.PositionAxes(pair_axis=range(70), num_axes=2).pair_axis == list(range(70))
