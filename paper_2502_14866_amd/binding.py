@@ -250,7 +250,7 @@ class _CtypesCalls:
         (q_at, q_stride), (k_at, k_stride) = _rows("lserve_rotary", q, hq, dim, "q"), _rows("lserve_rotary", k, hkv, dim, "k")
         _checked("lserve_rotary", (positions, torch.int32, 1), (inv_freq, torch.float64, r.rotary_dim // 2 if r.rotary_dim <= dim else 0), (q, dt, total * hq * dim),
                  (q_out, dt, total * hq * dim), (k, dt, total * hkv * dim), (k_out, dt, total * hkv * dim))
-        return load_library().lserve_rotary(d, r, q_at, k_at, _ptr(positions), total, q_stride, k_stride, _ptr(q_out), _ptr(k_out), stream)
+        return load_library().lserve_rotary(d, _rotary_struct(rotary, inv_freq), q_at, k_at, _ptr(positions), total, q_stride, k_stride, _ptr(q_out), _ptr(k_out), stream)
 
     @staticmethod
     def turned(desc, norm, rotary, axes, q_weight, k_weight, inv_freq, q, k, positions, q_out, k_out, stream):
@@ -262,7 +262,7 @@ class _CtypesCalls:
         at, apart = _places(where, positions, axes, total)
         _checked(where, *_turn_tensors(d, norm, rotary, q_weight, k_weight, inv_freq), (positions, torch.int32, 1), (q, dt, total * hq * dim),
                  (q_out, dt, total * hq * dim), (k, dt, total * hkv * dim), (k_out, dt, total * hkv * dim))
-        lib, n, r, a = load_library(), _norm_struct(norm, q_weight, k_weight), _struct(_CRotaryDesc, rotary), _struct(_CPositionAxes, axes)
+        lib, n, r, a = load_library(), _norm_struct(norm, q_weight, k_weight), _rotary_struct(rotary, inv_freq), _struct(_CPositionAxes, axes)
         if norm:
             return lib.lserve_norm_rotary(d, n, r, a, q_at, k_at, at, apart, total, q_stride, k_stride, _ptr(q_out), _ptr(k_out), stream)
         return lib.lserve_rotary_axes(d, r, a, q_at, k_at, at, apart, total, q_stride, k_stride, _ptr(q_out), _ptr(k_out), stream)
@@ -288,7 +288,7 @@ class _CtypesCalls:
                  (kv.v_pool, kind, pool), (kv.k_pool_stream, kind, bounded), (kv.v_pool_stream, kind, bounded), (kv.stats, dt, spans),
                  (kv.ring_table, i32, batch * _ring(d) if kv.k_pool_stream is not None else 0))
         return load_library().lserve_rotary_append_kv(
-            d, kv.c(), _norm_struct(norm, q_weight, k_weight), _struct(_CRotaryDesc, rotary), _struct(_CPositionAxes, axes), rows[0][0], rows[1][0], rows[2][0],
+            d, kv.c(), _norm_struct(norm, q_weight, k_weight), _rotary_struct(rotary, inv_freq), _struct(_CPositionAxes, axes), rows[0][0], rows[1][0], rows[2][0],
             rows[0][1], rows[1][1], rows[2][1], at, apart, _ptr(cu_new), _ptr(start_pos), total, max_new_per_seq, _ptr(q_out), _ptr(k_out), _ptr(v_out),
             stream)
 
@@ -353,6 +353,15 @@ def _checked(where: str, *args) -> None:
 
 def _struct(kind, address: int):
     return kind.from_address(address) if address else None
+
+
+def _rotary_struct(address: int, inv_freq: Optional[torch.Tensor]) -> Optional["_CRotaryDesc"]:
+    """A description of rotary positions with its frequencies where they are now."""
+    if not address:
+        return None
+    r = _CRotaryDesc.from_buffer_copy(_CRotaryDesc.from_address(address))
+    r.inv_freq = _ptr(inv_freq) if r.inv_freq else None
+    return r
 
 
 def _norm_struct(address: int, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor]) -> Optional["_CHeadNorm"]:
@@ -770,7 +779,8 @@ def lserve_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: s
 @dataclass
 class RotaryDesc:
     """Mirror of lserve_rotary_desc: how the heads of a layer turn.  The frequencies are those of lserve_rotary_frequencies, or the
-    caller's own (inv_freq: float64 [rotary_dim / 2], radians per position), kept on `device` (the current GPU)."""
+    caller's own (inv_freq: float64 [rotary_dim / 2], radians per position), kept on `device` (the current GPU); calls read inv_freq where it is
+    by then."""
     rotary_dim: int = 128
     interleaved: bool = False
     base: float = 10000.0

@@ -257,6 +257,14 @@ const void* rows(const char* where, const at::Tensor* t, int64_t heads, int64_t 
     return t->data_ptr();
 }
 
+// A description of rotary positions with its frequencies where they are now.
+const lserve_rotary_desc* described_now(const lserve_rotary_desc* r, const at::Tensor* freq, lserve_rotary_desc* now) {
+    if (!r) return nullptr;
+    *now = *r;
+    if (r->inv_freq) now->inv_freq = address<const double>(freq);
+    return now;
+}
+
 PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 9, [&] {
         const lserve_attn_desc* desc = description(a[0]);
@@ -270,6 +278,8 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
         check("lserve_rotary", {{pos, kInt, 1}, {freq, kDouble, rot->rotary_dim <= dim ? rot->rotary_dim / 2 : 0}, {q, t, total * hq * dim}, {qo, t, total * hq * dim},
                                 {k, t, total * hkv * dim}, {ko, t, total * hkv * dim}});
         const int32_t* p_pos = address<int32_t>(pos);
+        lserve_rotary_desc now;
+        rot = described_now(rot, freq, &now);
         void *p_qo = address(qo), *p_ko = address(ko), *stream = stream_handle(a[8]);
         const WithoutLock w;
         return rotary(desc, rot, p_q, p_k, p_pos, (int32_t)total, q_stride, k_stride, p_qo, p_ko, stream);
@@ -281,6 +291,7 @@ template <class S> const S* described(PyObject* o) { return reinterpret_cast<con
 // How heads are normed and turned: descriptions by address, and the tensors that they name, at their addresses of now.
 struct Turn {
     lserve_head_norm norm_now = {};
+    lserve_rotary_desc rotary_now = {};
     const lserve_head_norm* norm;
     const lserve_rotary_desc* rotary;
     const lserve_position_axes* axes;
@@ -293,6 +304,7 @@ struct Turn {
         q_least = norm && norm->per_head ? dim * d->num_q_heads : dim;
         k_least = norm && norm->per_head ? dim * d->num_kv_heads : dim;
         freq_least = turning <= dim ? turning / 2 : 0;
+        rotary = described_now(rotary, freq, &rotary_now);
         if (norm) {
             norm_now = *norm;
             if (norm->q_weight) norm_now.q_weight = address<const float>(q_weight);

@@ -1,8 +1,9 @@
-"""A description of how heads are normed changed after it was made: the next call works with what it says now, or the change is refused."""
+"""Descriptions of how heads are normed and turned, changed after they were made: the next call works with what they say now, or the change is refused."""
 import pytest
 import torch
 
 import paper_2502_14866_amd as L
+from paper_2502_14866_amd import binding as B
 from test_turned_calls_native import _stand_in, _tensors
 
 ROUTES = pytest.mark.parametrize("route", ["native", "ctypes"])
@@ -82,3 +83,26 @@ def test_axes_stay_as_they_were_made():
     assert axes == L.PositionAxes([0, 1, 2, 0] * 16) and axes != L.PositionAxes([0] * 64, 3) and axes != L.PositionAxes([0, 1, 2, 0] * 16, 4)
     assert repr(L.PositionAxes([0, 1], 3)) == "PositionAxes(pair_axis=[0, 1], num_axes=3)"
     assert L.PositionAxes(pair_axis=range(70), num_axes=2).pair_axis == list(range(70))
+
+
+@ROUTES
+def test_frequencies_whose_memory_is_another(monkeypatch, route):
+    from test_new_calls_native import _stand_in as stand_in_of_lserve_rotary
+
+    t = _tensors()
+    rot = L.RotaryDesc(rotary_dim=64, inv_freq=t["freq"], device="cpu")
+    desc, axes = L.AttnDesc(4, 2, [1, 0]), L.PositionAxes([0, 1, 2, 0] * 8)
+    for other in (torch.ones(32, dtype=torch.float64), torch.ones(40, dtype=torch.float64)):
+        if other.numel() == 32:
+            rot.inv_freq.data = other
+        else:
+            rot.inv_freq = other
+        with _stand_in(monkeypatch, route) as seen:
+            L.lserve_rotary_axes(desc, rot, axes, t["qn"], t["kn"], t["wide"][:, :6], t["qo"], t["ko"], 0x10)
+        assert seen[0][2].inv_freq == other.data_ptr() and seen[0][2].rotary_dim == 64
+        with stand_in_of_lserve_rotary(monkeypatch, route) as seen:
+            L.lserve_rotary(desc, rot, t["qn"], t["kn"], t["pos"], t["qo"], t["ko"], 0x20)
+        assert B._CRotaryDesc.from_buffer_copy(seen[0][2]).inv_freq == other.data_ptr()
+    rot.inv_freq = torch.ones(31, dtype=torch.float64)
+    with _stand_in(monkeypatch, route), pytest.raises(ValueError):
+        L.lserve_rotary_axes(desc, rot, axes, t["qn"], t["kn"], t["wide"][:, :6], t["qo"], t["ko"], 0x10)
