@@ -84,14 +84,14 @@ class DecodeSession:
         statistics in the same pass."""
         B.lserve_append_kv(self.desc, self.kv, k_new, v_new, cu_new, start_pos, max_new_per_seq)
 
-    def append_rotary(self, rotary: Optional[B.RotaryDesc], q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor,
+    def append_rotary(self, rotary: Optional[B.RotaryDesc], q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor,
                       start_pos: torch.Tensor, max_new_per_seq: int, norm: Optional[B.HeadNorm] = None, axes: Optional[B.PositionAxes] = None,
                       positions: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
-                      v_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+                      v_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """`append` of rows as they come out of a fused projection (lserve_rotary_append_kv): keys are normed and turned on their way into the
-        pages, and so are the queries, which are returned (a new tensor each time, so that a captured call keeps its own).  k_out and v_out: the
+        pages, and so are the queries, which are returned (a new tensor each time, so that a captured call keeps its own; None without queries).  k_out and v_out: the
         turned keys and the values as dense rows too, for the attention of a prompt."""
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = None if q is None else torch.empty(q.shape, dtype=q.dtype, device=q.device)
         B.lserve_rotary_append_kv(self.desc, self.kv, rotary, q, k, v, cu_new, start_pos, max_new_per_seq, q_out, k_out=k_out, v_out=v_out, norm=norm,
                                   axes=axes, positions=positions)
         return q_out

@@ -1,4 +1,5 @@
-"""Descriptions of how heads are normed and turned, changed after they were made: the next call works with what they say now, or the change is refused."""
+"""Descriptions of how heads are normed and turned, changed after they were made: the next call works with what they say now, or the change is refused.  And
+a session's call of the same arguments."""
 import pytest
 import torch
 
@@ -106,3 +107,20 @@ def test_frequencies_whose_memory_is_another(monkeypatch, route):
     rot.inv_freq = torch.ones(31, dtype=torch.float64)
     with _stand_in(monkeypatch, route), pytest.raises(ValueError):
         L.lserve_rotary_axes(desc, rot, axes, t["qn"], t["kn"], t["wide"][:, :6], t["qo"], t["ko"], 0x10)
+
+
+@ROUTES
+def test_a_session_s_rows_without_queries(monkeypatch, route):
+    """Queries that are somebody else's: nothing comes back of them."""
+    from paper_2502_14866_amd.session import DecodeSession
+
+    t = _tensors()
+    pool = lambda n: torch.zeros((n, 1, 64, 128), dtype=torch.float16)  # noqa: E731
+    s = DecodeSession(pool(8), pool(8), t["table"], 4, [1, 0], 128, 512, budget_tokens=256, k_pool_stream=pool(20), v_pool_stream=pool(20), ring_table=t["ring"])
+    rot = L.RotaryDesc(rotary_dim=64, inv_freq=t["freq"], device="cpu")
+    with _stand_in(monkeypatch, route) as seen:
+        monkeypatch.setattr(B, "_stream", lambda stream: 0)
+        assert s.append_rotary(rot, None, t["kn"], t["vn"], t["cu"], t["start"], 3, k_out=t["ko"]) is None
+        out = s.append_rotary(rot, t["qn"], t["kn"], t["vn"], t["cu"], t["start"], 3)
+    assert out.shape == t["qn"].shape and [x[0] for x in seen] == ["lserve_rotary_append_kv"] * 2
+    assert seen[0][6] is None and seen[0][18:20] == (None, t["ko"].data_ptr()) and seen[1][6] == t["qn"].data_ptr() and seen[1][18] == out.data_ptr()
