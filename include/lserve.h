@@ -33,7 +33,7 @@
  *   - Return value: LSERVE_OK (0) or a negative LSERVE_ERR_* code.  Nothing is printed, nothing
  *     aborts.  After LSERVE_ERR_HIP, lserve_last_hip_error() returns the hipError_t value.
  *   - Device-side data errors (a page id outside the pool, a sequence length of 0 or beyond
- *     max_pages_per_seq * page_size, a selected page >= the sequence's page count, duplicates in a
+ *     max_pages_per_seq * page_size or, where the cache is read, 2^31 - 128, a selected page >= the sequence's page count, duplicates in a
  *     selection) are not detected and give undefined results.
  *   - All device pointers must be 16-byte aligned.  Element type of Q/K/V/O/pools/stats is IEEE
  *     binary16 (dtype 0) or bfloat16 (dtype 1); accumulation is fp32.
@@ -178,7 +178,7 @@ int lserve_build_page_stats(const lserve_attn_desc *desc, const lserve_paged_kv 
  *
  *   k_new, v_new   device [total_new][Hkv][D], tokens of all sequences concatenated
  *   cu_new         device [batch + 1], cu_new[0] = 0
- *   start_pos      device [batch]; start_pos[b] + n_b <= max_pages_per_seq * N_P
+ *   start_pos      device [batch]; start_pos[b] + n_b <= max_pages_per_seq * N_P and < 2^31
  *   max_new_per_seq  host upper bound of n_b (sizes the launch); > 0
  * Reads page_table, k_new, v_new, stats; writes k_pool, v_pool, stats.  No workspace.
  */

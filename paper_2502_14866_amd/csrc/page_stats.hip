@@ -80,16 +80,17 @@ __global__ __launch_bounds__(kWave* kMaxLogical) void append_kv_kernel(LayerPara
     const int s = start_pos[b], src0 = cu_new[b];
     const int e = s + (cu_new[b + 1] - src0);  // new tokens occupy positions [s, e)
     const int p = s / lp.NP + (int)blockIdx.x;
-    const int lo = p * lp.NP + j * lp.NL, hi = lo + lp.NL;  // this wave's logical page
-    const int t0 = max(lo, s), t1 = min(hi, e);
-    if (t0 >= t1) return;
+    if ((unsigned)p * lp.NP >= (unsigned)e) return;
+    const int lo = p * lp.NP + j * lp.NL;  // this wave's logical page
+    const int t0 = max(lo, s), rows = lo - t0 + min(lp.NL, e - lo);  // (in differences: the page may end past 2^31)
+    if (rows <= 0) return;
     const bool streaming = (lp.streaming_mask >> hk) & 1ull;
     size_t ph;  // (page, head) index inside the pool that stores this head
     uint4 *kdst, *vdst;
     if (in_stream_pool(lp, kv, hk)) {
         // bounded pool: only sink pages and the pages that are still local once all new tokens are in
         // are stored; a local page lands on the ring slot of the page w positions before it
-        if (p >= lp.sink_pages && p < ceil_div(e, lp.NP) - lp.local_pages) return;
+        if (p >= lp.sink_pages && p <= (e - 1) / lp.NP - lp.local_pages) return;
         const int phys = kv.ring_table[(size_t)b * kv.ring + ring_slot(lp, p)];
         ph = (size_t)phys * kv.stream_heads + pool_rank(lp, kv, hk, true);
         kdst = reinterpret_cast<uint4*>(const_cast<void*>(kv.k_stream));
@@ -108,20 +109,20 @@ __global__ __launch_bounds__(kWave* kMaxLogical) void append_kv_kernel(LayerPara
     // work on a row is some 140 vector instructions.  16-bit rows, which are only copied, four at a time: 16 sequences of 100 to 300
     // tokens, fp16, 5.8 us and with sixteen at a time 6.15, one of 4000 6.4 and 6.7, of 65536 113 and 115.
     constexpr int kRows = BITS == 16 ? 1 : 4;  // per lane row
-    for (int tb = t0; tb < t1; tb += 4 * kRows) {
+    const int first = src0 + (t0 - s), first_slot = t0 - p * lp.NP;
+    for (int tb = 0; tb < rows; tb += 4 * kRows) {
         uint4 x[kRows], y[kRows];
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
-            const int t = min(tb + 4 * u + r, t1 - 1);
-            const size_t src = ((size_t)(src0 + t - s) * lp.Hkv + hk) * (kHeadDim / 8) + c;
+            const size_t src = ((size_t)(first + min(tb + 4 * u + r, rows - 1)) * lp.Hkv + hk) * (kHeadDim / 8) + c;
             x[u] = k_new[src];
             y[u] = v_new[src];
         }
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
             const int t = tb + 4 * u + r;
-            if (t >= t1) continue;
-            const int slot = t - p * lp.NP;
+            if (t >= rows) continue;
+            const int slot = first_slot + t;
             const size_t dst = (size_t)slot * (kHeadDim / 8) + c;
             if constexpr (BITS == 16) {
                 kdst[dst] = x[u];
@@ -257,7 +258,7 @@ hipError_t launch_append_kv(int dtype, const LayerParams& lp, const PagedParams&
         return hipGetLastError();
     }
     // the new tokens of a sequence touch at most ceil(n / N_P) + 1 physical pages
-    dim3 grid((max_new_per_seq + lp.NP - 1) / lp.NP + 1, lp.Hkv, kv.batch);
+    dim3 grid((max_new_per_seq - 1) / lp.NP + 2, lp.Hkv, kv.batch);
     dim3 block(kWave * lp.g);
     const uint4* k4 = reinterpret_cast<const uint4*>(k_new);
     const uint4* v4 = reinterpret_cast<const uint4*>(v_new);
