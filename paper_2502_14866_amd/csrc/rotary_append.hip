@@ -123,9 +123,11 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
     // (workgroups go to the XCDs in turn: the parts, some of them dearer, move on by one with every block)
     const int at = blockIdx.x / share, part = (blockIdx.x + at) % share;
     const Found found = sequence_of(a.cu_new, a.start_pos, kv.batch, block, at, lane);
-    const int b = found.b, src0 = found.cu, s = found.start, e = s + min(found.cu_next, a.total) - src0;
-    const int lo = (s / block + at - first_block(src0, b, block)) * block;
-    const int t0 = max(lo, s), t1 = min(lo + block, e);
+    const int b = found.b, src0 = found.cu, s = found.start, e = s + (min(found.cu_next, a.total) - src0);
+    const int nth = s / block + at - first_block(src0, b, block);
+    if ((unsigned)nth * block >= (unsigned)max(e, 0)) return;
+    const int lo = nth * block;
+    const int t0 = max(lo, s), t1 = lo + min(block, e - lo);  // (the block may end past 2^31)
     if (t0 >= t1) return;
 
     const int page = lo / lp.NP, in_page = lo - page * lp.NP;
@@ -145,7 +147,7 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
             h = u < lp.Hkv ? u : u - lp.Hkv;
         } else {
             const int i = u - 2 * lp.Hkv;
-            t = t0 + (i / groups * chunks + c) * 2 + half;
+            t = t0 + min((i / groups * chunks + c) * 2 + half, t1 - t0);
             h = i % groups * 8 + r;
         }
         const int held = min(max(t, t0), t1 - 1), head = min(h, lp.H - 1);
@@ -157,7 +159,7 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const Row row = row_of(u, c, half);
-            load_pieces(from, (size_t)(src0 + row.t - s) * apart + row.head * kHeadDim, p, x[half], y[half]);
+            load_pieces(from, (size_t)(src0 + (row.t - s)) * apart + row.head * kHeadDim, p, x[half], y[half]);
         }
     };
     int u = wave + kAppendWaves * part, c = 0;
@@ -167,8 +169,8 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
     const int pairs = a.turn.rotary_dim / 2;
     if (lane < pairs) {
         const double f = a.turn.inv_freq[lane];
-        for (int t = t0 + wave; t < t1; t += kAppendWaves)
-            lds[(t - lo) * kTurnRow + turn_place<LAYOUT>(lane)] = turn_of(position_of(a.turn, src0 + t - s, t, lane), f, a.turn.scale);
+        for (int i = t0 - lo + wave; i < t1 - lo; i += kAppendWaves)
+            lds[i * kTurnRow + turn_place<LAYOUT>(lane)] = turn_of(position_of(a.turn, src0 + (lo - s) + i, lo + i, lane), f, a.turn.scale);
     }
     __syncthreads();
 
@@ -198,11 +200,11 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
             arrived(next_x[1], next_y[1]);
 #pragma unroll
             for (int half = 0; half < 2; ++half)
-                if (rows[half].there) store_pieces(a.q_out, ((size_t)(src0 + rows[half].t - s) * lp.H + rows[half].head) * kHeadDim, p, x[half], y[half]);
+                if (rows[half].there) store_pieces(a.q_out, ((size_t)(src0 + (rows[half].t - s)) * lp.H + rows[half].head) * kHeadDim, p, x[half], y[half]);
         } else {
             const int hk = is_v ? u - lp.Hkv : u;
             // bounded pool: only sink pages and those that are local once all new tokens are in
-            const bool kept = !in_stream_pool(lp, kv, hk) || page < lp.sink_pages || page >= ceil_div(e, lp.NP) - lp.local_pages;
+            const bool kept = !in_stream_pool(lp, kv, hk) || page < lp.sink_pages || page > (e - 1) / lp.NP - lp.local_pages;
             const bool scored = !is_v && !((lp.streaming_mask >> hk) & 1ull);
             if (scored) {
                 // The rows change hands in LDS: two channels to a lane, so that a range is four registers and needs no other lane
@@ -221,13 +223,13 @@ __global__ __launch_bounds__(kAppendThreads) void turned_append_kernel(TurnedApp
             if (dense) {
 #pragma unroll
                 for (int half = 0; half < 2; ++half)
-                    if (rows[half].there) store_pieces(dense, ((size_t)(src0 + rows[half].t - s) * lp.Hkv + hk) * kHeadDim, p, x[half], y[half]);
+                    if (rows[half].there) store_pieces(dense, ((size_t)(src0 + (rows[half].t - s)) * lp.Hkv + hk) * kHeadDim, p, x[half], y[half]);
             }
             const Slab slab = slab_of(lp, kv, pages, hk, BITS);
             if (kept) {
                 uint4* to = is_v ? slab.v : slab.k;
-                if (rows[0].there) write_row<BITS>(to, lp.NP, in_page + rows[0].t - lo, p, l, first_row);
-                if (rows[1].there) write_row<BITS>(to, lp.NP, in_page + rows[1].t - lo, p, l, second_row);
+                if (rows[0].there) write_row<BITS>(to, lp.NP, in_page + (rows[0].t - lo), p, l, first_row);
+                if (rows[1].there) write_row<BITS>(to, lp.NP, in_page + (rows[1].t - lo), p, l, second_row);
             }
             if (scored) {
                 const int from = lo + 16 * c;
@@ -312,7 +314,7 @@ __global__ __launch_bounds__(kStepThreads) void turned_step_kernel(TurnedAppendA
         if (kind != 2) {
             slab = slab_of(lp, kv, pages_of(lp, kv, b, page), head, BITS);
             // bounded pool: only sink pages and those that are local once all new tokens are in
-            kept = !in_stream_pool(lp, kv, head) || page < lp.sink_pages || page >= ceil_div(start + n, lp.NP) - lp.local_pages;
+            kept = !in_stream_pool(lp, kv, head) || page < lp.sink_pages || page > (start + (n - 1)) / lp.NP - lp.local_pages;
             if (scored) {
                 stats = reinterpret_cast<uint4*>(kv.stats) + ((slab.page_head * lp.g + j) * 2) * (kHeadDim / 8);
                 if (slot == j * lp.NL) {  // nothing yet: infinities of either sign
