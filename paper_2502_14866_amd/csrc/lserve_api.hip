@@ -174,7 +174,7 @@ bool rotary_is_fine(const lserve_rotary_desc* r) {
 }
 
 // How heads are normed and turned; positions as they are handed over (null is fine here where `own_places` says what stands in for them).
-int make_turn(const LayerParams& lp, const lserve_head_norm* norm, const lserve_rotary_desc* rotary, const lserve_position_axes* axes,
+int make_turn(const lserve_head_norm* norm, const lserve_rotary_desc* rotary, const lserve_position_axes* axes,
               const int32_t* positions, int64_t positions_stride, int total, bool own_places, TurnArgs* t) {
     if (norm) {
         if ((norm->kind != LSERVE_NORM_RMS && norm->kind != LSERVE_NORM_CENTRED) || (norm->per_head != 0 && norm->per_head != 1)) return LSERVE_ERR_INVALID_ARG;
@@ -623,16 +623,12 @@ int lserve_rotary(const lserve_attn_desc* desc, const lserve_rotary_desc* rotary
     LayerParams lp;
     const int rc = make_layer(desc, &lp);
     if (rc) return rc;
-    if (!rotary || !rotary->inv_freq || !positions || total <= 0 || (!q && !k) || !q != !q_out || !k != !k_out) return LSERVE_ERR_INVALID_ARG;
-    if (rotary->rotary_dim < 2 || rotary->rotary_dim % 2 != 0) return LSERVE_ERR_INVALID_ARG;
-    if (!(rotary->scale >= 0.f) || std::isinf(rotary->scale) || (rotary->interleaved != 0 && rotary->interleaved != 1))
-        return LSERVE_ERR_INVALID_ARG;
+    if (!rotary || !rotary_is_fine(rotary) || !positions || total <= 0 || (!q && !k) || !q != !q_out || !k != !k_out) return LSERVE_ERR_INVALID_ARG;
     if (rotary->rotary_dim > kHeadDim) return LSERVE_ERR_UNSUPPORTED;
     const int64_t q_row = (int64_t)lp.H * kHeadDim, k_row = (int64_t)lp.Hkv * kHeadDim;
     if (q && (q_stride < q_row || q_stride % 8 != 0 || (q_out == q && q_stride != q_row))) return LSERVE_ERR_INVALID_ARG;
     if (k && (k_stride < k_row || k_stride % 8 != 0 || (k_out == k && k_stride != k_row))) return LSERVE_ERR_INVALID_ARG;
-    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(positions) || !aligned16(rotary->inv_freq))
-        return LSERVE_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(positions)) return LSERVE_ERR_INVALID_ARG;
     // (outputs are whole, inputs rows that may lie apart; in place a row is read before it is written)
     const Rows q_in = {q, q_row * 2, q_stride * 2, total}, k_in = {k, k_row * 2, k_stride * 2, total};
     const Range q_to = {q_out, total * q_row * 2}, k_to = {k_out, total * k_row * 2}, at = {positions, total * 4LL},
@@ -697,7 +693,7 @@ int lserve_rotary_axes(const lserve_attn_desc* desc, const lserve_rotary_desc* r
     if (rc) return rc;
     if (!rotary || !axes) return LSERVE_ERR_INVALID_ARG;
     TurnArgs turn = {};
-    rc = make_turn(lp, nullptr, rotary, axes, positions, positions_stride, total, false, &turn);
+    rc = make_turn(nullptr, rotary, axes, positions, positions_stride, total, false, &turn);
     return rc ? rc : turned_rows(desc, lp, turn, q, k, total, q_stride, k_stride, q_out, k_out, stream);
 }
 
@@ -709,7 +705,7 @@ int lserve_norm_rotary(const lserve_attn_desc* desc, const lserve_head_norm* nor
     if (rc) return rc;
     if (!norm) return LSERVE_ERR_INVALID_ARG;
     TurnArgs turn = {};
-    rc = make_turn(lp, norm, rotary, axes, positions, positions_stride, total, false, &turn);
+    rc = make_turn(norm, rotary, axes, positions, positions_stride, total, false, &turn);
     return rc ? rc : turned_rows(desc, lp, turn, q, k, total, q_stride, k_stride, q_out, k_out, stream);
 }
 
@@ -724,7 +720,7 @@ int lserve_rotary_append_kv(const lserve_attn_desc* desc, const lserve_paged_kv*
     rc = make_paged(kv, a.lp, true, true, selecting > 0, true, &a.kv);
     if (rc) return rc;
     if (!k || !v || !q != !q_out || !cu_new || !start_pos || total_new <= 0 || max_new_per_seq <= 0) return LSERVE_ERR_INVALID_ARG;
-    rc = make_turn(a.lp, norm, rotary, axes, positions, positions_stride, total_new, true, &a.turn);
+    rc = make_turn(norm, rotary, axes, positions, positions_stride, total_new, true, &a.turn);
     if (rc) return rc;
     const int64_t q_row = (int64_t)a.lp.H * kHeadDim, k_row = (int64_t)a.lp.Hkv * kHeadDim;
     if ((q && !rows_are_fine(q, q_stride, q_row, q_out)) || !rows_are_fine(k, k_stride, k_row, k_out) || !rows_are_fine(v, v_stride, k_row, v_out))

@@ -37,11 +37,6 @@ template <int LAYOUT> __device__ __forceinline__ Pieces pieces_of(int l, int rot
     const int half = rotary_dim / 16;
     return l < half ? Pieces{l, l + half, true} : Pieces{2 * l, 2 * l + 1, false};
 }
-// The lane's eight pairs: 0 .. 3 and 4 .. 7 are, interleaved, those of either piece.
-template <int LAYOUT> __device__ __forceinline__ int pair_of(const Pieces& p, int i) {
-    return LAYOUT == kInterleaved ? (i < 4 ? 4 * p.p0 + i : 4 * p.p1 + i - 4) : 8 * p.p0 + i;
-}
-
 // A lane's weights of a row's norm: of its two pieces.
 struct Weights {
     float x[8], y[8];
@@ -89,7 +84,7 @@ __device__ __forceinline__ float2 turned(float a, float b, float2 turn) {
     return make_float2(__builtin_fmaf(a, turn.x, -(b * turn.y)), __builtin_fmaf(b, turn.x, a * turn.y));
 }
 
-// A lane's two pieces of a row, normed and turned; turn: of its eight pairs.  Channels that do not turn keep their bits without a norm.
+// A lane's two pieces of a row, normed and turned; turn: of its eight pairs (interleaved 0 .. 3 and 4 .. 7 are those of either piece).  Channels that do not turn keep their bits without a norm.
 // kOddHalves: `room` is kHeadDim floats of LDS for the row, its own; turns: (cos, sin) of all pairs of the row's token.
 template <class T, int LAYOUT, bool NORM>
 __device__ __forceinline__ void turn_row(uint32_t (&x)[4], uint32_t (&y)[4], const float2 (&turn)[8], const TurnArgs& t, bool weighted,
