@@ -519,7 +519,7 @@ int lserve_rotary_axes(const lserve_attn_desc *desc, const lserve_rotary_desc *r
 
 /*
  * Norm of every query and key head over its D channels: (x - m) / sqrt(mean((x - m)^2) + eps) * weight, m = 0 or the mean of x.  In fp32
- * throughout: the squares of a row have to add up to less than 2^128.
+ * throughout, the weights too (16-bit ones are converted once, by who loads them): the squares of a row have to add up to less than 2^128.
  */
 #define LSERVE_NORM_RMS 0     /* m = 0 */
 #define LSERVE_NORM_CENTRED 1 /* m = mean(x) */

@@ -1,8 +1,9 @@
 // New tokens on their way from a projection into the paged cache: queries normed and turned, keys normed, turned and written to their pages
 // (16-bit rows or codes) with the key statistics brought up to date, values written next to them.  The cache is left as lserve_append_kv would
 // leave it, handed the turned keys.  Bound: HBM, every row read once, queries and pages written once: 65536 tokens of 32 / 8 heads, 1.62 GB
-// with 16-bit pages, 300 us = 5.4 TB/s (a copy of 671 MiB runs at 5.3); eight of 512 to 8192 into 8-bit pages with dense keys and values kept, 618 MB, 120
-// us; 16 single tokens 4.2 us, which is a launch and the loads of a place, an angle, a row and a page one after the other.
+// with 16-bit pages, 300 us = 5.4 TB/s (a copy of 671 MiB runs at 5.3); eight of 512 to 8192 into 8-bit pages with dense keys and values kept, 618 MB, 120 to
+// 126 us (under the profiler 118 at least, 132 in the median); 16 single tokens 4.1 us, which is a launch and the loads of a place, an angle, a row and a page
+// one after the other, 4.8 into pages of codes.
 #include <algorithm>
 
 #include "quantize.h"
