@@ -559,7 +559,7 @@ int lserve_norm_rotary(const lserve_attn_desc *desc, const lserve_head_norm *nor
  *   positions  device [A][positions_stride] (axes NULL: [total_new]), or NULL: a token's position is start_pos[b] + j on every axis.  Any
  *              numbers: where a token is written does not depend on them, and a negative one turns backwards
  *   cu_new     device [batch + 1] (batch = kv->batch), cu_new[0] = 0; rows from cu_new[batch] on are left alone, here and in all outputs
- *   start_pos  device [batch]; start_pos[b] + n_b <= max_pages_per_seq * N_P (of pages that some head uses) and < 2^31.  kv->seq_lens may be
+ *   start_pos  device [batch]; start_pos[b] + n_b < 2^31 and, unless every head is in the ring, <= max_pages_per_seq * N_P.  kv->seq_lens may be
  *              given; kv->seq_lens itself is not read
  *   total_new  host: rows of q, k and v, and of the outputs
  *   max_new_per_seq  host bound of n_b, > 0; 1 (a decode step) and a few (2, more in larger batches) have a form of their own

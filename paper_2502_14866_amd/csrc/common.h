@@ -46,6 +46,15 @@ template <> struct Elem<BF16> {
     }
 };
 
+// A value with a signalling not-a-number quieted, which the forms of three operands (v_min3, v_max3) would take for the range so far.  (Conversions
+// from fp16 have done so.  Written out: the compiler drops its own form as one that a minimum or maximum makes needless.)
+template <class T> __device__ __forceinline__ float quieted(float x) { return x; }
+template <> __device__ __forceinline__ float quieted<BF16>(float x) {
+    float r;
+    asm("v_max_f32 %0, %1, %1" : "=v"(r) : "v"(x));
+    return r;
+}
+
 // ---- DPP cross-lane primitives (row = 16 consecutive lanes) ------------------------------------
 
 template <int Ctrl> __device__ __forceinline__ float dpp_f(float x) {

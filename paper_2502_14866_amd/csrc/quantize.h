@@ -24,15 +24,6 @@ __device__ __forceinline__ half2_t quiet(uint32_t w) {
     return pk_max(x, x);
 }
 
-// A value with a signalling not-a-number quieted, which the forms of three operands (v_min3, v_max3) would take for the range so far.  (Conversions
-// from fp16 have done so.  Written out: the compiler drops its own form as one that a minimum or maximum makes needless.)
-template <class T> __device__ __forceinline__ float quieted(float x) { return x; }
-template <> __device__ __forceinline__ float quieted<BF16>(float x) {
-    float r;
-    asm("v_max_f32 %0, %1, %1" : "=v"(r) : "v"(x));
-    return r;
-}
-
 // Smallest and largest of eight values (f: the same as numbers); what is not a number gives way.
 template <class T> __device__ __forceinline__ void range8(const uint32_t (&)[4], const float (&f)[8], float& lo, float& hi) {
     lo = hi = quieted<T>(f[0]);

@@ -45,7 +45,7 @@ template <class T> __device__ __forceinline__ void rebuild_rows(const uint4* __r
             const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float a = Elem<T>::lo(w[i]), d = Elem<T>::hi(w[i]);
+                const float a = quieted<T>(Elem<T>::lo(w[i])), d = quieted<T>(Elem<T>::hi(w[i]));
                 vmax[2 * i] = fmaxf(vmax[2 * i], a);
                 vmin[2 * i] = fminf(vmin[2 * i], a);
                 vmax[2 * i + 1] = fmaxf(vmax[2 * i + 1], d);

@@ -102,3 +102,43 @@ def test_a_token_of_nothing_but_not_a_numbers(dtype, at):
             assert (got[0] == -float("inf")).all() and (got[1] == float("inf")).all()
         else:
             assert (got == 3.0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("logical", [8, 16, 64])
+def test_statistics_from_the_pages(dtype, logical):
+    """lserve_build_page_stats and the selector's own rebuild find what lserve_append_kv left."""
+    import paper_2502_14866_amd as L
+
+    L.load_library()
+    g = torch.Generator().manual_seed(logical)
+    desc = L.AttnDesc(4, 2, [0, 0], dtype=dtype, logical_page_size=logical)
+    counts = [130, 1, 64, 77]
+    kv = _cache(L, g, dtype, desc, [0] * 4, counts, 16, False, 64)
+    k = torch.randn((sum(counts), 2, 128), generator=g).to(dtype)
+    row = k.view(torch.int16).view(-1)
+    odd = torch.tensor([0x7c00, 0xfc00, 0x7e00, 0x7c01, 0x7d01, 0x7f80, 0xff80, 0x7fc0, 0x7f81, 0x7fa1, 0xffa1], dtype=torch.int32).to(torch.int16)
+    at = torch.randint(0, row.numel(), (row.numel() // 12,), generator=g)
+    row[at] = odd[torch.randint(0, len(odd), at.shape, generator=g)]
+    cu = torch.tensor([0] + torch.tensor(counts).cumsum(0).tolist(), dtype=torch.int32, device=DEV)
+    L.lserve_append_kv(desc, kv, k.to(DEV), k.to(DEV), cu, kv.seq_lens, max(counts))
+    torch.cuda.synchronize()
+    want = kv.stats.clone()
+    kv.seq_lens = torch.tensor(counts, dtype=torch.int32, device=DEV)
+    used = torch.zeros(kv.stats.shape[:3], dtype=torch.bool, device=DEV)
+    for b, n in enumerate(counts):
+        for first in range(0, n, logical):
+            used[kv.page_table[b, first // 64].long(), :, first % 64 // logical] = True
+    none = torch.zeros(4, dtype=torch.int32, device=DEV)
+    q = torch.randn((4, 4, 128), generator=g).to(dtype).to(DEV)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=DEV)  # noqa: E731
+    workspace = torch.zeros(L.lserve_workspace_bytes(1, desc, 4, kv.page_table.shape[1], 2, 0) + 16, dtype=torch.uint8, device=DEV)
+    for rebuild in ("call", "selector"):
+        kv.stats.zero_()
+        if rebuild == "call":
+            L.lserve_build_page_stats(desc, kv, None, 0)
+        else:
+            L.lserve_select_pages(desc, kv, q, 128, i32(4, 2, 2), i32(4, 2), i32(4), None, workspace, stats_valid_len=none)
+        torch.cuda.synchronize()
+        # (as numbers: the larger of zeros of both signs is either)
+        assert torch.equal(kv.stats[used].float(), want[used].float()), rebuild
