@@ -10,6 +10,7 @@
 // with a 4-pass radix select.  Both emit in index order, so the output is ascending and ties resolve
 // to the lower page index.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -27,9 +28,9 @@ __device__ __forceinline__ unsigned orderable(float s) {
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Max and min rows of a logical page of `cnt` tokens, from its keys: this lane's eight channels.
-template <class T> __device__ __forceinline__ void rebuild_rows(const uint4* __restrict__ keys, int cnt, uint4& mx, uint4& mn) {
-    float vmax[8], vmin[8];
+// Channel-wise max and min of `cnt` keys, this lane's eight channels, by the functions that are given.
+template <class T, class Larger, class Smaller>
+__device__ __forceinline__ void fold_rows(const uint4* __restrict__ keys, int cnt, float (&vmax)[8], float (&vmin)[8], Larger larger, Smaller smaller) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         vmax[i] = -INFINITY;
@@ -45,13 +46,32 @@ template <class T> __device__ __forceinline__ void rebuild_rows(const uint4* __r
             const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float a = quieted<T>(Elem<T>::lo(w[i])), d = quieted<T>(Elem<T>::hi(w[i]));
-                vmax[2 * i] = fmaxf(vmax[2 * i], a);
-                vmin[2 * i] = fminf(vmin[2 * i], a);
-                vmax[2 * i + 1] = fmaxf(vmax[2 * i + 1], d);
-                vmin[2 * i + 1] = fminf(vmin[2 * i + 1], d);
+                const float a = Elem<T>::lo(w[i]), d = Elem<T>::hi(w[i]);
+                vmax[2 * i] = larger(vmax[2 * i], a);
+                vmin[2 * i] = smaller(vmin[2 * i], a);
+                vmax[2 * i + 1] = larger(vmax[2 * i + 1], d);
+                vmin[2 * i + 1] = smaller(vmin[2 * i + 1], d);
             }
         }
+    }
+}
+
+// Max and min rows of a logical page of `cnt` tokens, from its keys: this lane's eight channels.  What is not a number takes no part.  fp16: conversions quiet it, and the
+// forms that leave it out do the rest.  bf16: first by the forms that such a value turns into one of their result; where there was one, once more by those that
+// leave it out, which want every value quieted (200 tokens of 16 sequences: 13.6 us that way throughout, 13.1 this way).
+template <class T> __device__ __forceinline__ void rebuild_rows(const uint4* __restrict__ keys, int cnt, uint4& mx, uint4& mn) {
+    float vmax[8], vmin[8];
+    auto larger = [](float a, float b) { return fmaxf(a, quieted<T>(b)); };
+    auto smaller = [](float a, float b) { return fminf(a, quieted<T>(b)); };
+    if constexpr (std::is_same_v<T, F16>) {
+        fold_rows<T>(keys, cnt, vmax, vmin, larger, smaller);
+    } else {
+        fold_rows<T>(keys, cnt, vmax, vmin, [](float a, float b) { return __builtin_elementwise_maximum(a, b); },
+                     [](float a, float b) { return __builtin_elementwise_minimum(a, b); });
+        float largest = vmax[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) largest = __builtin_elementwise_maximum(largest, vmax[i]);
+        if (__ballot(largest != largest) != 0) fold_rows<T>(keys, cnt, vmax, vmin, larger, smaller);
     }
     mx = make_uint4(Elem<T>::pack(vmax[0], vmax[1]), Elem<T>::pack(vmax[2], vmax[3]),
                     Elem<T>::pack(vmax[4], vmax[5]), Elem<T>::pack(vmax[6], vmax[7]));
