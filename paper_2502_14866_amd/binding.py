@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 import warnings
 from dataclasses import dataclass
@@ -819,6 +820,15 @@ def lserve_rotary(desc: AttnDesc, rotary: RotaryDesc, q: Optional[torch.Tensor],
            "lserve_rotary")
 
 
+@functools.lru_cache(maxsize=256)
+def _axes_of_pairs(pairs: bytes):
+    """The library's list of axes: it reads rotary_dim / 2 of them, 64 at most, and what is not named here is no axis.  Kept for the lists that a program has, so
+    that a description made for a single call does not take its list with it."""
+    axes = (ctypes.c_uint8 * max(64, len(pairs)))(*([255] * 64))
+    axes[:len(pairs)] = pairs
+    return axes
+
+
 class PositionAxes:
     """Mirror of lserve_position_axes: the axis of each of a head's rotary_dim / 2 pairs (num_axes: as many as are named).  Stays as it was made."""
 
@@ -826,10 +836,7 @@ class PositionAxes:
         pairs = [int(a) for a in pair_axis]
         if not pairs or min(pairs) < 0 or max(pairs) > 255:
             raise ValueError("PositionAxes: an axis for every pair")
-        # (the library reads rotary_dim / 2 of them, 64 at most; what is not named here is no axis)
-        self._pairs = len(pairs)
-        self._axes = (ctypes.c_uint8 * max(64, len(pairs)))(*([255] * 64))
-        self._axes[:len(pairs)] = pairs
+        self._pairs, self._axes = len(pairs), _axes_of_pairs(bytes(pairs))
         self._c = _CPositionAxes(num_axes or max(pairs) + 1, ctypes.cast(self._axes, ctypes.POINTER(ctypes.c_uint8)))
         self._address = ctypes.addressof(self._c)
 

@@ -1,5 +1,7 @@
 """Descriptions of how heads are normed and turned, changed after they were made: the next call works with what they say now, or the change is refused.  And
 a session's call of the same arguments."""
+import ctypes
+
 import pytest
 import torch
 
@@ -124,3 +126,14 @@ def test_a_session_s_rows_without_queries(monkeypatch, route):
         out = s.append_rotary(rot, t["qn"], t["kn"], t["vn"], t["cu"], t["start"], 3)
     assert out.shape == t["qn"].shape and [x[0] for x in seen] == ["lserve_rotary_append_kv"] * 2
     assert seen[0][6] is None and seen[0][18:20] == (None, t["ko"].data_ptr()) and seen[1][6] == t["qn"].data_ptr() and seen[1][18] == out.data_ptr()
+
+
+def test_a_list_of_axes_outlives_its_description():
+    """What was handed over of a description made for one call alone is still the list when that description is gone."""
+    import gc
+
+    where = ctypes.cast(L.PositionAxes([2, 1, 0, 1] * 8)._c.pair_axis, ctypes.c_void_p).value
+    gc.collect()
+    others = [L.PositionAxes([1] * n) for n in range(1, 65)]
+    assert list((ctypes.c_uint8 * 33).from_address(where)) == [2, 1, 0, 1] * 8 + [255]
+    assert all(a.pair_axis == [1] * n for n, a in enumerate(others, 1))
